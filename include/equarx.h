@@ -370,6 +370,158 @@ int equarx_reduce_variant_hops_strided(const void *const *partials_bf16, int32_t
                                        uint32_t flags, void *out_bf16, void *workspace, size_t workspace_bytes,
                                        void *stream);
 
+/*
+ * Microscaled 4-bit numbers and their product: the row-parallel layers whose
+ * partial sums the calls above reduce.
+ *
+ * A row of `cols` elements is cut into blocks of 32 that share a scale
+ * 2^(s - 127), one byte s; an element is 4 bits, a sign and one of 0, 0.5, 1,
+ * 1.5, 2, 3, 4, 6 (the formats E8M0 and E2M1 of the OCP microscaling
+ * specification).  s - 127 is the exponent of the block's largest magnitude
+ * less two (0 for zeros, and for exponents that would need less than 0); an
+ * element is the nearest of the eight magnitudes to |x| / 2^(s - 127), ties to
+ * the even code, from 6 on 6.  A block with a NaN or an infinity has s = 255
+ * and reads back as NaN.
+ *
+ *   codes    uint8 [rows][16 * equarx_mx4_row_blocks(cols)], the first element
+ *            of a pair in a byte's low half;
+ *   scales   uint8 [rows][equarx_mx4_row_blocks(cols)].
+ * Rows are padded to whole groups of EQUARX_MX4_GROUP elements, 4 blocks; the
+ * padding holds zero elements and is written by equarx_mx4_quantize.
+ *
+ * Limits of all calls here: rows, cols, M, N and K up to 2^31 - 1, and every
+ * tensor up to 2^40 elements (EQUARX_BAD_SHAPE).  A row stride counts elements,
+ * is at least the row's length, and need be a multiple of nothing.
+ */
+#define EQUARX_MX4_BLOCK 32
+#define EQUARX_MX4_GROUP 128
+
+/* Blocks of a padded row: 4 * ceil(cols / 128) (0 for invalid arguments). */
+int64_t equarx_mx4_row_blocks(int64_t cols);
+
+/* bf16 x [rows][cols], row i at x + i * x_stride -> codes, scales. */
+int equarx_mx4_quantize(const void *x_bf16, int64_t rows, int64_t cols, int64_t x_stride,
+                        uint8_t *codes, uint8_t *scales, void *stream);
+
+/* codes, scales -> bf16 out [rows][cols], row i at out + i * out_stride: exactly
+ * the values that the elements stand for. */
+int equarx_mx4_dequantize(const uint8_t *codes, const uint8_t *scales, int64_t rows, int64_t cols,
+                          void *out_bf16, int64_t out_stride, void *stream);
+
+/*
+ * out[m][n] = bf16(sum over k of x[m][k] * w[n][k]), summed in fp32: x [M][K]
+ * and w [N][K] are packed rows, out is bf16 [M][N] with row m at
+ * out + m * out_stride.  K == 0 gives zeros.  A NaN block makes its row's (its column's)
+ * outputs NaN.  The order of the sum depends on the shape alone.
+ *
+ * equarx_mx4_linear takes x as bf16 [M][K] (row m at x + m * x_stride) and
+ * quantizes it as equarx_mx4_quantize does: same bits as the two calls.
+ *
+ *   workspace   device, equarx_mx4_workspace_bytes(M, N, K) bytes for either
+ *               call, 256-byte aligned (may be NULL where that is 0); nothing
+ *               in it needs clearing.
+ * No output may overlap another buffer of the call (EQUARX_BAD_SHAPE).
+ */
+int equarx_mx4_product(const uint8_t *x_codes, const uint8_t *x_scales, const uint8_t *w_codes, const uint8_t *w_scales,
+                       int64_t M, int64_t N, int64_t K, void *out_bf16, int64_t out_stride,
+                       void *workspace, size_t workspace_bytes, void *stream);
+int equarx_mx4_linear(const void *x_bf16, int64_t x_stride, const uint8_t *w_codes, const uint8_t *w_scales,
+                      int64_t M, int64_t N, int64_t K, void *out_bf16, int64_t out_stride,
+                      void *workspace, size_t workspace_bytes, void *stream);
+size_t equarx_mx4_workspace_bytes(int64_t M, int64_t N, int64_t K);
+
+/*
+ * A key/value cache in the block-wise int8 form of equarx_quantize, and the
+ * attention that reads it.
+ *
+ * The cache is a pool of `pages` pages of `page` token slots; slot
+ * p * page + i is entry i of page p.  A token has `heads` keys and as many
+ * values of `dim` elements, each cut into dim / block blocks with one scale.
+ *
+ *   k_codes    int8 [pages][heads][page][dim]
+ *   v_codes    int8 [pages][heads][page / 16][dim][16]: the 16 tokens of a
+ *              group are together, as the sum over tokens wants them
+ *   k_scales, v_scales   fp32 [pages][heads][dim / block][page]
+ *   dim        64, 128 or 256; block 64, 128 or 256, at most dim
+ *              (EQUARX_BAD_BLOCK); page a multiple of 16, at most 65536; heads at most
+ *              65535; the codes of one of the two up to 2^40.
+ * A block with a NaN or an infinity has scale NaN; otherwise codes and scales
+ * are those of equarx_quantize.
+ *
+ * Sequence b of a call is the first lengths[b] tokens of the pages
+ * page_table[b][0], page_table[b][1], ...: page_table int32
+ * [sequences][table_width] and lengths int32 [sequences] on the device.
+ * (Arrays of numbers -- tables, lengths, starts, slots -- need only their
+ * elements' alignment.)  Lengths below 0 count as 0, lengths beyond the table as its end.  A page
+ * number outside [0, pages) holds no tokens: attention does not see them,
+ * reading back gives zeros.
+ */
+typedef struct equarx_cache {
+    int8_t *k_codes;
+    float *k_scales;
+    int8_t *v_codes;
+    float *v_scales;
+    int64_t pages;
+    int32_t heads, page, dim, block;
+} equarx_cache;
+
+/*
+ * Quantize `tokens` new tokens into their slots: k and v bf16, element
+ * [t][h][d] at t * row_stride + h * head_stride + d, strides multiples of 8 in
+ * elements; slots int64 [tokens] on the device, slots outside the pool are
+ * skipped.  Two tokens of one call must not share a slot.
+ */
+int equarx_cache_write(const equarx_cache *cache, const void *k_bf16, int64_t k_row_stride, int64_t k_head_stride,
+                       const void *v_bf16, int64_t v_row_stride, int64_t v_head_stride, int64_t tokens,
+                       const int64_t *slots, void *stream);
+
+/*
+ * Read sequences back: token t of sequence b goes, as bf16(code * scale), to row
+ * starts[b] + t of k_out and v_out, bf16 [rows][heads][dim] both.  starts int32
+ * [sequences] on the device; rows outside [0, rows) are not written.
+ * max_length: the longest sequence, as far as the host knows; it sizes the launch and
+ * changes no result.
+ */
+int equarx_cache_read(const equarx_cache *cache, const int32_t *page_table, int64_t table_width, const int32_t *lengths,
+                      const int32_t *starts, int32_t sequences, int64_t max_length, int64_t rows, void *k_out,
+                      void *v_out, void *stream);
+
+/*
+ * Softmax attention over cached sequences.  Sequence b has the query rows
+ * q_starts[b] .. q_starts[b + 1] - 1 (q_starts int32 [sequences + 1] on the
+ * device, not decreasing, within [0, q_rows]) of q, bf16 with element
+ * [r][h][d] at r * q_row_stride + h * q_head_stride + d, strides multiples of 8.
+ * q_heads is a multiple of cache->heads; query head h reads key head
+ * h / (q_heads / heads).
+ *
+ *   s_t = scale * sum_d q_d k_td,   lse = log sum_t exp(s_t),
+ *   out = sum_t exp(s_t - lse) v_t
+ * over the tokens t that the row sees, with k and v the codes times their scales,
+ * unrounded.  Sums and statistics are fp32; the products exp(..) * v scale
+ * are rounded to bf16 before they meet the codes.
+ *
+ *   flags    EQUARX_CAUSAL: query i of n sees token t of L if t <= L - n + i
+ *            (its own token is in the cache already); without it, all.
+ *   window   0, or with EQUARX_CAUSAL also t > L - n + i - window.
+ * A row that sees nothing has out 0 and lse -inf.
+ *
+ *   out [q_rows][q_heads][dim] bf16, lse fp32 [q_rows][q_heads] or NULL; rows of
+ *   no sequence are not written.
+ *   max_queries, max_length   the longest query run and sequence, as far as
+ *            the host knows (>= 1): they size the launch and choose how a long context
+ *            is split, and hence the order of the sums; larger actual values cost time, not correctness.
+ *   workspace  equarx_cache_attention_workspace_bytes(...) bytes, 256-byte
+ *            aligned (may be NULL where that is 0); nothing in it needs clearing.
+ */
+#define EQUARX_CAUSAL 1u
+int equarx_cache_attention(const equarx_cache *cache, const void *q_bf16, int64_t q_rows, int32_t q_heads,
+                           int64_t q_row_stride, int64_t q_head_stride, const int32_t *q_starts,
+                           const int32_t *page_table, int64_t table_width, const int32_t *lengths, int32_t sequences,
+                           float scale, int32_t max_queries, int64_t max_length, uint32_t flags, int32_t window,
+                           void *out_bf16, float *lse, void *workspace, size_t workspace_bytes, void *stream);
+size_t equarx_cache_attention_workspace_bytes(int32_t heads, int32_t dim, int64_t q_rows, int32_t q_heads,
+                                              int32_t sequences, int32_t max_queries, int64_t max_length);
+
 /* Bytes of workspace equarx_reduce_quantized needs (0 for invalid arguments). */
 size_t equarx_workspace_bytes(int32_t P, int64_t n, int32_t block);
 

@@ -14,6 +14,7 @@ import ctypes
 import importlib.util
 import os
 import warnings
+from typing import NamedTuple
 
 import torch
 
@@ -69,6 +70,13 @@ MAX_PARTIALS = 64
 BLOCK_SIZES = (32, 64, 128, 256, 512)
 SEMI_LOOP, RS_UNQUANTIZED, AG_UNQUANTIZED, RING_ORDER = 1, 2, 4, 8
 
+class _CCache(ctypes.Structure):
+    """equarx_cache of include/equarx.h."""
+    _fields_ = [("k_codes", ctypes.c_void_p), ("k_scales", ctypes.c_void_p), ("v_codes", ctypes.c_void_p),
+                ("v_scales", ctypes.c_void_p), ("pages", ctypes.c_int64), ("heads", ctypes.c_int32), ("page", ctypes.c_int32),
+                ("dim", ctypes.c_int32), ("block", ctypes.c_int32)]
+
+
 # name -> (restype, argtypes); SIGNATURES mirrors include/equarx.h, DEVTOOLS_SIGNATURES include/equarx_devtools.h
 _vp, _i64, _i32, _sz = ctypes.c_void_p, ctypes.c_int64, ctypes.c_int32, ctypes.c_size_t
 SIGNATURES = {
@@ -94,6 +102,17 @@ SIGNATURES = {
     "equarx_reduce_variant_strided": (ctypes.c_int, [ctypes.POINTER(_vp), _i32, _i64, _i32, ctypes.c_uint32, _vp, _vp]),
     "equarx_reduce_variant_hops_strided": (ctypes.c_int, [ctypes.POINTER(_vp), _i32, _i64, _i32, ctypes.c_uint32, _vp, _vp,
                                                           _sz, _vp]),
+    "equarx_mx4_row_blocks": (_i64, [_i64]),
+    "equarx_mx4_quantize": (ctypes.c_int, [_vp, _i64, _i64, _i64, _vp, _vp, _vp]),
+    "equarx_mx4_dequantize": (ctypes.c_int, [_vp, _vp, _i64, _i64, _vp, _i64, _vp]),
+    "equarx_mx4_product": (ctypes.c_int, [_vp, _vp, _vp, _vp, _i64, _i64, _i64, _vp, _i64, _vp, _sz, _vp]),
+    "equarx_mx4_linear": (ctypes.c_int, [_vp, _i64, _vp, _vp, _i64, _i64, _i64, _vp, _i64, _vp, _sz, _vp]),
+    "equarx_mx4_workspace_bytes": (_sz, [_i64, _i64, _i64]),
+    "equarx_cache_write": (ctypes.c_int, [ctypes.POINTER(_CCache), _vp, _i64, _i64, _vp, _i64, _i64, _i64, _vp, _vp]),
+    "equarx_cache_read": (ctypes.c_int, [ctypes.POINTER(_CCache), _vp, _i64, _vp, _vp, _i32, _i64, _i64, _vp, _vp, _vp]),
+    "equarx_cache_attention": (ctypes.c_int, [ctypes.POINTER(_CCache), _vp, _i64, _i32, _i64, _i64, _vp, _vp, _i64, _vp, _i32,
+                                              ctypes.c_float, _i32, _i64, ctypes.c_uint32, _i32, _vp, _vp, _vp, _sz, _vp]),
+    "equarx_cache_attention_workspace_bytes": (_sz, [_i32, _i32, _i64, _i32, _i32, _i32, _i64]),
     "equarx_workspace_bytes": (_sz, [_i32, _i64, _i32]),
     "equarx_num_blocks": (_i64, [_i64, _i32]),
     "equarx_wire_row_codes": (_i64, [_i64]),
@@ -516,6 +535,218 @@ def equarx_reduce_variant_hops_strided(partials, chunks: int, flags: int, out_bf
     _check(load().equarx_reduce_variant_hops_strided(table, P, n, chunks, flags, _ptr(out_bf16), _ptr(workspace),
                                                      workspace.numel() * workspace.element_size(), _stream()),
            "equarx_reduce_variant_hops_strided")
+
+
+def mx4_row_blocks(cols: int) -> int:
+    return int(load().equarx_mx4_row_blocks(cols))
+
+
+def alloc_mx4(rows: int, cols: int, device="cuda"):
+    """Buffers for the packed form of [rows, cols]: codes uint8 [rows, 16 * blocks], scales uint8 [rows, blocks]."""
+    blocks = mx4_row_blocks(cols)
+    return (torch.empty((rows, 16 * blocks), dtype=torch.uint8, device=device),
+            torch.empty((rows, blocks), dtype=torch.uint8, device=device))
+
+
+def alloc_mx4_workspace(M: int, N: int, K: int, device="cuda") -> torch.Tensor:
+    """What equarx_mx4_linear and equarx_mx4_product need beside their operands."""
+    return torch.empty(max(int(load().equarx_mx4_workspace_bytes(M, N, K)), 256), dtype=torch.uint8, device=device)
+
+
+def _need_rows(t, dims: int, what: str):
+    """A bf16 CUDA tensor of `dims` dimensions, the last one contiguous, and the strides of the others."""
+    if t is None or not t.is_cuda or t.dtype != torch.bfloat16 or t.dim() != dims or (t.shape[-1] > 1 and t.stride(-1) != 1):
+        raise ValueError(f"{what}: need a CUDA torch.bfloat16 tensor of {dims} dimensions, the last one contiguous")
+    cols = t.shape[-1]
+    head = t.stride(1) if dims == 3 and t.shape[1] > 1 else cols
+    row = t.stride(0) if t.shape[0] > 1 else t.shape[1] * cols if dims == 3 else cols
+    return row, head
+
+
+def _need_packed(codes, scales, rows: int, cols: int, what: str) -> None:
+    blocks = mx4_row_blocks(cols)
+    for t, width in ((codes, 16 * blocks), (scales, blocks)):
+        if t is None or not t.is_cuda or t.dtype != torch.uint8 or not t.is_contiguous() or tuple(t.shape) != (rows, width):
+            raise ValueError(f"{what}: need contiguous CUDA torch.uint8 codes [{rows}, {16 * blocks}] and scales [{rows}, {blocks}]")
+
+
+def _need_workspace(workspace) -> int:
+    if workspace is None:
+        return 0
+    if not (workspace.is_cuda and workspace.is_contiguous()):
+        raise ValueError("workspace: need a contiguous CUDA tensor")
+    return workspace.numel() * workspace.element_size()
+
+
+def equarx_mx4_quantize(x, codes, scales) -> None:
+    """codes, scales <- the 4-bit microscaled form of bf16 x [rows, cols] (any row stride)."""
+    status = _native.equarx_mx4_quantize(x, codes, scales)
+    if status >= 0:
+        return _check(status, "equarx_mx4_quantize")
+    stride, _ = _need_rows(x, 2, "x_bf16")
+    rows, cols = x.shape
+    _need_packed(codes, scales, rows, cols, "packed x")
+    _check(load().equarx_mx4_quantize(_ptr(x), rows, cols, stride, _ptr(codes), _ptr(scales), _stream()), "equarx_mx4_quantize")
+
+
+def equarx_mx4_dequantize(codes, scales, out_bf16) -> None:
+    """out_bf16 [rows, cols] (any row stride) <- the values that packed rows stand for."""
+    status = _native.equarx_mx4_dequantize(codes, scales, out_bf16)
+    if status >= 0:
+        return _check(status, "equarx_mx4_dequantize")
+    stride, _ = _need_rows(out_bf16, 2, "out_bf16")
+    rows, cols = out_bf16.shape
+    _need_packed(codes, scales, rows, cols, "packed rows")
+    _check(load().equarx_mx4_dequantize(_ptr(codes), _ptr(scales), rows, cols, _ptr(out_bf16), stride, _stream()),
+           "equarx_mx4_dequantize")
+
+
+def equarx_mx4_product(x_codes, x_scales, w_codes, w_scales, K: int, out_bf16, workspace=None) -> None:
+    """out_bf16 [M, N] <- x [M, K] w [N, K]^T, both packed."""
+    status = _native.equarx_mx4_product(x_codes, x_scales, w_codes, w_scales, K, out_bf16, workspace)
+    if status >= 0:
+        return _check(status, "equarx_mx4_product")
+    stride, _ = _need_rows(out_bf16, 2, "out_bf16")
+    M, N = out_bf16.shape
+    if not isinstance(K, int) or K < 0:
+        raise ValueError("K: need an int that is not negative")
+    _need_packed(x_codes, x_scales, M, K, "packed x")
+    _need_packed(w_codes, w_scales, N, K, "packed w")
+    nbytes = _need_workspace(workspace)
+    _check(load().equarx_mx4_product(_ptr(x_codes), _ptr(x_scales), _ptr(w_codes), _ptr(w_scales), M, N, K, _ptr(out_bf16),
+                                     stride, _ptr(workspace), nbytes, _stream()), "equarx_mx4_product")
+
+
+def equarx_mx4_linear(x, w_codes, w_scales, out_bf16, workspace=None) -> None:
+    """out_bf16 [M, N] <- x [M, K] w [N, K]^T with x bf16, quantized in the call: a row-parallel layer's partial sum."""
+    status = _native.equarx_mx4_linear(x, w_codes, w_scales, out_bf16, workspace)
+    if status >= 0:
+        return _check(status, "equarx_mx4_linear")
+    x_stride, _ = _need_rows(x, 2, "x_bf16")
+    out_stride, _ = _need_rows(out_bf16, 2, "out_bf16")
+    (M, K), N = x.shape, out_bf16.shape[1]
+    if out_bf16.shape[0] != M:
+        raise ValueError("x_bf16 and out_bf16 differ in rows")
+    _need_packed(w_codes, w_scales, N, K, "packed w")
+    nbytes = _need_workspace(workspace)
+    _check(load().equarx_mx4_linear(_ptr(x), x_stride, _ptr(w_codes), _ptr(w_scales), M, N, K, _ptr(out_bf16), out_stride,
+                                    _ptr(workspace), nbytes, _stream()), "equarx_mx4_linear")
+
+
+class Cache(NamedTuple):
+    """The buffers of a key/value cache: k_codes int8 [pages, heads, page, dim], k_scales fp32 [pages, heads, dim / block,
+    page], v_codes int8 [pages, heads, page / 16, dim, 16], v_scales as k_scales."""
+    k_codes: torch.Tensor
+    k_scales: torch.Tensor
+    v_codes: torch.Tensor
+    v_scales: torch.Tensor
+
+
+def alloc_cache(pages: int, heads: int, page: int, dim: int, block: int, device="cuda") -> Cache:
+    """A cache that holds zeros."""
+    zeros = lambda *shape, dtype: torch.zeros(shape, dtype=dtype, device=device)
+    return Cache(zeros(pages, heads, page, dim, dtype=torch.int8), zeros(pages, heads, dim // block, page, dtype=torch.float32),
+                 zeros(pages, heads, page // 16, dim, 16, dtype=torch.int8),
+                 zeros(pages, heads, dim // block, page, dtype=torch.float32))
+
+
+def _need_cache(cache):
+    """The C structure of a Cache whose tensors have the shapes they should have."""
+    kc, ks, vc, vs = cache
+    good = kc.dim() == 4 and ks.dim() == 4 and ks.shape[2] > 0 and kc.shape[3] % ks.shape[2] == 0
+    if good:
+        pages, heads, page, dim = kc.shape
+        scales = (pages, heads, ks.shape[2], page)
+        good = (tuple(ks.shape) == scales and tuple(vs.shape) == scales and page % 16 == 0
+                and tuple(vc.shape) == (pages, heads, page // 16, dim, 16) and kc.numel() > 0)
+    good = good and all(t.is_cuda and t.is_contiguous() and t.dtype == (torch.float32 if i % 2 else torch.int8)
+                        for i, t in enumerate(cache))
+    if not good:
+        raise ValueError("cache: need contiguous CUDA tensors of the shapes and types that alloc_cache makes")
+    return _CCache(_ptr(kc), _ptr(ks), _ptr(vc), _ptr(vs), pages, heads, page, dim, dim // ks.shape[2])
+
+
+def _need_sequences(page_table, lengths) -> None:
+    for t, what, dims in ((page_table, "page_table", 2), (lengths, "lengths", 1)):
+        if t is None or not t.is_cuda or t.dtype != torch.int32 or not t.is_contiguous() or t.dim() != dims:
+            raise ValueError(f"{what}: need a contiguous CUDA torch.int32 tensor of {dims} dimensions")
+    if lengths.numel() != page_table.shape[0]:
+        raise ValueError("page_table and lengths differ in sequences")
+
+
+def equarx_cache_write(cache: Cache, k, v, slots) -> None:
+    """Quantize k, v bf16 [tokens, heads, dim] (strided views welcome) into the slots int64 [tokens] of a cache."""
+    status = _native.equarx_cache_write(cache, k, v, slots)
+    if status >= 0:
+        return _check(status, "equarx_cache_write")
+    c = _need_cache(cache)
+    strides = []
+    for t, what in ((k, "k_bf16"), (v, "v_bf16")):
+        strides.append(_need_rows(t, 3, what))
+        if t.shape[0] != k.shape[0] or tuple(t.shape[1:]) != (c.heads, c.dim):
+            raise ValueError(f"{what}: need [tokens, {c.heads}, {c.dim}]")
+    _need(slots, torch.int64, k.shape[0], "slots")
+    if slots.numel() != k.shape[0]:
+        raise ValueError("one slot for every token")
+    _check(load().equarx_cache_write(ctypes.byref(c), _ptr(k), *strides[0], _ptr(v), *strides[1], k.shape[0], _ptr(slots),
+                                     _stream()), "equarx_cache_write")
+
+
+def equarx_cache_read(cache: Cache, page_table, lengths, starts, k_out, v_out, max_length=None) -> None:
+    """Sequences back as bf16: token t of sequence b to row starts[b] + t of k_out and v_out [rows, heads, dim]."""
+    if max_length is None:
+        max_length = page_table.shape[-1] * cache[0].shape[2]
+    status = _native.equarx_cache_read(cache, page_table, lengths, starts, k_out, v_out, max_length)
+    if status >= 0:
+        return _check(status, "equarx_cache_read")
+    c = _need_cache(cache)
+    _need_sequences(page_table, lengths)
+    sequences, width = page_table.shape
+    _need(starts, torch.int32, sequences, "starts")
+    for t, what in ((k_out, "k_out"), (v_out, "v_out")):
+        if (t is None or not t.is_cuda or t.dtype != torch.bfloat16 or not t.is_contiguous() or t.dim() != 3
+                or tuple(t.shape) != (k_out.shape[0], c.heads, c.dim)):
+            raise ValueError(f"{what}: need a contiguous CUDA torch.bfloat16 tensor [rows, {c.heads}, {c.dim}]")
+    _check(load().equarx_cache_read(ctypes.byref(c), _ptr(page_table), width, _ptr(lengths), _ptr(starts), sequences, max_length,
+                                    k_out.shape[0], _ptr(k_out), _ptr(v_out), _stream()), "equarx_cache_read")
+
+
+def alloc_cache_attention_workspace(cache: Cache, q_rows: int, q_heads: int, sequences: int, max_queries: int, max_length: int,
+                                    device="cuda") -> torch.Tensor:
+    heads, dim = cache[0].shape[1], cache[0].shape[3]
+    nbytes = load().equarx_cache_attention_workspace_bytes(heads, dim, q_rows, q_heads, sequences, max_queries, max_length)
+    return torch.empty(max(int(nbytes), 256), dtype=torch.uint8, device=device)
+
+
+def equarx_cache_attention(cache: Cache, q, q_starts, page_table, lengths, out, scale: float, max_queries: int, max_length: int,
+                           causal: bool = True, window: int = 0, lse=None, workspace=None) -> None:
+    """out [q_rows, q_heads, dim] <- softmax attention of q [q_rows, q_heads, dim] over cached sequences; sequence b has the
+    query rows q_starts[b] .. q_starts[b + 1] - 1, the last of which stands at its last token."""
+    status = _native.equarx_cache_attention(cache, q, q_starts, page_table, lengths, out, scale, max_queries, max_length, causal,
+                                            window, lse, workspace)
+    if status >= 0:
+        return _check(status, "equarx_cache_attention")
+    c = _need_cache(cache)
+    row, head = _need_rows(q, 3, "q_bf16")
+    q_rows, q_heads, dim = q.shape
+    if dim != c.dim:
+        raise ValueError(f"q_bf16: need heads of {c.dim} elements")
+    _need_sequences(page_table, lengths)
+    sequences, width = page_table.shape
+    _need(q_starts, torch.int32, sequences + 1, "q_starts")
+    if q_starts.numel() != sequences + 1:
+        raise ValueError("q_starts: need one entry more than there are sequences")
+    if out is None or not out.is_cuda or out.dtype != torch.bfloat16 or not out.is_contiguous() or out.shape != q.shape:
+        raise ValueError("out: need a contiguous CUDA torch.bfloat16 tensor of q's shape")
+    if lse is not None:
+        _need(lse, torch.float32, q_rows * q_heads, "lse")
+        if lse.numel() != q_rows * q_heads:
+            raise ValueError("lse: need one entry for every row and head of q")
+    nbytes = _need_workspace(workspace)
+    _check(load().equarx_cache_attention(ctypes.byref(c), _ptr(q), q_rows, q_heads, row, head, _ptr(q_starts), _ptr(page_table),
+                                         width, _ptr(lengths), sequences, float(scale), max_queries, max_length,
+                                         1 if causal else 0, window, _ptr(out), _ptr(lse), _ptr(workspace), nbytes, _stream()),
+           "equarx_cache_attention")
 
 
 def equarx_calib_copy(src: torch.Tensor, dst: torch.Tensor) -> None:

@@ -10,9 +10,9 @@ _ROOT = os.path.dirname(_PKG)
 CSRC = os.path.join(_PKG, "csrc")
 INCLUDE = os.path.join(_ROOT, "include")
 LIB_PATH = os.path.join(_PKG, "libequarx.so")
-SOURCES = [os.path.join(CSRC, "equarx_api.hip"), os.path.join(CSRC, "equarx_devtools.hip")]
+SOURCES = [os.path.join(CSRC, name) for name in ("equarx_api.hip", "equarx_devtools.hip", "equarx_mx4.hip", "equarx_cache.hip")]
 HEADERS = [os.path.join(CSRC, name) for name in ("equarx_device.hpp", "equarx_strided.hpp", "equarx_launch.hpp", "equarx_passes.hpp",
-                                                  "equarx_devtools_kernels.hpp")]
+                                                  "equarx_devtools_kernels.hpp", "equarx_mx4.hpp", "equarx_cache.hpp")]
 HEADERS += [os.path.join(INCLUDE, "equarx.h"), os.path.join(INCLUDE, "equarx_devtools.h")]
 
 HIPCC_FLAGS = [

@@ -1,0 +1,282 @@
+// Host side of the key/value cache calls: argument validation, kernel selection and launch.
+#include "equarx.h"
+
+#include <type_traits>
+
+#include "equarx_cache.hpp"
+#include "equarx_launch.hpp"
+
+namespace {
+
+using namespace equarx;
+using namespace equarx::host;
+using namespace equarx::cache;
+
+constexpr int64_t kMostElements = (int64_t)1 << 40;
+constexpr int kGridDim = 65535;         // of a grid's second and third dimension
+
+int check_cache(const equarx_cache *c)
+{
+    if (!c) return EQUARX_NULL_POINTER;
+    if (c->dim != 64 && c->dim != 128 && c->dim != 256) return EQUARX_BAD_SHAPE;
+    if ((c->block != 64 && c->block != 128 && c->block != 256) || c->block > c->dim) return EQUARX_BAD_BLOCK;
+    if (c->pages < 1 || c->heads < 1 || c->heads > kGridDim || c->page < 16 || c->page % 16 != 0 || c->page > 65536)
+        return EQUARX_BAD_SHAPE;
+    if (c->pages > INT32_MAX || c->pages > kMostElements / ((int64_t)c->heads * c->page * c->dim)) return EQUARX_BAD_SHAPE;
+    if (!c->k_codes || !c->k_scales || !c->v_codes || !c->v_scales) return EQUARX_NULL_POINTER;
+    if (misaligned(c->k_codes, kAlign) || misaligned(c->k_scales, kAlign) || misaligned(c->v_codes, kAlign) ||
+        misaligned(c->v_scales, kAlign))
+        return EQUARX_MISALIGNED;
+    return EQUARX_OK;
+}
+
+Pool pool_of(const equarx_cache &c)
+{
+    Pool p{c.k_codes, c.k_scales, c.v_codes, c.v_scales, c.pages, c.heads, c.page, -1};
+    for (int s = 4; s <= 16; ++s) {
+        if (c.page == 1 << s) p.page_shift = s;
+    }
+    return p;
+}
+
+void list_cache(const equarx_cache &c, bool written, Aliasing &mem)
+{
+    const size_t codes = (size_t)c.pages * c.heads * c.page * c.dim, scales = codes / c.block * sizeof(float);
+    const void *const parts[4] = {c.k_codes, c.v_codes, c.k_scales, c.v_scales};
+    for (int i = 0; i < 4; ++i) {
+        if (written) {
+            mem.writes(parts[i], i < 2 ? codes : scales);
+        } else {
+            mem.reads(parts[i], i < 2 ? codes : scales);
+        }
+    }
+}
+
+// bf16 [rows][heads][dim] with strides; the bytes from its first element to its last.
+int check_tokens(const void *p, int64_t rows, int64_t heads, int64_t dim, int64_t row_stride, int64_t head_stride, size_t &bytes)
+{
+    if (!p) return EQUARX_NULL_POINTER;
+    if (misaligned(p, kAlign) || row_stride % 8 != 0 || head_stride % 8 != 0) return EQUARX_MISALIGNED;
+    if (row_stride < 0 || head_stride < 0 || row_stride > kMostElements / rows || head_stride > kMostElements / heads)
+        return EQUARX_BAD_SHAPE;
+    bytes = (size_t)((rows - 1) * row_stride + (heads - 1) * head_stride + dim) * 2;
+    return EQUARX_OK;
+}
+
+// f(dim, block) as compile-time constants.
+template <typename F>
+void with_geometry(int32_t dim, int32_t block, F f)
+{
+    using std::integral_constant;
+#define EQUARX_GEOMETRY(D, B) \
+    if (dim == D && block == B) f(integral_constant<int, D>{}, integral_constant<int, B>{})
+    EQUARX_GEOMETRY(64, 64);
+    EQUARX_GEOMETRY(128, 64);
+    EQUARX_GEOMETRY(128, 128);
+    EQUARX_GEOMETRY(256, 64);
+    EQUARX_GEOMETRY(256, 128);
+    EQUARX_GEOMETRY(256, 256);
+#undef EQUARX_GEOMETRY
+}
+
+int check_sequences(const int32_t *page_table, int64_t table_width, const int32_t *lengths, int32_t sequences, Aliasing &mem)
+{
+    if (!page_table || !lengths) return EQUARX_NULL_POINTER;
+    if (misaligned(page_table, sizeof(int32_t)) || misaligned(lengths, sizeof(int32_t))) return EQUARX_MISALIGNED;
+    mem.reads(page_table, (size_t)sequences * (size_t)table_width * sizeof(int32_t));
+    mem.reads(lengths, (size_t)sequences * sizeof(int32_t));
+    return EQUARX_OK;
+}
+
+// ---------------------------------------------------------------- how an attention call is cut
+
+struct AttentionPlan {
+    bool on_tokens;             // the waves of a workgroup share their rows
+    int rows16;                 // sixteens of rows of a wave
+    int64_t row_tiles;          // of the longest query run
+    int32_t splits, chunk;
+};
+
+AttentionPlan plan_attention(int32_t heads, int32_t q_heads, int32_t sequences, int64_t max_queries, int64_t max_length)
+{
+    AttentionPlan p;
+    const int64_t rows = max_queries * (q_heads / heads);
+    p.on_tokens = rows <= 32;
+    p.rows16 = rows <= 16 ? 1 : 2;
+    const int64_t per = (p.on_tokens ? 1 : 4) * p.rows16 * 16;
+    p.row_tiles = (rows + per - 1) / per;
+    const int64_t workgroups = p.row_tiles * heads * sequences;
+    // enough workgroups for four a CU, none with fewer than four tiles of tokens
+    int64_t splits = (1024 + workgroups - 1) / workgroups;
+    const int64_t most = (max_length + 255) / 256;
+    if (splits > most) splits = most;
+    if (splits > 128) splits = 128;
+    if (splits * heads > kGridDim) splits = kGridDim / heads;
+    if (splits < 1) splits = 1;
+    p.chunk = (int32_t)(((max_length + splits - 1) / splits + 63) / 64 * 64);
+    p.splits = (int32_t)((max_length + p.chunk - 1) / p.chunk);
+    return p;
+}
+
+size_t attention_workspace(const AttentionPlan &p, int32_t dim, int64_t q_rows, int32_t q_heads)
+{
+    return p.splits == 1 ? 0 : (size_t)p.splits * (size_t)q_rows * (size_t)q_heads * ((size_t)dim + 2) * sizeof(float);
+}
+
+int check_heads(int32_t heads, int64_t q_rows, int32_t q_heads, int32_t dim, int32_t sequences, int32_t max_queries,
+                int64_t max_length)
+{
+    if (heads < 1 || heads > kGridDim || q_heads < 1 || q_heads % heads != 0) return EQUARX_BAD_SHAPE;
+    if (q_rows < 0 || sequences < 0 || max_queries < 1 || max_length < 1 || max_length > INT32_MAX - 63) return EQUARX_BAD_SHAPE;
+    if (dim != 64 && dim != 128 && dim != 256) return EQUARX_BAD_SHAPE;
+    if (q_rows > INT32_MAX || q_rows > kMostElements / ((int64_t)q_heads * dim)) return EQUARX_BAD_SHAPE;
+    return EQUARX_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int equarx_cache_write(const equarx_cache *cache, const void *k_bf16, int64_t k_row_stride, int64_t k_head_stride,
+                       const void *v_bf16, int64_t v_row_stride, int64_t v_head_stride, int64_t tokens, const int64_t *slots,
+                       void *stream)
+{
+    LaunchCtx ctx(stream);
+    if (int st = check_cache(cache)) return st;
+    if (tokens < 0 || tokens > (1 << 30)) return EQUARX_BAD_SHAPE;
+    if (tokens == 0) return EQUARX_OK;
+    size_t k_bytes, v_bytes;
+    if (int st = check_tokens(k_bf16, tokens, cache->heads, cache->dim, k_row_stride, k_head_stride, k_bytes)) return st;
+    if (int st = check_tokens(v_bf16, tokens, cache->heads, cache->dim, v_row_stride, v_head_stride, v_bytes)) return st;
+    if (!slots) return EQUARX_NULL_POINTER;
+    if (misaligned(slots, sizeof(int64_t))) return EQUARX_MISALIGNED;
+    Aliasing mem;
+    mem.reads(k_bf16, k_bytes);
+    mem.reads(v_bf16, v_bytes);
+    mem.reads(slots, (size_t)tokens * sizeof(int64_t));
+    list_cache(*cache, true, mem);
+    if (int st = mem.check()) return st;
+    with_geometry(cache->dim, cache->block, [&](auto dim, auto block) {
+        constexpr int D = decltype(dim)::value, B = decltype(block)::value;
+        constexpr int kTokens = 256 / (D / 8) * 4;
+        ctx.launch2d(write_kernel<D, B>, (unsigned)((tokens + kTokens - 1) / kTokens), (unsigned)cache->heads, 256,
+                     static_cast<const uint16_t *>(k_bf16), static_cast<const uint16_t *>(v_bf16), slots, k_row_stride,
+                     v_row_stride, (int32_t)tokens, k_head_stride, v_head_stride, pool_of(*cache));
+    });
+    return ctx.status();
+}
+
+int equarx_cache_read(const equarx_cache *cache, const int32_t *page_table, int64_t table_width, const int32_t *lengths,
+                      const int32_t *starts, int32_t sequences, int64_t max_length, int64_t rows, void *k_out, void *v_out,
+                      void *stream)
+{
+    LaunchCtx ctx(stream);
+    if (int st = check_cache(cache)) return st;
+    if (sequences < 0 || table_width < 0 || table_width > INT32_MAX || max_length < 0 || rows < 0 || rows > INT32_MAX ||
+        rows > kMostElements / ((int64_t)cache->heads * cache->dim))
+        return EQUARX_BAD_SHAPE;
+    if (sequences == 0 || table_width == 0 || rows == 0) return EQUARX_OK;
+    Aliasing mem;
+    if (int st = check_sequences(page_table, table_width, lengths, sequences, mem)) return st;
+    if (!starts || !k_out || !v_out) return EQUARX_NULL_POINTER;
+    if (misaligned(starts, sizeof(int32_t)) || misaligned(k_out, kAlign) || misaligned(v_out, kAlign)) return EQUARX_MISALIGNED;
+    const size_t out_bytes = (size_t)rows * cache->heads * cache->dim * 2;
+    mem.reads(starts, (size_t)sequences * sizeof(int32_t));
+    mem.writes(k_out, out_bytes);
+    mem.writes(v_out, out_bytes);
+    list_cache(*cache, false, mem);
+    if (int st = mem.check()) return st;
+    with_geometry(cache->dim, cache->block, [&](auto dim, auto block) {
+        constexpr int D = decltype(dim)::value, B = decltype(block)::value;
+        constexpr int kTokens = 256 / (D / 8) * 4;
+        int64_t tiles = (max_length + kTokens - 1) / kTokens;
+        tiles = tiles < 1 ? 1 : tiles < 4096 ? tiles : 4096;
+        for (int32_t at = 0; at < sequences; at += kGridDim) {
+            const int32_t count = sequences - at < kGridDim ? sequences - at : kGridDim;
+            ctx.launch3d(read_kernel<D, B>, (unsigned)tiles, (unsigned)cache->heads, (unsigned)count, 256,
+                         static_cast<uint16_t *>(k_out), static_cast<uint16_t *>(v_out), starts + at, rows,
+                         Sequences{page_table + at * table_width, lengths + at, table_width}, pool_of(*cache));
+        }
+    });
+    return ctx.status();
+}
+
+size_t equarx_cache_attention_workspace_bytes(int32_t heads, int32_t dim, int64_t q_rows, int32_t q_heads, int32_t sequences,
+                                              int32_t max_queries, int64_t max_length)
+{
+    if (check_heads(heads, q_rows, q_heads, dim, sequences, max_queries, max_length) != EQUARX_OK || sequences == 0) return 0;
+    return attention_workspace(plan_attention(heads, q_heads, sequences, max_queries, max_length), dim, q_rows, q_heads);
+}
+
+int equarx_cache_attention(const equarx_cache *cache, const void *q_bf16, int64_t q_rows, int32_t q_heads,
+                           int64_t q_row_stride, int64_t q_head_stride, const int32_t *q_starts, const int32_t *page_table,
+                           int64_t table_width, const int32_t *lengths, int32_t sequences, float scale, int32_t max_queries,
+                           int64_t max_length, uint32_t flags, int32_t window, void *out_bf16, float *lse, void *workspace,
+                           size_t workspace_bytes, void *stream)
+{
+    LaunchCtx ctx(stream);
+    if (int st = check_cache(cache)) return st;
+    if (int st = check_heads(cache->heads, q_rows, q_heads, cache->dim, sequences, max_queries, max_length)) return st;
+    if (table_width < 1 || table_width > INT32_MAX || (flags & ~EQUARX_CAUSAL) != 0 || window < 0 ||
+        (window > 0 && !(flags & EQUARX_CAUSAL)))
+        return EQUARX_BAD_SHAPE;
+    if (sequences == 0 || q_rows == 0) return EQUARX_OK;
+    size_t q_bytes;
+    if (int st = check_tokens(q_bf16, q_rows, q_heads, cache->dim, q_row_stride, q_head_stride, q_bytes)) return st;
+    Aliasing mem;
+    if (int st = check_sequences(page_table, table_width, lengths, sequences, mem)) return st;
+    if (!q_starts || !out_bf16) return EQUARX_NULL_POINTER;
+    if (misaligned(q_starts, sizeof(int32_t)) || misaligned(out_bf16, kAlign) || misaligned(lse, kAlign) ||
+        misaligned(workspace, kWorkspaceAlign))
+        return EQUARX_MISALIGNED;
+    const AttentionPlan plan = plan_attention(cache->heads, q_heads, sequences, max_queries, max_length);
+    const size_t need = attention_workspace(plan, cache->dim, q_rows, q_heads);
+    if (need > 0 && !workspace) return EQUARX_NULL_POINTER;
+    if (workspace_bytes < need) return EQUARX_WORKSPACE_TOO_SMALL;
+    mem.reads(q_bf16, q_bytes);
+    mem.reads(q_starts, ((size_t)sequences + 1) * sizeof(int32_t));
+    list_cache(*cache, false, mem);
+    mem.writes(out_bf16, (size_t)q_rows * q_heads * cache->dim * 2);
+    mem.writes(lse, (size_t)q_rows * q_heads * sizeof(float));
+    mem.writes(workspace, need);
+    if (int st = mem.check()) return st;
+
+    AttentionCall call{};
+    call.q = static_cast<const uint16_t *>(q_bf16);
+    call.q_row = q_row_stride;
+    call.q_head = q_head_stride;
+    call.q_starts = q_starts;
+    call.out = static_cast<uint16_t *>(out_bf16);
+    call.lse = lse;
+    call.part = static_cast<float *>(workspace);
+    call.q_rows = q_rows;
+    call.q_heads = q_heads;
+    call.group = q_heads / cache->heads;
+    call.scale = scale * 1.44269504089f;
+    call.causal = (flags & EQUARX_CAUSAL) != 0;
+    call.window = window;
+    call.chunk = plan.chunk;
+    call.splits = plan.splits;
+    const Pool pool = pool_of(*cache);
+    const int64_t tiles = plan.row_tiles < 65536 ? plan.row_tiles : 65536;
+    with_geometry(cache->dim, cache->block, [&](auto dim, auto block) {
+        constexpr int D = decltype(dim)::value, NB = D / decltype(block)::value;
+        const auto kernel = !plan.on_tokens     ? attention_kernel<D, NB, 2, false>
+                            : plan.rows16 == 1 ? attention_kernel<D, NB, 1, true>
+                                               : attention_kernel<D, NB, 2, true>;
+        for (int32_t at = 0; at < sequences; at += kGridDim) {
+            const int32_t count = sequences - at < kGridDim ? sequences - at : kGridDim;
+            AttentionCall part = call;
+            part.q_starts += at;
+            ctx.launch3d(kernel, (unsigned)tiles, (unsigned)(cache->heads * plan.splits), (unsigned)count, 256, part,
+                         Sequences{page_table + at * table_width, lengths + at, table_width}, pool);
+        }
+        if (plan.splits > 1) {
+            const int64_t all = q_rows * q_heads, per = 256 / (D / 4);
+            ctx.launch(join_kernel<D>, (unsigned)((all + per - 1) / per), 256, call, sequences);
+        }
+    });
+    return ctx.status();
+}
+
+}  // extern "C"

@@ -1,0 +1,225 @@
+// Device code of the 4-bit microscaled format: quantizing rows, reading them back, and the product of packed rows.
+#pragma once
+
+#include "equarx_device.hpp"
+
+namespace equarx {
+namespace mx4 {
+
+typedef int v8i __attribute__((ext_vector_type(8)));
+typedef float v4f __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+// 16 bytes at any even address: rows of any stride are read and written whole where they lie
+typedef u32x4 u32x4_anywhere __attribute__((aligned(2)));
+
+constexpr int kBlock = 32, kGroup = 128;
+
+// n / d for n < 2^31 by a multiplication, d fixed for a launch (Granlund and Montgomery's round-up form).
+struct Divisor {
+    uint32_t magic, shift, d;
+    explicit Divisor(uint32_t by) : magic(0), shift(0), d(by)
+    {
+        while (((uint64_t)1 << shift) < d) ++shift;
+        magic = (uint32_t)((((((uint64_t)1 << shift) - d) << 32) / d) + 1);
+    }
+    __device__ __forceinline__ uint32_t of(uint32_t n) const { return (__umulhi(n, magic) + n) >> shift; }
+};
+
+// ---------------------------------------------------------------- rows of bf16
+
+// Elements [col, col + 8) of a row of `cols`; zeros past its end.
+__device__ __forceinline__ u32x4 load_row8(const uint16_t *row, int64_t col, int64_t cols)
+{
+    if (col + 8 <= cols) return *reinterpret_cast<const u32x4_anywhere *>(row + col);
+    uint32_t e[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) e[i] = col + i < cols ? row[col + i] : 0;
+    return u32x4{e[0] | e[1] << 16, e[2] | e[3] << 16, e[4] | e[5] << 16, e[6] | e[7] << 16};
+}
+
+__device__ __forceinline__ void store_row8(uint16_t *row, int64_t col, int64_t cols, const u32x4 &v)
+{
+    if (col + 8 <= cols) {
+        *reinterpret_cast<u32x4_anywhere *>(row + col) = v;
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        if (col + i < cols) row[col + i] = (uint16_t)(v[i / 2] >> (16 * (i & 1)));
+    }
+}
+
+// ---------------------------------------------------------------- one block's scale and codes
+
+// The larger of each half of two words, as unsigned 16-bit numbers: magnitudes of bf16 numbers are ordered like their
+// patterns.
+__device__ __forceinline__ uint32_t umax16x2(uint32_t a, uint32_t b)
+{
+    typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, a), __builtin_bit_cast(u16x2, b)));
+}
+
+// The scale byte of a block whose largest magnitude has the bf16 pattern `top`.
+__device__ __forceinline__ uint32_t scale_byte(uint32_t top)
+{
+    const uint32_t e = top >> 7;
+    return e == 255 ? 255 : e > 2 ? e - 2 : 0;
+}
+
+// 2^(byte - 127) as the instructions take it: they read the exponent field alone.
+__device__ __forceinline__ float scale_of(uint32_t byte) { return __uint_as_float(byte << 23); }
+
+// Eight bf16 numbers as codes at a scale: the hardware rounds to nearest, ties to even, and clamps at 6.
+__device__ __forceinline__ uint32_t codes_of(const u32x4 &x, float scale)
+{
+    const uint32_t d[4] = {x.x, x.y, x.z, x.w};      // not a cast of x[i]: the compiler casts the first element each time
+    uint32_t w = 0;
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, __builtin_bit_cast(bf16x2, d[0]), scale, 0);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, __builtin_bit_cast(bf16x2, d[1]), scale, 1);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, __builtin_bit_cast(bf16x2, d[2]), scale, 2);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, __builtin_bit_cast(bf16x2, d[3]), scale, 3);
+    return w;
+}
+
+__device__ __forceinline__ uint32_t magnitudes_max(const u32x4 &x)
+{
+    constexpr uint32_t kMagnitude = 0x7fff7fffu;
+    return umax16x2(umax16x2(x[0] & kMagnitude, x[1] & kMagnitude), umax16x2(x[2] & kMagnitude, x[3] & kMagnitude));
+}
+
+// ---------------------------------------------------------------- rows <-> packed rows
+// A lane has eight elements, a quad a block, a row of sixteen lanes a group: `units` pieces of eight in all, the
+// padding among them, `unit` counting through the packed rows.
+
+__global__ __launch_bounds__(256) void quantize_rows_kernel(Global<const uint16_t> x, int64_t x_stride, Global<uint8_t> codes,
+                                                            Global<uint8_t> scales, int64_t cols, uint32_t units,
+                                                            const Divisor row_units)
+{
+    const uint32_t unit = blockIdx.x * 256 + threadIdx.x;
+    if (unit >= units) return;                                  // whole rows of sixteen lanes: units is a multiple of 16
+    const uint32_t row = row_units.of(unit);
+    const int64_t col = (int64_t)(unit - row * row_units.d) * 8;
+    const u32x4 v = load_row8(x + row * x_stride, col, cols);
+    uint32_t top = magnitudes_max(v);
+    top = umax(top & 0xffff, top >> 16);
+    top = umax(top, dpp_read<0xB1>(top));
+    top = umax(top, dpp_read<0x4E>(top));
+    const uint32_t byte = scale_byte(top);
+    reinterpret_cast<uint32_t *>((uint8_t *)codes)[unit] = byte == 255 ? 0 : codes_of(v, scale_of(byte));
+    uint32_t four = byte << (8 * ((threadIdx.x >> 2) & 3));
+    four |= dpp_read<0x141>(four);
+    four |= dpp_read<0x140>(four);
+    if ((threadIdx.x & 15) == 0) reinterpret_cast<uint32_t *>((uint8_t *)scales)[unit / 16] = four;
+}
+
+__device__ __forceinline__ u32x4 values_of(uint32_t codes, float scale)
+{
+    u32x4 v;
+    v[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 0));
+    v[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 1));
+    v[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 2));
+    v[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 3));
+    return v;
+}
+
+__global__ __launch_bounds__(256) void dequantize_rows_kernel(Global<const uint8_t> codes, Global<const uint8_t> scales,
+                                                              Global<uint16_t> out, int64_t out_stride, int64_t cols,
+                                                              uint32_t units, const Divisor row_units)
+{
+    const uint32_t unit = blockIdx.x * 256 + threadIdx.x;
+    if (unit >= units) return;
+    const uint32_t row = row_units.of(unit);
+    const int64_t col = (int64_t)(unit - row * row_units.d) * 8;
+    if (col >= cols) return;
+    const uint32_t w = reinterpret_cast<const uint32_t *>((const uint8_t *)codes)[unit];
+    const uint32_t byte = scales[unit / 4];
+    u32x4 v = values_of(w, scale_of(byte));
+    if (byte == 255) v = u32x4{0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u};
+    store_row8(out + row * out_stride, col, cols, v);
+}
+
+// ---------------------------------------------------------------- product of packed rows
+// One 16x16x128 matrix instruction takes 128 elements of 16 rows of w and of 16 rows of x: lane l has row l % 16 and
+// its block l / 16 of four, with that block's scale.  Its result lane l has column l % 16 (a row of x) and the four rows
+// of w 4 * (l / 16) + 0 .. 3: four consecutive outputs.
+
+struct Packed {
+    const uint8_t *codes, *scales;
+    int64_t rows, blocks;
+};
+
+struct Fragment {
+    u32x4 codes;
+    uint32_t scale;
+};
+
+__device__ __forceinline__ Fragment load_fragment(const uint8_t *codes, const uint8_t *scales, int64_t block)
+{
+    Fragment f;
+    f.codes = *reinterpret_cast<const u32x4 *>(codes + block * 16);
+    f.scale = scales[block];
+    return f;
+}
+
+__device__ __forceinline__ v4f multiply(const Fragment &w, const Fragment &x, const v4f &sum)
+{
+    const v8i a = {(int)w.codes[0], (int)w.codes[1], (int)w.codes[2], (int)w.codes[3], 0, 0, 0, 0};
+    const v8i b = {(int)x.codes[0], (int)x.codes[1], (int)x.codes[2], (int)x.codes[3], 0, 0, 0, 0};
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, sum, 4, 4, 0, (int)w.scale, 0, (int)x.scale);
+}
+
+// Four consecutive outputs of one row, as far as the row goes.
+__device__ __forceinline__ void store_out4(uint16_t *row, int64_t n, int64_t N, const v4f &v)
+{
+    typedef u32x2 u32x2_anywhere __attribute__((aligned(2)));
+    const u32x2 w = {narrow_bf16x2(v[0], v[1]), narrow_bf16x2(v[2], v[3])};
+    if (n + 4 <= N) {
+        *reinterpret_cast<u32x2_anywhere *>(row + n) = w;
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if (n + i < N) row[n + i] = (uint16_t)(w[i / 2] >> (16 * (i & 1)));
+    }
+}
+
+// Sixteen rows of w by MT * 16 rows of x in a workgroup, the sum over k cut into W parts, one for a wave, that are added
+// in order.
+template <int W, int MT>
+__global__ __launch_bounds__(64 * W) void product_rows_kernel(Global<const uint8_t> xc, Global<const uint8_t> xs,
+                                                              Global<const uint8_t> wc, Global<const uint8_t> ws,
+                                                              Global<uint16_t> out, int32_t M, int32_t N, int32_t groups,
+                                                              int64_t out_stride)
+{
+    __shared__ v4f part[W][MT][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int r = lane & 15, g = lane >> 4;
+    const int64_t n0 = (int64_t)blockIdx.x * 16, m0 = (int64_t)blockIdx.y * (16 * MT);
+    const int64_t blocks = (int64_t)groups * 4;
+    const int64_t wr = n0 + r < N ? n0 + r : N - 1;
+    v4f sum[MT];
+#pragma unroll
+    for (int t = 0; t < MT; ++t) sum[t] = v4f{0, 0, 0, 0};
+    const uint8_t *const wcr = wc + wr * blocks * 16, *const wsr = ws + wr * blocks;
+    for (int s = wave; s < groups; s += W) {
+        const Fragment w = load_fragment(wcr, wsr, 4 * s + g);
+#pragma unroll
+        for (int t = 0; t < MT; ++t) {
+            const int64_t m = m0 + 16 * t + r, xr = m < M ? m : M - 1;
+            sum[t] = multiply(w, load_fragment(xc + xr * blocks * 16, xs + xr * blocks, 4 * s + g), sum[t]);
+        }
+    }
+#pragma unroll
+    for (int t = 0; t < MT; ++t) part[wave][t][lane] = sum[t];
+    __syncthreads();
+    for (int t = wave; t < MT; t += W) {
+        v4f total = part[0][t][lane];
+#pragma unroll
+        for (int i = 1; i < W; ++i) total += part[i][t][lane];
+        const int64_t m = m0 + 16 * t + r;
+        if (m < M) store_out4(out + m * out_stride, n0 + 4 * g, N, total);
+    }
+}
+
+}  // namespace mx4
+}  // namespace equarx

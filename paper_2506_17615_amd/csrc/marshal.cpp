@@ -21,6 +21,9 @@ constexpr int kNotPlain = -1;
 constexpr auto kBF16 = at::ScalarType::BFloat16;
 constexpr auto kInt8 = at::ScalarType::Char;
 constexpr auto kFloat = at::ScalarType::Float;
+constexpr auto kByte = at::ScalarType::Byte;
+constexpr auto kInt = at::ScalarType::Int;
+constexpr auto kLong = at::ScalarType::Long;
 
 // The library's entry points, as binding.load() found them.
 struct Library {
@@ -29,7 +32,9 @@ struct Library {
     X(equarx_reduce_quantized_static) X(equarx_reduce_quantized_fused_ends) X(equarx_reduce_fused)                   \
     X(equarx_reduce_variant) X(equarx_reduce_variant_hops) X(equarx_reduce_flat) X(equarx_quantize_strided)          \
     X(equarx_dequantize_strided) X(equarx_reduce_stage_strided) X(equarx_reduce_quantized_strided)                   \
-    X(equarx_reduce_fused_strided) X(equarx_reduce_variant_strided) X(equarx_reduce_variant_hops_strided)
+    X(equarx_reduce_fused_strided) X(equarx_reduce_variant_strided) X(equarx_reduce_variant_hops_strided)            \
+    X(equarx_mx4_quantize) X(equarx_mx4_dequantize) X(equarx_mx4_product) X(equarx_mx4_linear)                       \
+    X(equarx_cache_write) X(equarx_cache_read) X(equarx_cache_attention)
 #define X(name) decltype(&::name) name;
     EQUARX_CALLS(X)
 #undef X
@@ -301,6 +306,191 @@ int reduce_flat(PyObject *const *a)
                 out.ptr, static_cast<int8_t *>(codes_out.ptr), static_cast<float *>(scales_out.ptr));
 }
 
+// ---------------------------------------------------------------- 4-bit rows and the cache
+
+// A bf16 tensor of `dims` dimensions whose last one is contiguous; `row` and `head` are the strides of the first and (with
+// three) the second, those of a packed tensor where there is but one index.
+struct Rows {
+    void *ptr = nullptr;
+    int64_t size[3] = {0, 0, 0}, row = 0, head = 0;
+
+    bool of(PyObject *o, int dims)
+    {
+        if (!THPVariable_CheckExact(o)) return false;
+        const at::Tensor &t = THPVariable_Unpack(o);
+        if (!t.defined() || !t.is_cuda() || !t.has_storage() || t.scalar_type() != kBF16 || t.dim() != dims) return false;
+        if (t.numel() == 0) return false;
+        for (int i = 0; i < dims; ++i) size[i] = t.size(i);
+        const int64_t cols = size[dims - 1];
+        if (cols > 1 && t.stride(dims - 1) != 1) return false;
+        head = dims == 3 && size[1] > 1 ? t.stride(1) : cols;
+        row = size[0] > 1 ? t.stride(0) : dims == 3 ? size[1] * cols : cols;
+        ptr = t.data_ptr();
+        return true;
+    }
+};
+
+// uint8 codes [rows][16 * blocks] and scales [rows][blocks], contiguous.
+struct PackedRows {
+    uint8_t *codes = nullptr, *scales = nullptr;
+    int64_t rows = 0;
+
+    bool of(PyObject *c, PyObject *s, int64_t cols)
+    {
+        const at::Tensor *tc = plain(c), *ts = plain(s);
+        if (!tc || !ts || tc->scalar_type() != kByte || ts->scalar_type() != kByte || tc->dim() != 2 || ts->dim() != 2)
+            return false;
+        const int64_t per = (cols + EQUARX_MX4_GROUP - 1) / EQUARX_MX4_GROUP * (EQUARX_MX4_GROUP / EQUARX_MX4_BLOCK);
+        rows = tc->size(0);
+        if (ts->size(0) != rows || tc->size(1) != 16 * per || ts->size(1) != per) return false;
+        codes = static_cast<uint8_t *>(tc->data_ptr());
+        scales = static_cast<uint8_t *>(ts->data_ptr());
+        return true;
+    }
+};
+
+int mx4_quantize(PyObject *const *a)
+{
+    Rows x;
+    PackedRows p;
+    if (!x.of(a[0], 2) || !p.of(a[1], a[2], x.size[1]) || p.rows != x.size[0]) return kNotPlain;
+    return call(lib.equarx_mx4_quantize, x.ptr, x.size[0], x.size[1], x.row, p.codes, p.scales);
+}
+
+int mx4_dequantize(PyObject *const *a)
+{
+    Rows out;
+    PackedRows p;
+    if (!out.of(a[2], 2) || !p.of(a[0], a[1], out.size[1]) || p.rows != out.size[0]) return kNotPlain;
+    return call(lib.equarx_mx4_dequantize, p.codes, p.scales, out.size[0], out.size[1], out.ptr, out.row);
+}
+
+int mx4_product(PyObject *const *a)
+{
+    Rows out;
+    PackedRows x, w;
+    Workspace ws;
+    long long K;
+    if (!integer(a[4], 1, INT32_MAX, K) || !out.of(a[5], 2) || !x.of(a[0], a[1], K) || !w.of(a[2], a[3], K) || !ws.of(a[6]))
+        return kNotPlain;
+    if (x.rows != out.size[0] || w.rows != out.size[1]) return kNotPlain;
+    return call(lib.equarx_mx4_product, x.codes, x.scales, w.codes, w.scales, out.size[0], out.size[1], (int64_t)K, out.ptr,
+                out.row, ws.ptr, ws.bytes);
+}
+
+int mx4_linear(PyObject *const *a)
+{
+    Rows x, out;
+    PackedRows w;
+    Workspace ws;
+    if (!x.of(a[0], 2) || !w.of(a[1], a[2], x.size[1]) || !out.of(a[3], 2) || !ws.of(a[4])) return kNotPlain;
+    if (x.size[0] != out.size[0] || w.rows != out.size[1]) return kNotPlain;
+    return call(lib.equarx_mx4_linear, x.ptr, x.row, w.codes, w.scales, out.size[0], out.size[1], x.size[1], out.ptr, out.row,
+                ws.ptr, ws.bytes);
+}
+
+// A Cache: a tuple of four tensors of the shapes that the header gives.
+bool a_cache(PyObject *o, equarx_cache &c)
+{
+    if (!PyTuple_Check(o) || PyTuple_GET_SIZE(o) != 4) return false;
+    const at::Tensor *t[4];
+    for (int i = 0; i < 4; ++i) {
+        t[i] = plain(PyTuple_GET_ITEM(o, i));
+        if (!t[i] || t[i]->scalar_type() != (i % 2 ? kFloat : kInt8) || t[i]->dim() != (i == 2 ? 5 : 4) || t[i]->numel() == 0)
+            return false;
+    }
+    const int64_t pages = t[0]->size(0), heads = t[0]->size(1), page = t[0]->size(2), dim = t[0]->size(3), blocks = t[1]->size(2);
+    if (heads > INT32_MAX || page > INT32_MAX || dim > INT32_MAX || blocks < 1 || dim % blocks != 0) return false;
+    for (int i = 1; i < 4; i += 2) {
+        if (t[i]->size(0) != pages || t[i]->size(1) != heads || t[i]->size(2) != blocks || t[i]->size(3) != page) return false;
+    }
+    if (t[2]->size(0) != pages || t[2]->size(1) != heads || t[2]->size(2) * 16 != page || t[2]->size(3) != dim ||
+        t[2]->size(4) != 16)
+        return false;
+    c.k_codes = static_cast<int8_t *>(t[0]->data_ptr());
+    c.k_scales = static_cast<float *>(t[1]->data_ptr());
+    c.v_codes = static_cast<int8_t *>(t[2]->data_ptr());
+    c.v_scales = static_cast<float *>(t[3]->data_ptr());
+    c.pages = pages;
+    c.heads = (int32_t)heads;
+    c.page = (int32_t)page;
+    c.dim = (int32_t)dim;
+    c.block = (int32_t)(dim / blocks);
+    return true;
+}
+
+bool same_heads(const Rows &r, const equarx_cache &c) { return r.size[1] == c.heads && r.size[2] == c.dim; }
+
+// page_table [sequences][width] and lengths [sequences].
+struct SequenceList {
+    const int32_t *table = nullptr, *lengths = nullptr;
+    int64_t width = 0;
+    int32_t count = 0;
+
+    bool of(PyObject *tab, PyObject *len)
+    {
+        Buffer t, n;
+        if (!t.of(tab, kInt) || t.t->dim() != 2 || t.count == 0 || t.t->size(0) > INT32_MAX) return false;
+        count = (int32_t)t.t->size(0);
+        width = t.t->size(1);
+        if (!n.of(len, kInt) || n.count != count) return false;
+        table = static_cast<const int32_t *>(t.ptr);
+        lengths = static_cast<const int32_t *>(n.ptr);
+        return true;
+    }
+};
+
+int cache_write(PyObject *const *a)
+{
+    equarx_cache c;
+    Rows k, v;
+    Buffer slots;
+    if (!a_cache(a[0], c) || !k.of(a[1], 3) || !v.of(a[2], 3) || !same_heads(k, c) || !same_heads(v, c)) return kNotPlain;
+    if (v.size[0] != k.size[0] || !slots.of(a[3], kLong) || slots.count != k.size[0]) return kNotPlain;
+    return call(lib.equarx_cache_write, &c, k.ptr, k.row, k.head, v.ptr, v.row, v.head, k.size[0],
+                static_cast<const int64_t *>(slots.ptr));
+}
+
+int cache_read(PyObject *const *a)
+{
+    equarx_cache c;
+    SequenceList seqs;
+    Buffer starts;
+    long long longest;
+    if (!a_cache(a[0], c) || !seqs.of(a[1], a[2]) || !starts.of(a[3], kInt, seqs.count)) return kNotPlain;
+    const at::Tensor *const k = plain(a[4]), *const v = plain(a[5]);
+    for (const at::Tensor *t : {k, v}) {
+        if (!t || t->scalar_type() != kBF16 || t->dim() != 3 || t->numel() == 0 || t->size(1) != c.heads || t->size(2) != c.dim)
+            return kNotPlain;
+    }
+    if (k->size(0) != v->size(0) || !integer(a[6], 0, INT64_MAX, longest)) return kNotPlain;
+    return call(lib.equarx_cache_read, &c, seqs.table, seqs.width, seqs.lengths, static_cast<const int32_t *>(starts.ptr),
+                seqs.count, (int64_t)longest, k->size(0), k->data_ptr(), v->data_ptr());
+}
+
+int cache_attention(PyObject *const *a)
+{
+    equarx_cache c;
+    Rows q;
+    SequenceList seqs;
+    Buffer starts, out, lse;
+    Workspace ws;
+    long long queries, longest, window;
+    if (!a_cache(a[0], c) || !q.of(a[1], 3) || q.size[2] != c.dim || q.size[1] > INT32_MAX || !seqs.of(a[3], a[4])) return kNotPlain;
+    if (!starts.of(a[2], kInt) || starts.count != (int64_t)seqs.count + 1) return kNotPlain;
+    if (!out.of(a[5], kBF16) || out.t->dim() != 3 || out.t->size(0) != q.size[0] || out.t->size(1) != q.size[1] ||
+        out.t->size(2) != q.size[2])
+        return kNotPlain;
+    if (!PyFloat_CheckExact(a[6]) || !integer(a[7], 1, INT32_MAX, queries) || !integer(a[8], 1, INT32_MAX, longest)) return kNotPlain;
+    if (!PyBool_Check(a[9]) || !integer(a[10], 0, INT32_MAX, window)) return kNotPlain;
+    if (a[11] != Py_None && (!lse.of(a[11], kFloat) || lse.count != q.size[0] * q.size[1])) return kNotPlain;
+    if (!ws.of(a[12])) return kNotPlain;
+    return call(lib.equarx_cache_attention, &c, q.ptr, q.size[0], (int32_t)q.size[1], q.row, q.head,
+                static_cast<const int32_t *>(starts.ptr), seqs.table, seqs.width, seqs.lengths, seqs.count,
+                (float)PyFloat_AS_DOUBLE(a[6]), (int32_t)queries, (int64_t)longest,
+                a[9] == Py_True ? EQUARX_CAUSAL : 0u, (int32_t)window, out.ptr, static_cast<float *>(lse.ptr), ws.ptr, ws.bytes);
+}
+
 // The Python-callable form of f: kArgs positional arguments; an exception from torch is "not plain" too.
 template <int kArgs, typename F>
 PyObject *enter(PyObject *const *a, Py_ssize_t count, F f)
@@ -343,6 +533,13 @@ ENTRY(4, equarx_reduce_quantized_strided, reduce_quantized_strided(a))
 ENTRY(3, equarx_reduce_fused_strided, reduce_fused_strided(a))
 ENTRY(4, equarx_reduce_variant_strided, reduce_variant(a, true))
 ENTRY(5, equarx_reduce_variant_hops_strided, reduce_variant_hops(a, true))
+ENTRY(3, equarx_mx4_quantize, mx4_quantize(a))
+ENTRY(3, equarx_mx4_dequantize, mx4_dequantize(a))
+ENTRY(7, equarx_mx4_product, mx4_product(a))
+ENTRY(5, equarx_mx4_linear, mx4_linear(a))
+ENTRY(4, equarx_cache_write, cache_write(a))
+ENTRY(7, equarx_cache_read, cache_read(a))
+ENTRY(13, equarx_cache_attention, cache_attention(a))
 #undef ENTRY
 
 // bind({name: address}): where the library's entry points are.
