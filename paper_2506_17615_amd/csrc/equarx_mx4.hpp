@@ -8,6 +8,7 @@ namespace mx4 {
 
 typedef int v8i __attribute__((ext_vector_type(8)));
 typedef float v4f __attribute__((ext_vector_type(4)));
+typedef float v16f __attribute__((ext_vector_type(16)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 // 16 bytes at any even address: rows of any stride are read and written whole where they lie
 typedef u32x4 u32x4_anywhere __attribute__((aligned(2)));
@@ -218,6 +219,208 @@ __global__ __launch_bounds__(64 * W) void product_rows_kernel(Global<const uint8
         for (int i = 1; i < W; ++i) total += part[i][t][lane];
         const int64_t m = m0 + 16 * t + r;
         if (m < M) store_out4(out + m * out_stride, n0 + 4 * g, N, total);
+    }
+}
+
+// ---- large products
+// A workgroup of WN x WM waves has WN * FN * 32 rows of w by WM * FM * 32 rows of x, a wave FN x FM results of 32 x 32 in
+// registers.  The 128 elements of a step (a group) come to LDS with direct loads, kept in kRing buffers that are filled kRing - 1
+// steps ahead; a step is two 32x32x64 instructions a result, whose lane l has row l % 32 and block l / 32 of two.
+//
+// In LDS 16 rows of a step are 1 KB: the rows' first blocks, their second ones, and so on.  A direct load, which writes lane after
+// lane, brings the 64 bytes of 16 rows; a read takes the first or last two blocks of 32 rows, 256 bytes in a row at four places
+// with every bank's share the same.  Scales: the four bytes of a row and step as one word; a lane shifts it by its block and
+// the instruction picks byte 0 or 2.
+
+constexpr int kRing = 4;
+
+// A side's buffer of so many sixteens of rows: codes, then scales.
+template <int kSixteens>
+constexpr int side_bytes = kSixteens * (1024 + 64);
+
+// One direct load of 16 (or 4) bytes a lane: LDS `to` + lane * 16 (or 4) <- `from`.
+__device__ __forceinline__ void direct_load16(uint32_t to, const uint8_t *from)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(to), "v"(from) : "memory", "m0");
+}
+__device__ __forceinline__ void direct_load4(uint32_t to, const uint8_t *from)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(to), "v"(from) : "memory", "m0");
+}
+
+// What one of W waves loads of a side in every step: sixteens of rows wave, wave + W, ..., and, some of the waves, scales of 64
+// rows.
+template <int kSixteens, int W>
+struct SideLoads {
+    static constexpr int kPer = kSixteens / W, kScaleWaves = kSixteens / 4;
+    static_assert(kSixteens % W == 0, "every wave loads as much as the others");
+    const uint8_t *codes[kPer];
+    const uint8_t *scale;
+
+    __device__ __forceinline__ void start(const uint8_t *c, const uint8_t *s, int64_t row0, int64_t rows, int64_t blocks, int wave,
+                                          int scale_wave, int lane)
+    {
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+            int64_t row = row0 + (wave + W * i) * 16 + (lane & 15);
+            if (row >= rows) row = rows - 1;                        // loaded twice, stored nowhere
+            codes[i] = c + row * blocks * 16 + (lane >> 4) * 16;
+        }
+        int64_t row = row0 + scale_wave * 64 + lane;
+        if (row >= rows) row = rows - 1;
+        scale = s + row * blocks;
+    }
+    // step `at`'s codes into the buffer at LDS address `to`
+    __device__ __forceinline__ void issue(uint32_t to, int64_t at, int wave) const
+    {
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) direct_load16(to + (wave + W * i) * 1024, codes[i] + at * 64);
+    }
+    __device__ __forceinline__ void issue_scales(uint32_t to, int64_t at, int scale_wave) const
+    {
+        direct_load4(to + kSixteens * 1024 + scale_wave * 256, scale + at * 4);
+    }
+};
+
+// 32 rows of a step in registers.
+struct Rows32 {
+    u32x4 codes[2];
+    uint32_t scales;
+
+    template <int kSixteens>
+    __device__ __forceinline__ void read(const uint8_t *side, int i, int lane)
+    {
+        const int r = lane & 31, h = lane >> 5;
+        const uint8_t *const at = side + i * 2048 + (r >> 4) * 1024 + h * 256 + (r & 15) * 16;
+        codes[0] = *reinterpret_cast<const u32x4 *>(at);
+        codes[1] = *reinterpret_cast<const u32x4 *>(at + 512);
+        scales = *reinterpret_cast<const uint32_t *>(side + kSixteens * 1024 + (i * 32 + r) * 4);
+    }
+};
+
+template <int kHalf>
+__device__ __forceinline__ v16f multiply32(const Rows32 &w, uint32_t w_scale, const Rows32 &x, uint32_t x_scale, const v16f &sum)
+{
+    const u32x4 p = w.codes[kHalf], q = x.codes[kHalf];
+    const v8i a = {(int)p[0], (int)p[1], (int)p[2], (int)p[3], 0, 0, 0, 0};
+    const v8i b = {(int)q[0], (int)q[1], (int)q[2], (int)q[3], 0, 0, 0, 0};
+    return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, sum, 4, 4, 2 * kHalf, (int)w_scale, 2 * kHalf, (int)x_scale);
+}
+
+template <int WN, int WM, int FN, int FM>
+__global__ __launch_bounds__(64 * WN * WM) void product_tiles_kernel(Global<const uint8_t> xc, Global<const uint8_t> xs,
+                                                                     Global<const uint8_t> wc, Global<const uint8_t> ws,
+                                                                     Global<uint16_t> out, int32_t M, int32_t N, int32_t groups,
+                                                                     int64_t out_stride, uint32_t tiles_n, uint32_t tiles_m)
+{
+    constexpr int W = WN * WM, kSixteenN = WN * FN * 2, kSixteenM = WM * FM * 2;
+    constexpr int kSideN = side_bytes<kSixteenN>, kStage = kSideN + side_bytes<kSixteenM>;
+    __shared__ __align__(1024) uint8_t lds[kRing * kStage];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int h = lane >> 5;
+    const uint32_t tile_n = blockIdx.x % tiles_n, tile_m = blockIdx.x / tiles_n;
+    const int64_t n0 = (int64_t)tile_n * (kSixteenN * 16), m0 = (int64_t)tile_m * (kSixteenM * 16);
+    const int64_t blocks = (int64_t)groups * 4;
+    using LoadsN = SideLoads<kSixteenN, W>;
+    using LoadsM = SideLoads<kSixteenM, W>;
+    // scales: W waves share them out, a wave has one load of them a step, or one of either side
+    constexpr int kScaleN = LoadsN::kScaleWaves, kScaleM = LoadsM::kScaleWaves;
+    constexpr bool kBoth = kScaleN + kScaleM > W;
+    static_assert(kBoth ? kScaleN == W && kScaleM == W : true, "a wave's loads a step are the same for all, or fewer");
+    LoadsN wl;
+    LoadsM xl;
+    const int scale_m = kBoth ? wave : wave - kScaleN;
+    wl.start(wc, ws, n0, N, blocks, wave, wave, lane);
+    xl.start(xc, xs, m0, M, blocks, wave, scale_m, lane);
+    const uint32_t base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)lds;
+    constexpr int kStepLoads = LoadsN::kPer + LoadsM::kPer + (kBoth ? 2 : 1);
+    static_assert(kBoth || kScaleN + kScaleM == W, "every wave has as many loads in flight");
+    auto issue = [&](int step) {
+        const uint32_t to = base + (uint32_t)(step % kRing) * kStage;
+        const int64_t at = step < groups ? step : groups - 1;               // past the end: loaded again, not used
+        wl.issue(to, at, wave);
+        xl.issue(to + kSideN, at, wave);
+        if (kBoth || wave < kScaleN) wl.issue_scales(to, at, wave);
+        if (kBoth || wave >= kScaleN) xl.issue_scales(to + kSideN, at, scale_m);
+    };
+    v16f sum[FN][FM];
+#pragma unroll
+    for (int i = 0; i < FN; ++i)
+#pragma unroll
+        for (int j = 0; j < FM; ++j) sum[i][j] = v16f{0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
+
+    // Of w a lane holds this line of results' rows and the next line's, of x all of this step's and those of the next as they
+    // come: nothing is waited for that was asked for less than a line ago.
+    Rows32 w[2], x[2][FM];
+    static_assert(FN % 2 == 0 && FM <= FN, "a step asks for the next one's rows of x line by line");
+    const int part_n = wave % WN, part_m = wave / WN;
+    auto buffer = [&](int step) { return lds + (uint32_t)(step % kRing) * kStage; };
+    auto read_w = [&](Rows32 &to, int step, int i) { to.read<kSixteenN>(buffer(step), part_n * FN + i, lane); };
+    auto read_x = [&](Rows32 &to, int step, int j) { to.read<kSixteenM>(buffer(step) + kSideN, part_m * FM + j, lane); };
+    for (int i = 0; i < kRing - 1; ++i) issue(i);
+    asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"((kRing - 2) * kStepLoads) : "memory");
+#pragma unroll
+    for (int j = 0; j < FM; ++j) read_x(x[0][j], 0, j);
+    read_w(w[0], 0, 0);
+    auto step = [&](int at, int now, bool last) {
+        if (!last) {
+            // step at + 1 is in LDS for all waves, and step at - 1 has been read by all: its buffer is free
+            asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((kRing - 3) * kStepLoads) : "memory");
+            issue(at + kRing - 1);
+        }
+        uint32_t sx[FM];
+#pragma unroll
+        for (int j = 0; j < FM; ++j) sx[j] = x[now][j].scales >> (8 * h);
+#pragma unroll
+        for (int i = 0; i < FN; ++i) {
+            if (i + 1 < FN) {
+                read_w(w[(i + 1) % 2], at, i + 1);
+            } else if (!last) {
+                read_w(w[0], at + 1, 0);
+            }
+            if (i < FM && !last) read_x(x[1 - now][i], at + 1, i);
+            const uint32_t sw = w[i % 2].scales >> (8 * h);
+#pragma unroll
+            for (int j = 0; j < FM; ++j) sum[i][j] = multiply32<0>(w[i % 2], sw, x[now][j], sx[j], sum[i][j]);
+#pragma unroll
+            for (int j = 0; j < FM; ++j) sum[i][j] = multiply32<1>(w[i % 2], sw, x[now][j], sx[j], sum[i][j]);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+    int at = 0;
+    for (; at + 1 < groups; at += 2) {
+        step(at, 0, false);
+        step(at + 1, 1, false);
+    }
+    if (at < groups) step(at, 0, true);
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");            // what was loaded past the end lands before LDS is another's
+
+    // A lane has four consecutive outputs at 8 q + 4 h: after the exchange of halves it has eight, of an even q or an odd one.
+    const bool wide = out_stride % 8 == 0;
+#pragma unroll
+    for (int j = 0; j < FM; ++j) {
+        const int64_t m = m0 + (part_m * FM + j) * 32 + (lane & 31);
+        uint16_t *const row = out + m * out_stride;
+#pragma unroll
+        for (int i = 0; i < FN; ++i) {
+#pragma unroll
+            for (int q = 0; q < 4; q += 2) {
+                const v16f &s = sum[i][j];
+                auto lo = __builtin_amdgcn_permlane32_swap(narrow_bf16x2(s[4 * q], s[4 * q + 1]),
+                                                           narrow_bf16x2(s[4 * q + 4], s[4 * q + 5]), false, false);
+                auto hi = __builtin_amdgcn_permlane32_swap(narrow_bf16x2(s[4 * q + 2], s[4 * q + 3]),
+                                                           narrow_bf16x2(s[4 * q + 6], s[4 * q + 7]), false, false);
+                const int64_t n = n0 + (part_n * FN + i) * 32 + (q + h) * 8;
+                const u32x4 v = {lo[0], hi[0], lo[1], hi[1]};
+                if (m < M) {
+                    if (wide && n + 8 <= N) {
+                        *reinterpret_cast<u32x4 *>(row + n) = v;
+                    } else {
+                        store_row8(row, n, N, v);
+                    }
+                }
+            }
+        }
     }
 }
 
