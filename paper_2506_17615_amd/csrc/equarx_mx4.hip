@@ -53,7 +53,7 @@ void launch_product(const uint8_t *xc, const uint8_t *xs, const uint8_t *wc, con
                     int64_t K, uint16_t *out, int64_t out_stride, LaunchCtx &ctx)
 {
     const int32_t groups = (int32_t)groups_of(K);
-    if (M > 64 && groups >= 4) {
+    if (M > 64 && groups >= 4 && groups <= kMostTileGroups) {
         const uint32_t tiles_n = (uint32_t)((N + 255) / 256), tiles_m = (uint32_t)((M + 255) / 256);
         ctx.launch(product_tiles_kernel<2, 2, 4, 4>, tiles_n * tiles_m, 256, xc, xs, wc, ws, out, (int32_t)M, (int32_t)N, groups,
                    out_stride, tiles_n, tiles_m);

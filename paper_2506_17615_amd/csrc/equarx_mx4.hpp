@@ -237,11 +237,14 @@ __global__ __launch_bounds__(64 * W) void product_rows_kernel(Global<const uint8
 
 constexpr int kRing = 4;
 
-// One direct load of 16 bytes a lane: LDS `to` + lane * 16 <- `from`.
-__device__ __forceinline__ void direct_load(uint32_t to, const uint8_t *from)
+// One direct load of 16 bytes a lane: LDS `to` + lane * 16 <- `from` + `offset`.
+__device__ __forceinline__ void direct_load(uint32_t to, const uint8_t *from, uint32_t offset)
 {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(to), "v"(from) : "memory", "m0");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(offset), "s"(from) : "memory", "m0");
 }
+
+// The longest row of codes whose 256 a lane's 32-bit offset reaches.
+constexpr int64_t kMostTileGroups = (int64_t)1 << 16;
 
 // What one of W waves loads of a side: in every step sixteens of rows wave, wave + W, ...; every fourth step four groups' scales
 // of 64 rows, kSixteens / 4 of the waves.
@@ -249,29 +252,30 @@ template <int kSixteens, int W>
 struct SideLoads {
     static constexpr int kPer = kSixteens / W, kScaleWaves = kSixteens / 4;
     static_assert(kSixteens % W == 0, "every wave loads as much as the others");
-    const uint8_t *codes[kPer];
-    const uint8_t *scale;
+    const uint8_t *codes, *scales;          // of the tile's first row
+    uint32_t code_at[kPer], scale_at;       // this lane's rows from there
 
     __device__ __forceinline__ void start(const uint8_t *c, const uint8_t *s, int64_t row0, int64_t rows, int64_t blocks, int wave,
                                           int scale_wave, int lane)
     {
+        codes = c + row0 * blocks * 16;
+        scales = s + row0 * blocks;
+        const int most = rows - row0 < kSixteens * 16 ? (int)(rows - row0) - 1 : kSixteens * 16 - 1;
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
             const int place = (wave + W * i) * 16 + lane / 4;
-            int64_t row = row0 + place;
-            if (row >= rows) row = rows - 1;                        // loaded twice, stored nowhere
-            codes[i] = c + row * blocks * 16 + ((lane & 3) ^ (place >> 2 & 3)) * 16;
+            const uint32_t row = place < most ? place : most;       // past the end the last row again, stored nowhere
+            code_at[i] = row * (uint32_t)blocks * 16 + ((lane & 3) ^ (place >> 2 & 3)) * 16;
         }
-        int64_t row = row0 + scale_wave * 64 + lane;
-        if (row >= rows) row = rows - 1;
-        scale = s + row * blocks;
+        const int place = scale_wave * 64 + lane;
+        scale_at = (uint32_t)(place < most ? place : most) * (uint32_t)blocks;
     }
-    // step `at`'s codes into the buffer at LDS address `to`
-    __device__ __forceinline__ void issue(uint32_t to, int64_t at, int wave) const
+    // sixteen i of this wave, of step `at`, into the buffer at LDS address `to`
+    __device__ __forceinline__ void issue(int i, uint32_t to, int64_t at, int wave) const
     {
-#pragma unroll
-        for (int i = 0; i < kPer; ++i) direct_load(to + (wave + W * i) * 1024, codes[i] + at * 64);
+        direct_load(to + (wave + W * i) * 1024, codes + at * 64, code_at[i]);
     }
+    __device__ __forceinline__ void issue_scales(uint32_t to, int64_t group) const { direct_load(to, scales + group * 4, scale_at); }
 };
 
 // 32 rows of a step in registers.
@@ -331,22 +335,28 @@ __global__ __launch_bounds__(64 * WN * WM) void product_tiles_kernel(Global<cons
     // Scales come four groups at a time; the last four of a row may begin inside the four before.
     auto window = [&](int step) { return (step & ~3) + 4 <= groups ? step & ~3 : groups - 4; };
     // phase: step % 4, known when the program is built
-    auto issue = [&](int step, auto phase) {
+    auto issue = [&](int step, auto phase, int part, int parts) {
         constexpr int kPhase = decltype(phase)::value;
         const uint32_t to = base + kPhase * kStage;
         const int64_t at = step < groups ? step : groups - 1;               // past the end: loaded again, not used
-        if (kPhase == 0) {      // before the codes, so that a wait for these is one for them; past the end, the last four again
+        if (kPhase == 0 && part == 0) {      // before the codes, so that a wait for these is one for them; past the end, the last four again
             const uint32_t scales = base + kRing * kStage + (uint32_t)(step / 4 % 2) * kScales;
-            const int from = window(step) * 4;
-            if (kScaleN == W || wave < kScaleN) direct_load(scales + wave * 1024, wl.scale + from);
+            const int from = window(step);
+            if (kScaleN == W || wave < kScaleN) wl.issue_scales(scales + wave * 1024, from);
             if (kBoth && kScaleM == W) {
-                direct_load(scales + kScalesN + scale_m * 1024, xl.scale + from);
+                xl.issue_scales(scales + kScalesN + scale_m * 1024, from);
             } else if (scale_m >= 0 && scale_m < kScaleM) {
-                direct_load(scales + kScalesN + scale_m * 1024, xl.scale + from);
+                xl.issue_scales(scales + kScalesN + scale_m * 1024, from);
             }
         }
-        wl.issue(to, at, wave);
-        xl.issue(to + kSideN, at, wave);
+#pragma unroll
+        for (int i = 0; i < LoadsN::kPer; ++i) {
+            if (i * parts / LoadsN::kPer == part) wl.issue(i, to, at, wave);
+        }
+#pragma unroll
+        for (int i = 0; i < LoadsM::kPer; ++i) {
+            if (i * parts / LoadsM::kPer == part) xl.issue(i, to + kSideN, at, wave);
+        }
     };
     v16f sum[FN][FM];
 #pragma unroll
@@ -366,9 +376,9 @@ __global__ __launch_bounds__(64 * WN * WM) void product_tiles_kernel(Global<cons
     auto read_x = [&](Rows32 &to, int step, int phase, int j) {
         to.read(lds + phase * kStage + kSideN, scales(step) + kScalesN, part_m * FM + j, (step - window(step)) & 3, lane);
     };
-    issue(0, std::integral_constant<int, 0>{});
-    issue(1, std::integral_constant<int, 1>{});
-    issue(2, std::integral_constant<int, 2>{});
+    issue(0, std::integral_constant<int, 0>{}, 0, 1);
+    issue(1, std::integral_constant<int, 1>{}, 0, 1);
+    issue(2, std::integral_constant<int, 2>{}, 0, 1);
     asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"((kRing - 2) * kStepLoads) : "memory");
 #pragma unroll
     for (int j = 0; j < FM; ++j) read_x(x[0][j], 0, 0, j);
@@ -377,24 +387,33 @@ __global__ __launch_bounds__(64 * WN * WM) void product_tiles_kernel(Global<cons
         constexpr int kPhase = decltype(phase)::value, kNow = kPhase % 2, kNext = (kPhase + 1) % 4;
         // step at + 1 is in LDS for all waves, and step at - 1 has been read by all: its buffer is free
         asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((kRing - 3) * kStepLoads) : "memory");
-        issue(at + kRing - 1, std::integral_constant<int, (kPhase + kRing - 1) % 4>{});
         uint32_t sx[FM];
 #pragma unroll
         for (int j = 0; j < FM; ++j) sx[j] = x[kNow][j].scales >> (8 * h);
 #pragma unroll
         for (int i = 0; i < FN; ++i) {
-            if (i + 1 < FN) {
-                read_w(w[(i + 1) % 2], at, kPhase, i + 1);
-            } else {
-                read_w(w[0], at + 1, kNext, 0);
-            }
-            if (i < FM) read_x(x[1 - kNow][i], at + 1, kNext, i);
             const uint32_t sw = w[i % 2].scales >> (8 * h);
+            // What else a line has to do goes between its instructions, a little at a time: a wave issues in order, and 32
+            // cycles of the matrix unit hide a handful of other instructions and no more.
 #pragma unroll
-            for (int j = 0; j < FM; ++j) sum[i][j] = multiply32<0>(w[i % 2], sw, x[kNow][j], sx[j], sum[i][j]);
+            for (int j = 0; j < FM; ++j) {
+                sum[i][j] = multiply32<0>(w[i % 2], sw, x[kNow][j], sx[j], sum[i][j]);
+                if (j == 0) {
+                    if (i + 1 < FN) {
+                        read_w(w[(i + 1) % 2], at, kPhase, i + 1);
+                    } else {
+                        read_w(w[0], at + 1, kNext, 0);
+                    }
+                }
+                if (j == 1 % FM && i < FM) read_x(x[1 - kNow][i], at + 1, kNext, i);
+                __builtin_amdgcn_sched_barrier(0);
+            }
 #pragma unroll
-            for (int j = 0; j < FM; ++j) sum[i][j] = multiply32<1>(w[i % 2], sw, x[kNow][j], sx[j], sum[i][j]);
-            __builtin_amdgcn_sched_barrier(0);
+            for (int j = 0; j < FM; ++j) {
+                sum[i][j] = multiply32<1>(w[i % 2], sw, x[kNow][j], sx[j], sum[i][j]);
+                if (j == 0) issue(at + kRing - 1, std::integral_constant<int, (kPhase + kRing - 1) % 4>{}, i, FN);
+                __builtin_amdgcn_sched_barrier(0);
+            }
         }
     };
     // No branch inside four steps: a compiler that may moves the instructions of one past the next one's wait.
