@@ -226,16 +226,15 @@ __global__ __launch_bounds__(64 * W) void product_rows_kernel(Global<const uint8
 
 // ---- large products
 // A workgroup of WN x WM waves has WN * FN * 32 rows of w by WM * FM * 32 rows of x, a wave FN x FM results of 32 x 32 in
-// registers.  The 128 elements of a step (a group) come to LDS with direct loads, kept in kRing buffers that are filled kRing - 1
-// steps ahead; a step is two 32x32x64 instructions a result, whose lane l has row l % 32 and block l / 32 of two.
+// registers.  A step is the 128 elements of a group, two 32x32x64 instructions a result, whose lane l has row l % 32 and block l / 32
+// of two.  Codes come to LDS with direct loads of two steps, a pair, into one of two buffers: a pair is asked for when
+// the one before last has been read, two steps before its own turn.
 //
-// In LDS a row of a step is 64 bytes, and rows follow each other as the lanes of a direct load do, four lanes a row (with a row
-// spread over distant lanes the loads of 8192 cubed took 40 % longer).  The four blocks of row r stand in the order of their number
-// xor r / 4 % 4, so that one block of sixteen rows is in all banks once.  Scales: the four bytes of a row
-// and step are a word; a lane shifts it by its block and the instruction picks byte 0 or 2.  Rows' scales lie far apart, a line
-// each, so that they are loaded for four steps at once (with a word a step they were half of the requests: 348 us, 283 us).
-
-constexpr int kRing = 4;
+// In LDS a row of a pair is 128 bytes, a line of memory, and rows follow each other as the lanes of a direct load do, eight
+// lanes a row (rows spread over distant lanes, or half lines, are more requests: 8192 cubed 383 and 291 us).  The eight blocks of
+// row r stand in the order of their number xor r / 2 % 8, so that one block of sixteen rows is in all banks once.  Scales: the
+// four bytes of a row and step are a word; a lane shifts it by its block and the instruction picks byte 0 or 2.  Rows' scales lie
+// far apart, a line each, so that they are loaded for four steps at once (a word a step: half of all requests).
 
 // One direct load of 16 bytes a lane: LDS `to` + lane * 16 <- `from` + `offset`.
 __device__ __forceinline__ void direct_load(uint32_t to, const uint8_t *from, uint32_t offset)
@@ -246,12 +245,12 @@ __device__ __forceinline__ void direct_load(uint32_t to, const uint8_t *from, ui
 // The longest row of codes whose 256 a lane's 32-bit offset reaches.
 constexpr int64_t kMostTileGroups = (int64_t)1 << 16;
 
-// What one of W waves loads of a side: in every step sixteens of rows wave, wave + W, ...; every fourth step four groups' scales
-// of 64 rows, kSixteens / 4 of the waves.
-template <int kSixteens, int W>
+// What one of W waves loads of a side: of every pair eights of rows wave, wave + W, ...; of every second one four groups' scales of
+// 64 rows, if the wave is one of the first kEights / 8.
+template <int kEights, int W>
 struct SideLoads {
-    static constexpr int kPer = kSixteens / W, kScaleWaves = kSixteens / 4;
-    static_assert(kSixteens % W == 0, "every wave loads as much as the others");
+    static constexpr int kPer = kEights / W, kScaleWaves = kEights / 8;
+    static_assert(kEights % W == 0, "every wave loads as much as the others");
     const uint8_t *codes, *scales;          // of the tile's first row
     uint32_t code_at[kPer], scale_at;       // this lane's rows from there
 
@@ -260,20 +259,22 @@ struct SideLoads {
     {
         codes = c + row0 * blocks * 16;
         scales = s + row0 * blocks;
-        const int most = rows - row0 < kSixteens * 16 ? (int)(rows - row0) - 1 : kSixteens * 16 - 1;
+        const int most = rows - row0 < kEights * 8 ? (int)(rows - row0) - 1 : kEights * 8 - 1;
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
-            const int place = (wave + W * i) * 16 + lane / 4;
+            const int place = (wave + W * i) * 8 + lane / 8;
             const uint32_t row = place < most ? place : most;       // past the end the last row again, stored nowhere
-            code_at[i] = row * (uint32_t)blocks * 16 + ((lane & 3) ^ (place >> 2 & 3)) * 16;
+            code_at[i] = row * (uint32_t)blocks * 16 + block(lane, wave + W * i) * 16;
         }
         const int place = scale_wave * 64 + lane;
         scale_at = (uint32_t)(place < most ? place : most) * (uint32_t)blocks;
     }
-    // sixteen i of this wave, of step `at`, into the buffer at LDS address `to`
-    __device__ __forceinline__ void issue(int i, uint32_t to, int64_t at, int wave) const
+    static __device__ __forceinline__ int block(int lane, int eight) { return (lane & 7) ^ ((eight * 8 + lane / 8) >> 1 & 7); }
+    // eight i of this wave, from step `at` on, into the buffer at LDS address `to`; `one`: a row has no second step
+    __device__ __forceinline__ void issue(int i, uint32_t to, int64_t at, bool one, int wave, int lane) const
     {
-        direct_load(to + (wave + W * i) * 1024, codes + at * 64, code_at[i]);
+        const uint32_t second = one && block(lane, wave + W * i) >= 4 ? 64 : 0;
+        direct_load(to + (wave + W * i) * 1024, codes + at * 64, code_at[i] - second);
     }
     __device__ __forceinline__ void issue_scales(uint32_t to, int64_t group) const { direct_load(to, scales + group * 4, scale_at); }
 };
@@ -283,14 +284,14 @@ struct Rows32 {
     u32x4 codes[2];
     uint32_t scales;
 
-    // rows 32 i .. 32 i + 31 of a side's codes and of its scales, `group` of the four there
-    __device__ __forceinline__ void read(const uint8_t *side, const uint8_t *side_scales, int i, int group, int lane)
+    // rows 32 i .. 32 i + 31 of a side's pair, its first step or its second, and of its scales, `group` of the four there
+    __device__ __forceinline__ void read(const uint8_t *side, const uint8_t *side_scales, int i, int second, int group, int lane)
     {
         const int r = lane & 31, h = lane >> 5;
-        const uint8_t *const row = side + i * 2048 + r * 64;
-        const int swizzle = (h ^ (r >> 2 & 3)) * 16;
-        codes[0] = *reinterpret_cast<const u32x4 *>(row + swizzle);
-        codes[1] = *reinterpret_cast<const u32x4 *>(row + (swizzle ^ 32));
+        const uint8_t *const row = side + i * 4096 + r * 128;
+        const int swizzle = (h ^ (r >> 1 & 7)) * 16;
+        codes[0] = *reinterpret_cast<const u32x4 *>(row + (swizzle ^ second * 64));
+        codes[1] = *reinterpret_cast<const u32x4 *>(row + (swizzle ^ (second * 64 + 32)));
         scales = *reinterpret_cast<const uint32_t *>(side_scales + (i * 32 + r) * 16 + group * 4);
     }
 };
@@ -304,43 +305,54 @@ __device__ __forceinline__ v16f multiply32(const Rows32 &w, uint32_t w_scale, co
     return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, sum, 4, 4, 2 * kHalf, (int)w_scale, 2 * kHalf, (int)x_scale);
 }
 
+// A tile of results in LDS to memory, as far as `rows` and `cols` go.
+template <int kThreadsOf, int kRows, int kElems, int kBytes>
+__device__ __forceinline__ void store_tile(const uint8_t *tile, uint16_t *out, int64_t stride, int64_t rows, int64_t cols)
+{
+    constexpr int kLanes = kElems / 8;
+    const int col = threadIdx.x % kLanes * 8;
+#pragma unroll 4
+    for (int row = threadIdx.x / kLanes; row < kRows; row += kThreadsOf / kLanes) {
+        if (row < rows) store_row8(out + row * stride, col, cols, *reinterpret_cast<const u32x4 *>(tile + row * kBytes + col * 2));
+    }
+}
+
 template <int WN, int WM, int FN, int FM>
 __global__ __launch_bounds__(64 * WN * WM) void product_tiles_kernel(Global<const uint8_t> xc, Global<const uint8_t> xs,
                                                                      Global<const uint8_t> wc, Global<const uint8_t> ws,
                                                                      Global<uint16_t> out, int32_t M, int32_t N, int32_t groups,
                                                                      int64_t out_stride, uint32_t tiles_n, uint32_t tiles_m)
 {
-    constexpr int W = WN * WM, kSixteenN = WN * FN * 2, kSixteenM = WM * FM * 2;
-    constexpr int kSideN = kSixteenN * 1024, kStage = kSideN + kSixteenM * 1024;
-    constexpr int kScalesN = kSixteenN * 256, kScales = kScalesN + kSixteenM * 256;
-    __shared__ __align__(1024) uint8_t lds[kRing * kStage + 2 * kScales];
+    constexpr int W = WN * WM, kEightN = WN * FN * 4, kEightM = WM * FM * 4;
+    constexpr int kSideN = kEightN * 1024, kPair = kSideN + kEightM * 1024;
+    constexpr int kScalesN = kEightN * 128, kScales = kScalesN + kEightM * 128;
+    __shared__ __align__(1024) uint8_t lds[2 * (kPair + kScales)];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int h = lane >> 5;
     const uint32_t tile_n = blockIdx.x % tiles_n, tile_m = blockIdx.x / tiles_n;
-    const int64_t n0 = (int64_t)tile_n * (kSixteenN * 16), m0 = (int64_t)tile_m * (kSixteenM * 16);
+    const int64_t n0 = (int64_t)tile_n * (kEightN * 8), m0 = (int64_t)tile_m * (kEightM * 8);
     const int64_t blocks = (int64_t)groups * 4;
-    using LoadsN = SideLoads<kSixteenN, W>;
-    using LoadsM = SideLoads<kSixteenM, W>;
+    using LoadsN = SideLoads<kEightN, W>;
+    using LoadsM = SideLoads<kEightM, W>;
     // the waves share out the scales: one load of either side each, or one of one side
     constexpr int kScaleN = LoadsN::kScaleWaves, kScaleM = LoadsM::kScaleWaves;
     constexpr bool kBoth = kScaleN + kScaleM > W;
-    static_assert(kBoth ? kScaleN <= W && kScaleM <= W : true, "at most one load of a side");
+    static_assert(kScaleN <= W && kScaleM <= W, "at most one load of a side");
     LoadsN wl;
     LoadsM xl;
     const int scale_m = kBoth ? wave : wave - kScaleN;
     wl.start(wc, ws, n0, N, blocks, wave, wave, lane);
     xl.start(xc, xs, m0, M, blocks, wave, scale_m, lane);
     const uint32_t base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)lds;
-    constexpr int kStepLoads = LoadsN::kPer + LoadsM::kPer;
     // Scales come four groups at a time; the last four of a row may begin inside the four before.
     auto window = [&](int step) { return (step & ~3) + 4 <= groups ? step & ~3 : groups - 4; };
-    // phase: step % 4, known when the program is built
-    auto issue = [&](int step, auto phase, int part, int parts) {
+    // A part of the loads of the pair that begins at `step`; phase: step % 4, known when the program is built.
+    constexpr int kParts = 4 * FM;
+    auto issue = [&](int step, auto phase, int part) {
         constexpr int kPhase = decltype(phase)::value;
-        const uint32_t to = base + kPhase * kStage;
-        const int64_t at = step < groups ? step : groups - 1;               // past the end: loaded again, not used
-        if (kPhase == 0 && part == 0) {      // before the codes, so that a wait for these is one for them; past the end, the last four again
-            const uint32_t scales = base + kRing * kStage + (uint32_t)(step / 4 % 2) * kScales;
+        const uint32_t to = base + kPhase / 2 * kPair;
+        if (kPhase == 0 && part == 0) {         // past the end, the last four again
+            const uint32_t scales = base + 2 * kPair + (uint32_t)(step / 4 % 2) * kScales;
             const int from = window(step);
             if (kScaleN == W || wave < kScaleN) wl.issue_scales(scales + wave * 1024, from);
             if (kBoth && kScaleM == W) {
@@ -349,13 +361,15 @@ __global__ __launch_bounds__(64 * WN * WM) void product_tiles_kernel(Global<cons
                 xl.issue_scales(scales + kScalesN + scale_m * 1024, from);
             }
         }
+        const int64_t at = step < groups ? step : groups - 1;               // past the end: loaded again, not used
+        const bool one = at + 1 == groups;
 #pragma unroll
         for (int i = 0; i < LoadsN::kPer; ++i) {
-            if (i * parts / LoadsN::kPer == part) wl.issue(i, to, at, wave);
+            if (i * kParts / LoadsN::kPer == part) wl.issue(i, to, at, one, wave, lane);
         }
 #pragma unroll
         for (int i = 0; i < LoadsM::kPer; ++i) {
-            if (i * parts / LoadsM::kPer == part) xl.issue(i, to + kSideN, at, wave);
+            if (i * kParts / LoadsM::kPer == part) xl.issue(i, to + kSideN, at, one, wave, lane);
         }
     };
     v16f sum[FN][FM];
@@ -364,37 +378,40 @@ __global__ __launch_bounds__(64 * WN * WM) void product_tiles_kernel(Global<cons
 #pragma unroll
         for (int j = 0; j < FM; ++j) sum[i][j] = v16f{0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
 
-    // Of w a lane holds this line of results' rows and the next line's, of x all of this step's and those of the next as they
-    // come: nothing is waited for that was asked for less than a line ago.
+    // Of w a lane holds this line of results' rows and the next line's, of x all of this step's and those of the next.
     Rows32 w[2], x[2][FM];
     static_assert(FN % 2 == 0 && FM <= FN, "a step asks for the next one's rows of x line by line");
     const int part_n = wave % WN, part_m = wave / WN;
-    auto scales = [&](int step) { return lds + kRing * kStage + (uint32_t)(step / 4 % 2) * kScales; };
+    auto scales = [&](int step) { return lds + 2 * kPair + (uint32_t)(step / 4 % 2) * kScales; };
     auto read_w = [&](Rows32 &to, int step, int phase, int i) {
-        to.read(lds + phase * kStage, scales(step), part_n * FN + i, (step - window(step)) & 3, lane);
+        to.read(lds + phase / 2 * kPair, scales(step), part_n * FN + i, phase % 2, (step - window(step)) & 3, lane);
     };
     auto read_x = [&](Rows32 &to, int step, int phase, int j) {
-        to.read(lds + phase * kStage + kSideN, scales(step) + kScalesN, part_m * FM + j, (step - window(step)) & 3, lane);
+        to.read(lds + phase / 2 * kPair + kSideN, scales(step) + kScalesN, part_m * FM + j, phase % 2, (step - window(step)) & 3, lane);
     };
-    issue(0, std::integral_constant<int, 0>{}, 0, 1);
-    issue(1, std::integral_constant<int, 1>{}, 0, 1);
-    issue(2, std::integral_constant<int, 2>{}, 0, 1);
-    asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"((kRing - 2) * kStepLoads) : "memory");
+    using std::integral_constant;
+#pragma unroll
+    for (int part = 0; part < kParts; ++part) issue(0, integral_constant<int, 0>{}, part);
+#pragma unroll
+    for (int part = 0; part < FM; ++part) issue(2, integral_constant<int, 2>{}, part);
+    asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"((LoadsN::kPer + LoadsM::kPer) / 4) : "memory");
 #pragma unroll
     for (int j = 0; j < FM; ++j) read_x(x[0][j], 0, 0, j);
     read_w(w[0], 0, 0, 0);
+    // What else a line has to do goes between its instructions, a little at a time: a wave issues in order.
     auto step = [&](int at, auto phase) {
         constexpr int kPhase = decltype(phase)::value, kNow = kPhase % 2, kNext = (kPhase + 1) % 4;
-        // step at + 1 is in LDS for all waves, and step at - 1 has been read by all: its buffer is free
-        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((kRing - 3) * kStepLoads) : "memory");
+        constexpr bool kSecond = kPhase % 2 == 1;
         uint32_t sx[FM];
 #pragma unroll
         for (int j = 0; j < FM; ++j) sx[j] = x[kNow][j].scales >> (8 * h);
 #pragma unroll
         for (int i = 0; i < FN; ++i) {
             const uint32_t sw = w[i % 2].scales >> (8 * h);
-            // What else a line has to do goes between its instructions, a little at a time: a wave issues in order, and 32
-            // cycles of the matrix unit hide a handful of other instructions and no more.
+            if (kSecond && i + 1 == FN) {
+                // the next pair is in LDS for all waves, and this one has been read by all: its buffer is free
+                asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+            }
 #pragma unroll
             for (int j = 0; j < FM; ++j) {
                 sum[i][j] = multiply32<0>(w[i % 2], sw, x[kNow][j], sx[j], sum[i][j]);
@@ -405,57 +422,62 @@ __global__ __launch_bounds__(64 * WN * WM) void product_tiles_kernel(Global<cons
                         read_w(w[0], at + 1, kNext, 0);
                     }
                 }
-                if (j == 1 % FM && i < FM) read_x(x[1 - kNow][i], at + 1, kNext, i);
+                if (kSecond && i + 1 == FN) {
+                    read_x(x[1 - kNow][j], at + 1, kNext, j);
+                } else if (!kSecond && j == 1 % FM && i < FM) {
+                    read_x(x[1 - kNow][i], at + 1, kNext, i);
+                }
                 __builtin_amdgcn_sched_barrier(0);
             }
 #pragma unroll
             for (int j = 0; j < FM; ++j) {
                 sum[i][j] = multiply32<1>(w[i % 2], sw, x[kNow][j], sx[j], sum[i][j]);
-                if (j == 0) issue(at + kRing - 1, std::integral_constant<int, (kPhase + kRing - 1) % 4>{}, i, FN);
+                // (four loads in a row instead of one an instruction: 277 us for 8192 cubed, sixteen: 298)
+                if (kSecond && i + 1 == FN) issue(at + 3, integral_constant<int, (kPhase + 3) % 4>{}, j);
+                if (!kSecond && i < 3) issue(at + 2, integral_constant<int, (kPhase + 2) % 4>{}, (i + 1) * FM + j);
                 __builtin_amdgcn_sched_barrier(0);
+            }
+            if (!kSecond && i + 1 == FN) {
+#pragma unroll
+                for (int part = (FN + 1) * FM; part < kParts; ++part) issue(at + 2, integral_constant<int, (kPhase + 2) % 4>{}, part);
             }
         }
     };
     // No branch inside four steps: a compiler that may moves the instructions of one past the next one's wait.
     int at = 0;
     for (; at + 4 <= groups; at += 4) {
-        step(at, std::integral_constant<int, 0>{});
-        step(at + 1, std::integral_constant<int, 1>{});
-        step(at + 2, std::integral_constant<int, 2>{});
-        step(at + 3, std::integral_constant<int, 3>{});
+        step(at, integral_constant<int, 0>{});
+        step(at + 1, integral_constant<int, 1>{});
+        step(at + 2, integral_constant<int, 2>{});
+        step(at + 3, integral_constant<int, 3>{});
     }
-    if (at < groups) step(at, std::integral_constant<int, 0>{});
-    if (at + 1 < groups) step(at + 1, std::integral_constant<int, 1>{});
-    if (at + 2 < groups) step(at + 2, std::integral_constant<int, 2>{});
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");            // what was loaded past the end lands before LDS is another's
-
-    // A lane has four consecutive outputs at 8 q + 4 h: after the exchange of halves it has eight, of an even q or an odd one.
-    const bool wide = out_stride % 8 == 0;
+    if (at < groups) step(at, integral_constant<int, 0>{});
+    if (at + 1 < groups) step(at + 1, integral_constant<int, 1>{});
+    if (at + 2 < groups) step(at + 2, integral_constant<int, 2>{});
+    // What was loaded past the end lands, all waves have read: LDS takes the results, bf16, a row of x after the other, from where
+    // they leave in rows as long as the tile.  (Stored from registers, 32 bytes a row at a time, they took 2.5 us longer a tile,
+    // and twice that where a row begins at an odd element.)
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    constexpr int kRowElems = WN * FN * 32, kRowBytes = kRowElems * 2 + 16, kRows = WM * FM * 32;
+    static_assert(kRows * kRowBytes <= (int)sizeof(lds), "the results take the codes' place");
 #pragma unroll
     for (int j = 0; j < FM; ++j) {
-        const int64_t m = m0 + (part_m * FM + j) * 32 + (lane & 31);
-        uint16_t *const row = out + m * out_stride;
+        uint8_t *const row = lds + ((part_m * FM + j) * 32 + (lane & 31)) * kRowBytes;
 #pragma unroll
         for (int i = 0; i < FN; ++i) {
 #pragma unroll
-            for (int q = 0; q < 4; q += 2) {
+            for (int q = 0; q < 4; q += 2) {        // a lane has four outputs from 8 q + 4 h on; after the exchange eight of one q
                 const v16f &s = sum[i][j];
                 auto lo = __builtin_amdgcn_permlane32_swap(narrow_bf16x2(s[4 * q], s[4 * q + 1]),
                                                            narrow_bf16x2(s[4 * q + 4], s[4 * q + 5]), false, false);
                 auto hi = __builtin_amdgcn_permlane32_swap(narrow_bf16x2(s[4 * q + 2], s[4 * q + 3]),
                                                            narrow_bf16x2(s[4 * q + 6], s[4 * q + 7]), false, false);
-                const int64_t n = n0 + (part_n * FN + i) * 32 + (q + h) * 8;
-                const u32x4 v = {lo[0], hi[0], lo[1], hi[1]};
-                if (m < M) {
-                    if (wide && n + 8 <= N) {
-                        *reinterpret_cast<u32x4 *>(row + n) = v;
-                    } else {
-                        store_row8(row, n, N, v);
-                    }
-                }
+                *reinterpret_cast<u32x4 *>(row + ((part_n * FN + i) * 32 + (q + h) * 8) * 2) = u32x4{lo[0], hi[0], lo[1], hi[1]};
             }
         }
     }
+    __syncthreads();
+    store_tile<64 * W, kRows, kRowElems, kRowBytes>(lds, out + m0 * out_stride + n0, out_stride, M - m0, N - n0);
 }
 
 }  // namespace mx4
