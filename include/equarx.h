@@ -389,8 +389,8 @@ int equarx_reduce_variant_hops_strided(const void *const *partials_bf16, int32_t
  * Rows are padded to whole groups of EQUARX_MX4_GROUP elements, 4 blocks; the
  * padding holds zero elements and is written by equarx_mx4_quantize.
  *
- * Limits of all calls here: rows, cols, M, N and K up to 2^31 - 1, and every
- * tensor up to 2^40 elements (EQUARX_BAD_SHAPE).  A row stride counts elements,
+ * Limits of all calls here: rows, cols, M and N up to 2^31 - 1, K up to 2^24, and
+ * every tensor up to 2^40 elements (EQUARX_BAD_SHAPE).  A row stride counts elements,
  * is at least the row's length, and need be a multiple of nothing.
  */
 #define EQUARX_MX4_BLOCK 32

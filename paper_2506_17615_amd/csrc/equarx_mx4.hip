@@ -49,22 +49,95 @@ void launch_quantize_rows(const uint16_t *x, int64_t rows, int64_t cols, int64_t
     });
 }
 
-void launch_product(const uint8_t *xc, const uint8_t *xs, const uint8_t *wc, const uint8_t *ws, int64_t M, int64_t N,
-                    int64_t K, uint16_t *out, int64_t out_stride, LaunchCtx &ctx)
+// A product's operands: x packed, or bf16 rows that the kernel packs (x_scales is then null and x_stride counts).
+struct Product {
+    const uint8_t *xc, *xs, *wc, *ws;
+    uint16_t *out;
+    int64_t M, N, K, out_stride, x_stride;
+};
+
+// Does a workgroup of the kernel for few rows pack x itself?
+inline bool packs_itself(int64_t M, int64_t K) { return M <= kMostQuantizedRows && M * groups_of(K) * kGroup <= kMostQuantized; }
+
+template <int WN, int WM, int FN, int FM, int kBuffers>
+void launch_tiles(const Product &p, LaunchCtx &ctx)
 {
-    const int32_t groups = (int32_t)groups_of(K);
-    if (M > 64 && groups >= 4 && groups <= kMostTileGroups) {
-        const uint32_t tiles_n = (uint32_t)((N + 255) / 256), tiles_m = (uint32_t)((M + 255) / 256);
-        ctx.launch(product_tiles_kernel<2, 2, 4, 4>, tiles_n * tiles_m, 256, xc, xs, wc, ws, out, (int32_t)M, (int32_t)N, groups,
-                   out_stride, tiles_n, tiles_m);
-        return;
+    constexpr int64_t kN = WN * FN * 32, kM = WM * FM * 32;
+    const int64_t tiles_n = (p.N + kN - 1) / kN;
+    const int64_t most = (kGridThreads / (64 * WN * WM)) / tiles_n * kM;        // rows of x in one launch
+    for (int64_t at = 0; at < p.M; at += most) {
+        const int64_t m = p.M - at < most ? p.M - at : most, tiles_m = (m + kM - 1) / kM;
+        const int64_t groups = groups_of(p.K);
+        ctx.launch(product_tiles_kernel<WN, WM, FN, FM, kBuffers>, (unsigned)(tiles_n * tiles_m), 64 * WN * WM, p.xc + at * groups * 64,
+                   p.xs + at * groups * 4, p.wc, p.ws, p.out + at * p.out_stride, (int32_t)m, (int32_t)p.N, (int32_t)groups,
+                   p.out_stride, (uint32_t)tiles_n, (uint32_t)tiles_m);
     }
-    const int64_t piece = 65535 * 64;                           // rows of x in one launch: the grid's second dimension
-    for (int64_t at = 0; at < M; at += piece) {
-        const int64_t m = M - at < piece ? M - at : piece;
-        ctx.launch2d(product_rows_kernel<4, 4>, (unsigned)((N + 15) / 16), (unsigned)((m + 63) / 64), 256,
-                     xc + at * groups * 64, xs + at * groups * 4, wc, ws, out + at * out_stride, (int32_t)m, (int32_t)N,
-                     groups, out_stride);
+}
+
+template <int MT, bool kQuantize>
+void launch_rows(const Product &p, LaunchCtx &ctx)
+{
+    const int64_t groups = groups_of(p.K);
+    constexpr int64_t kPieceN = (int64_t)1 << 26, kPieceM = (int64_t)32768 * 32 * MT;      // of one launch
+    for (int64_t n = 0; n < p.N; n += kPieceN) {
+        const int64_t N = p.N - n < kPieceN ? p.N - n : kPieceN;
+        for (int64_t m = 0; m < p.M; m += kPieceM) {
+            const int64_t M = p.M - m < kPieceM ? p.M - m : kPieceM;
+            ctx.launch2d(product_rows_kernel<MT, kQuantize>, (unsigned)((N + 31) / 32), (unsigned)((M + 32 * MT - 1) / (32 * MT)),
+                         256, kQuantize ? p.xc : p.xc + m * groups * 64, kQuantize ? p.xs : p.xs + m * groups * 4,
+                         p.wc + n * groups * 64, p.ws + n * groups * 4, p.out + m * p.out_stride + n, (int32_t)M, (int32_t)N,
+                         (int32_t)groups, p.out_stride, p.x_stride, (int32_t)p.K);
+        }
+    }
+}
+
+// Which kernel takes a product.  Up to 64 rows of x: the one for few rows.  Above, the smallest tile whose workgroups the chip's 256
+// CUs hold at once, one each, since a workgroup alone on its CU waits for loads more than for anything; with more workgroups
+// than that 128 x 128 with two on a CU, or 256 x 256, by the rounds they make, whole rounds and part ones (the mean of the
+// two), of 0.70 and 1.09 us a group of k.  Measured on MI355X, us (w rows n x x rows m; products of N x K):
+//                           128 x 64    128 x 128     two a CU
+//     M     N x K           32 x 128     4 buffers     2 buffers   256 x 256
+//     96    5376 x 5376     10.4   12.3     16.0          19.5       30.7
+//     192                   19.8   12.9     17.0          20.3       32.8
+//     333                   21.4   14.5     17.7          21.2       34.0
+//     512                   30.7   24.9     19.3          22.3       34.4
+//     1024                   --    39.5     36.0          29.0       37.8
+//     2048                   --    76.6     59.7          51.7       44.6
+//     192   2560 x 8192     14.0   15.7     22.2          27.9       43.6
+//     512                   27.5   16.6     22.8          28.5       45.3
+//     1024                   --    31.5     24.3          29.5       46.1
+//     2048                   --    46.9     47.0          38.8       48.7
+//     192   8192 x 1024      9.7    5.3      6.6           6.2       11.4
+//     512                   20.0    9.5      7.7           7.5       12.8
+//     1024                   --    17.4     13.5          11.8       14.7
+//     2048                   --    32.3     24.7          19.6       16.9
+//     8192  8192 x 8192                                    363        279
+// Fewer than four groups of k have their scales loaded one by one, which only the kernel for few rows does.
+constexpr int64_t kCUs = 256;
+
+void launch_product(const Product &p, LaunchCtx &ctx)
+{
+    const int64_t groups = groups_of(p.K);
+    auto tiles = [&](int64_t n, int64_t m) { return ((p.N + n - 1) / n) * ((p.M + m - 1) / m); };
+    auto rounds = [](int64_t t, int64_t at_once) { return (double)t / at_once + (double)((t + at_once - 1) / at_once); };
+    if (p.M <= 32) {
+        if (p.xs || groups == 0) {
+            launch_rows<1, false>(p, ctx);
+        } else {
+            launch_rows<1, true>(p, ctx);
+        }
+    } else if (p.M <= 64) {
+        launch_rows<2, false>(p, ctx);
+    } else if (groups < 4 || tiles(32, 128) <= kCUs) {
+        launch_rows<4, false>(p, ctx);
+    } else if (tiles(128, 64) <= kCUs) {
+        launch_tiles<2, 2, 2, 1, 4>(p, ctx);
+    } else if (tiles(128, 128) <= kCUs) {
+        launch_tiles<2, 2, 2, 2, 4>(p, ctx);
+    } else if (rounds(tiles(128, 128), 2 * kCUs) * 0.70 < rounds(tiles(256, 256), kCUs) * 1.09) {
+        launch_tiles<2, 2, 2, 2, 2>(p, ctx);
+    } else {
+        launch_tiles<2, 2, 4, 4, 2>(p, ctx);
     }
 }
 
@@ -84,7 +157,7 @@ Workspace plan_workspace(int64_t M, int64_t K)
 
 int check_product(int64_t M, int64_t N, int64_t K, int64_t out_stride)
 {
-    if (M < 0 || N < 0 || K < 0 || M > kMostRows || N > kMostRows || K > kMostRows) return EQUARX_BAD_SHAPE;
+    if (M < 0 || N < 0 || K < 0 || M > kMostRows || N > kMostRows || K > kMostK) return EQUARX_BAD_SHAPE;
     if (int st = check_rows(M, N, out_stride)) return st;
     if (int st = check_rows(M, K, K)) return st;
     return check_rows(N, K, K);
@@ -168,7 +241,7 @@ int equarx_mx4_product(const uint8_t *x_codes, const uint8_t *x_scales, const ui
     mem.writes(out_bf16, row_bytes(M, N, out_stride));
     mem.writes(workspace, need);
     if (int st = mem.check()) return st;
-    launch_product(x_codes, x_scales, w_codes, w_scales, M, N, K, static_cast<uint16_t *>(out_bf16), out_stride, ctx);
+    launch_product({x_codes, x_scales, w_codes, w_scales, static_cast<uint16_t *>(out_bf16), M, N, K, out_stride, 0}, ctx);
     return ctx.status();
 }
 
@@ -198,8 +271,14 @@ int equarx_mx4_linear(const void *x_bf16, int64_t x_stride, const uint8_t *w_cod
     if (int st = mem.check()) return st;
     uint8_t *const codes = static_cast<uint8_t *>(workspace);
     uint8_t *const scales = codes ? codes + plan.scales : nullptr;
-    if (K > 0) launch_quantize_rows(static_cast<const uint16_t *>(x_bf16), M, K, x_stride, codes, scales, ctx);
-    launch_product(codes, scales, w_codes, w_scales, M, N, K, static_cast<uint16_t *>(out_bf16), out_stride, ctx);
+    Product p{codes, scales, w_codes, w_scales, static_cast<uint16_t *>(out_bf16), M, N, K, out_stride, x_stride};
+    if (packs_itself(M, K)) {
+        p.xc = static_cast<const uint8_t *>(x_bf16);
+        p.xs = nullptr;
+    } else if (K > 0) {
+        launch_quantize_rows(static_cast<const uint16_t *>(x_bf16), M, K, x_stride, codes, scales, ctx);
+    }
+    launch_product(p, ctx);
     return ctx.status();
 }
 

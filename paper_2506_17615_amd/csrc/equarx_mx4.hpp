@@ -2,6 +2,7 @@
 #pragma once
 
 #include <type_traits>
+#include <utility>
 
 #include "equarx_device.hpp"
 
@@ -90,6 +91,17 @@ __device__ __forceinline__ uint32_t magnitudes_max(const u32x4 &x)
     return umax16x2(umax16x2(x[0] & kMagnitude, x[1] & kMagnitude), umax16x2(x[2] & kMagnitude, x[3] & kMagnitude));
 }
 
+// Eight elements of a block as codes, with the block's scale byte; the other 24 are in the other lanes of the quad.
+__device__ __forceinline__ uint32_t pack_unit(const u32x4 &v, uint32_t &byte)
+{
+    uint32_t top = magnitudes_max(v);
+    top = umax(top & 0xffff, top >> 16);
+    top = umax(top, dpp_read<0xB1>(top));
+    top = umax(top, dpp_read<0x4E>(top));
+    byte = scale_byte(top);
+    return byte == 255 ? 0 : codes_of(v, scale_of(byte));
+}
+
 // ---------------------------------------------------------------- rows <-> packed rows
 // A lane has eight elements, a quad a block, a row of sixteen lanes a group: `units` pieces of eight in all, the
 // padding among them, `unit` counting through the packed rows.
@@ -102,13 +114,9 @@ __global__ __launch_bounds__(256) void quantize_rows_kernel(Global<const uint16_
     if (unit >= units) return;                                  // whole rows of sixteen lanes: units is a multiple of 16
     const uint32_t row = row_units.of(unit);
     const int64_t col = (int64_t)(unit - row * row_units.d) * 8;
+    uint32_t byte;
     const u32x4 v = load_row8(x + row * x_stride, col, cols);
-    uint32_t top = magnitudes_max(v);
-    top = umax(top & 0xffff, top >> 16);
-    top = umax(top, dpp_read<0xB1>(top));
-    top = umax(top, dpp_read<0x4E>(top));
-    const uint32_t byte = scale_byte(top);
-    reinterpret_cast<uint32_t *>((uint8_t *)codes)[unit] = byte == 255 ? 0 : codes_of(v, scale_of(byte));
+    reinterpret_cast<uint32_t *>((uint8_t *)codes)[unit] = pack_unit(v, byte);
     uint32_t four = byte << (8 * ((threadIdx.x >> 2) & 3));
     four |= dpp_read<0x141>(four);
     four |= dpp_read<0x140>(four);
@@ -142,33 +150,16 @@ __global__ __launch_bounds__(256) void dequantize_rows_kernel(Global<const uint8
 }
 
 // ---------------------------------------------------------------- product of packed rows
-// One 16x16x128 matrix instruction takes 128 elements of 16 rows of w and of 16 rows of x: lane l has row l % 16 and
-// its block l / 16 of four, with that block's scale.  Its result lane l has column l % 16 (a row of x) and the four rows
-// of w 4 * (l / 16) + 0 .. 3: four consecutive outputs.
+// With the operands as w (rows of the result) and x (its columns) one 32x32x64 instruction takes two blocks of 32 rows of w and of 32
+// rows of x: lane l has row l % 32 and one of the two, l / 32, with the block's scale, any byte of a register.  Its result
+// lane l has column l % 32, a row of x, and the rows of w 8 q + 4 (l / 32) + 0 .. 3, q = 0 .. 3: four consecutive outputs each.
 
-struct Packed {
-    const uint8_t *codes, *scales;
-    int64_t rows, blocks;
-};
-
-struct Fragment {
-    u32x4 codes;
-    uint32_t scale;
-};
-
-__device__ __forceinline__ Fragment load_fragment(const uint8_t *codes, const uint8_t *scales, int64_t block)
+template <int kScaleByte>
+__device__ __forceinline__ v16f multiply(const u32x4 &w, uint32_t w_scale, const u32x4 &x, uint32_t x_scale, const v16f &sum)
 {
-    Fragment f;
-    f.codes = *reinterpret_cast<const u32x4 *>(codes + block * 16);
-    f.scale = scales[block];
-    return f;
-}
-
-__device__ __forceinline__ v4f multiply(const Fragment &w, const Fragment &x, const v4f &sum)
-{
-    const v8i a = {(int)w.codes[0], (int)w.codes[1], (int)w.codes[2], (int)w.codes[3], 0, 0, 0, 0};
-    const v8i b = {(int)x.codes[0], (int)x.codes[1], (int)x.codes[2], (int)x.codes[3], 0, 0, 0, 0};
-    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, sum, 4, 4, 0, (int)w.scale, 0, (int)x.scale);
+    const v8i a = {(int)w.x, (int)w.y, (int)w.z, (int)w.w, 0, 0, 0, 0};
+    const v8i b = {(int)x.x, (int)x.y, (int)x.z, (int)x.w, 0, 0, 0, 0};
+    return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, sum, 4, 4, kScaleByte, (int)w_scale, kScaleByte, (int)x_scale);
 }
 
 // Four consecutive outputs of one row, as far as the row goes.
@@ -186,64 +177,214 @@ __device__ __forceinline__ void store_out4(uint16_t *row, int64_t n, int64_t N, 
     }
 }
 
-// Sixteen rows of w by MT * 16 rows of x in a workgroup, the sum over k cut into W parts, one for a wave, that are added
-// in order.
-template <int W, int MT>
-__global__ __launch_bounds__(64 * W) void product_rows_kernel(Global<const uint8_t> xc, Global<const uint8_t> xs,
-                                                              Global<const uint8_t> wc, Global<const uint8_t> ws,
-                                                              Global<uint16_t> out, int32_t M, int32_t N, int32_t groups,
-                                                              int64_t out_stride)
-{
-    __shared__ v4f part[W][MT][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int r = lane & 15, g = lane >> 4;
-    const int64_t n0 = (int64_t)blockIdx.x * 16, m0 = (int64_t)blockIdx.y * (16 * MT);
-    const int64_t blocks = (int64_t)groups * 4;
-    const int64_t wr = n0 + r < N ? n0 + r : N - 1;
-    v4f sum[MT];
-#pragma unroll
-    for (int t = 0; t < MT; ++t) sum[t] = v4f{0, 0, 0, 0};
-    const uint8_t *const wcr = wc + wr * blocks * 16, *const wsr = ws + wr * blocks;
-    for (int s = wave; s < groups; s += W) {
-        const Fragment w = load_fragment(wcr, wsr, 4 * s + g);
-#pragma unroll
-        for (int t = 0; t < MT; ++t) {
-            const int64_t m = m0 + 16 * t + r, xr = m < M ? m : M - 1;
-            sum[t] = multiply(w, load_fragment(xc + xr * blocks * 16, xs + xr * blocks, 4 * s + g), sum[t]);
-        }
-    }
-#pragma unroll
-    for (int t = 0; t < MT; ++t) part[wave][t][lane] = sum[t];
-    __syncthreads();
-    for (int t = wave; t < MT; t += W) {
-        v4f total = part[0][t][lane];
-#pragma unroll
-        for (int i = 1; i < W; ++i) total += part[i][t][lane];
-        const int64_t m = m0 + 16 * t + r;
-        if (m < M) store_out4(out + m * out_stride, n0 + 4 * g, N, total);
-    }
-}
-
-// ---- large products
-// A workgroup of WN x WM waves has WN * FN * 32 rows of w by WM * FM * 32 rows of x, a wave FN x FM results of 32 x 32 in
-// registers.  A step is the 128 elements of a group, two 32x32x64 instructions a result, whose lane l has row l % 32 and block l / 32
-// of two.  Codes come to LDS with direct loads of two steps, a pair, into one of two buffers: a pair is asked for when
-// the one before last has been read, two steps before its own turn.
-//
-// In LDS a row of a pair is 128 bytes, a line of memory, and rows follow each other as the lanes of a direct load do, eight
-// lanes a row (rows spread over distant lanes, or half lines, are more requests: 8192 cubed 383 and 291 us).  The eight blocks of
-// row r stand in the order of their number xor r / 2 % 8, so that one block of sixteen rows is in all banks once.  Scales: the
-// four bytes of a row and step are a word; a lane shifts it by its block and the instruction picks byte 0 or 2.  Rows' scales lie
-// far apart, a line each, so that they are loaded for four steps at once (a word a step: half of all requests).
-
 // One direct load of 16 bytes a lane: LDS `to` + lane * 16 <- `from` + `offset`.
 __device__ __forceinline__ void direct_load(uint32_t to, const uint8_t *from, uint32_t offset)
 {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(offset), "s"(from) : "memory", "m0");
 }
 
-// The longest row of codes whose 256 a lane's 32-bit offset reaches.
-constexpr int64_t kMostTileGroups = (int64_t)1 << 16;
+__device__ __forceinline__ void direct_load(uint32_t to, const uint8_t *from)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(to), "v"(from) : "memory", "m0");
+}
+
+// A lane's 32-bit offset reaches 256 rows of codes of the longest product there is.
+constexpr int64_t kMostK = (int64_t)1 << 24;
+
+// ---- few rows of x
+// A workgroup has 32 rows of w and MT * 32 rows of x, and walks over all of k; what bounds it is reading w once, so what counts is
+// bytes in flight.  Pairs of groups, 128 bytes of every row, come to LDS with direct loads, kDepth - 1 pairs ahead of their turn (a lane
+// that loads its row's bytes into registers itself has its neighbours on other lines: 64 rows of x by 5376 x 5376 15.4 us).
+// In a pair wave q of the four has the blocks 2 q and 2 q + 1 of all rows, one instruction for 32 rows of x; the waves' sums are added
+// in order at the end.  LDS: a row is its 128 bytes, block b of row r in place b xor r / 2 % 8, which spreads sixteen rows' block
+// over all banks; of scales four groups' 16 bytes a row, every second pair.
+//
+// kQuantize: x is bf16 and little; every workgroup packs all of it into LDS first, with its first rows of w on the way.
+
+constexpr int kMostQuantized = 1 << 15;             // elements of x that a workgroup packs itself, padded groups counted
+constexpr int kMostQuantizedRows = 32;
+
+template <int MT, bool kQuantize>
+constexpr int kRowsDepth = MT == 4 ? 6 : 8;
+
+template <int MT, bool kQuantize>
+__global__ __launch_bounds__(256) void product_rows_kernel(Global<const uint8_t> xc, Global<const uint8_t> xs,
+                                                           Global<const uint8_t> wc, Global<const uint8_t> ws, Global<uint16_t> out,
+                                                           int32_t M, int32_t N, int32_t groups, int64_t out_stride,
+                                                           int64_t x_stride, int32_t K)
+{
+    constexpr int W = 4, kSides = kQuantize ? 1 : 1 + MT;           // of 32 rows each, w first
+    constexpr int kDepth = kRowsDepth<MT, kQuantize>;
+    constexpr int kPair = kSides * 4096, kScales = (kSides * 512 + 1023) / 1024 * 1024;     // bytes of codes; of four groups' scales
+    constexpr int kWindows = kDepth / 2 + 1;                        // fours of groups that the pairs in flight are of
+    constexpr int kScalesAt = kDepth * kPair, kXAt = kScalesAt + kWindows * kScales;
+    constexpr int kPacked = kQuantize ? kMostQuantized / 2 + kMostQuantized / 32 + kMostQuantizedRows * 16 : 0;
+    constexpr int kAll = kXAt + kPacked, kParts = W * MT * 4096;
+    static_assert(kDepth % 2 == 0 && (!kQuantize || MT == 1), "fours are of two pairs; little is a tile's rows");
+    __shared__ __align__(1024) uint8_t lds[kAll > kParts ? kAll : kParts];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int r = lane & 31, h = lane >> 5;
+    const int64_t n0 = (int64_t)blockIdx.x * 32, m0 = (int64_t)blockIdx.y * (32 * MT);
+    const int64_t blocks = (int64_t)groups * 4;
+    const int pairs = (groups + 1) / 2;
+    const uint32_t base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)lds;
+
+    // x that is packed here: what a thread reads first is asked for before w
+    constexpr int kFirst = 4;
+    const int row_units = groups * 16, units = kQuantize ? M * row_units : 0, x_pitch = groups * 64 + 16;
+    u32x4 unit_of_x[kFirst];
+    auto load_unit = [&](int unit) {
+        const int row = unit / row_units, col = (unit - row * row_units) * 8;
+        return load_row8(reinterpret_cast<const uint16_t *>((const uint8_t *)xc) + row * x_stride, col, K);
+    };
+    auto pack = [&](int unit, const u32x4 &v) {                     // whole rows of sixteen lanes together
+        const int row = unit / row_units, at = unit - row * row_units;
+        uint32_t byte;
+        const uint32_t codes = pack_unit(v, byte);
+        *reinterpret_cast<uint32_t *>(lds + kXAt + row * x_pitch + at * 4) = codes;
+        if (unit % 4 == 0) lds[kXAt + M * x_pitch + unit / 4] = (uint8_t)byte;
+    };
+    if constexpr (kQuantize) {
+#pragma unroll
+        for (int i = 0; i < kFirst; ++i) {
+            const int unit = threadIdx.x + i * 64 * W;
+            unit_of_x[i] = unit < units ? load_unit(unit) : u32x4{0, 0, 0, 0};
+        }
+    }
+
+    // Loads: eight rows of a side are one, wave q has rows 8 q .. 8 q + 7 of every side; of scales it is 64 rows of all sides.
+    const uint8_t *code_from[kSides];
+    uint32_t code_at[kSides];
+    const int eight = wave * 8 + lane / 8, block = (lane & 7) ^ (eight >> 1 & 7);
+    auto row_of = [&](int side, int i) {                            // past the end the last row again, stored nowhere
+        const int64_t row = (side == 0 ? n0 : m0 + 32 * (side - 1)) + i, most = (side == 0 ? N : M) - 1;
+        return row < most ? row : most;
+    };
+#pragma unroll
+    for (int i = 0; i < kSides; ++i) {
+        code_from[i] = (i == 0 ? (const uint8_t *)wc : (const uint8_t *)xc) + row_of(i, 0) * blocks * 16;
+        code_at[i] = (uint32_t)((row_of(i, eight) - row_of(i, 0)) * blocks * 16) + block * 16;
+    }
+    const bool has_scales = wave * 64 < kSides * 32 && groups >= 4;
+    const int scale_side = wave * 2 + h < kSides ? wave * 2 + h : kSides - 1;
+    const uint8_t *const scale_from = (scale_side == 0 ? (const uint8_t *)ws : (const uint8_t *)xs) + row_of(scale_side, r) * blocks;
+    // the four groups of scales that a pair's belong to; the last four of a row may begin inside the four before
+    auto window = [&](int pair) { return groups < 4 ? 0 : pair / 2 * 4 + 4 <= groups ? pair / 2 * 4 : groups - 4; };
+    auto issue = [&](int pair, int slot_at, bool even) {            // past the end the last pair again, not used
+        const int p = pair < pairs ? pair : pairs - 1;
+        if (even && has_scales)
+            direct_load(base + kScalesAt + (uint32_t)(pair / 2 % kWindows) * kScales + wave * 1024, scale_from + window(p) * 4);
+        const uint32_t second = 2 * p + 1 == groups && block >= 4 ? 64 : 0;     // the last group is alone: it stands in
+#pragma unroll
+        for (int i = 0; i < kSides; ++i)
+            direct_load(base + slot_at + i * 4096 + wave * 1024, code_from[i] + (int64_t)p * 128, code_at[i] - second);
+    };
+    if (groups < 4) {                                               // too few for a load of four
+        for (int i = threadIdx.x; i < kSides * 32; i += 64 * W) {
+            const uint8_t *const from = (i < 32 ? (const uint8_t *)ws : (const uint8_t *)xs) + row_of(i / 32, i % 32) * blocks;
+            for (int g = 0; g < groups; ++g)
+                *reinterpret_cast<uint32_t *>(lds + kScalesAt + i * 16 + g * 4) = *reinterpret_cast<const uint32_t *>(from + g * 4);
+        }
+    }
+    if (groups > 0) {
+#pragma unroll
+        for (int i = 0; i < kDepth - 1; ++i) issue(i, i * kPair, i % 2 == 0);
+    }
+    if constexpr (kQuantize) {
+#pragma unroll
+        for (int i = 0; i < kFirst; ++i) {
+            const int unit = threadIdx.x + i * 64 * W;
+            if (unit < units) pack(unit, unit_of_x[i]);
+        }
+        for (int unit = threadIdx.x + kFirst * 64 * W; unit < units; unit += 64 * W) pack(unit, load_unit(unit));
+    }
+    v16f sum[MT];
+#pragma unroll
+    for (int t = 0; t < MT; ++t) sum[t] = v16f{0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
+    const int mine = 2 * wave + h, place = r * 128 + (mine ^ (r >> 1 & 7)) * 16;    // this lane's block of a pair, where it lies
+    const int x_row = r < M ? r : M - 1;
+    struct Fragment {
+        u32x4 w, x[MT];
+        uint32_t w_scale, x_scale[MT];
+    } f[2];
+    auto read = [&](Fragment &to, int pair, int slot_at) {
+        const uint8_t *const codes = lds + slot_at + place;
+        const int group = (2 * pair + wave / 2 - window(pair)) & 3;
+        const uint8_t *const scales = lds + kScalesAt + (uint32_t)(pair / 2 % kWindows) * kScales + r * 16 + group * 4 + (mine & 3);
+        to.w = *reinterpret_cast<const u32x4 *>(codes);
+        to.w_scale = *scales;
+#pragma unroll
+        for (int t = 0; t < MT; ++t) {
+            if constexpr (kQuantize) {
+                const int at = pair < pairs ? pair * 8 + mine : mine;
+                to.x[t] = *reinterpret_cast<const u32x4 *>(lds + kXAt + x_row * x_pitch + at * 16);
+                to.x_scale[t] = lds[kXAt + M * x_pitch + x_row * (int)blocks + at];
+            } else {
+                to.x[t] = *reinterpret_cast<const u32x4 *>(codes + (t + 1) * 4096);
+                to.x_scale[t] = scales[(t + 1) * 512];
+            }
+        }
+    };
+    auto multiply_all = [&](Fragment &f) {
+#pragma unroll
+        for (int t = 0; t < MT; ++t) sum[t] = multiply<0>(f.w, f.w_scale, f.x[t], f.x_scale[t], sum[t]);
+    };
+    // Turn by turn: the next pair is in LDS for all waves, and this one in registers; the one before has been read by all, its
+    // buffer is free.
+    auto after = [](int slot_at) { return slot_at + kPair == kDepth * kPair ? 0 : slot_at + kPair; };
+    int slot_at = 0, next_at = (kDepth - 1) * kPair;
+    auto turn = [&](int pair, int now) {
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((kDepth - 3) * kSides) : "memory");
+        slot_at = after(slot_at);
+        issue(pair + kDepth - 1, next_at, (kDepth - 1 + now) % 2 == 0);
+        next_at = after(next_at);
+        read(f[1 - now], pair + 1, slot_at);
+        multiply_all(f[now]);
+    };
+    if (groups > 0) {
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((kDepth - 2) * kSides) : "memory");
+        read(f[0], 0, 0);
+        // the last pair is left over: a group that is alone has blocks for two of the waves
+        int pair = 0;
+        for (; pair + 2 < pairs; pair += 2) {
+            turn(pair, 0);
+            turn(pair + 1, 1);
+        }
+        if (pair + 1 < pairs) {
+            turn(pair, 0);
+            f[0] = f[1];
+        }
+        if (2 * pairs == groups || wave < 2) multiply_all(f[0]);
+    }
+    // what was loaded past the end has landed, and all have read: LDS takes the waves' sums
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    v4f *const part = reinterpret_cast<v4f *>(lds);
+#pragma unroll
+    for (int t = 0; t < MT; ++t)
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+            part[((wave * MT + t) * 4 + q) * 64 + lane] = v4f{sum[t][4 * q], sum[t][4 * q + 1], sum[t][4 * q + 2], sum[t][4 * q + 3]};
+    __syncthreads();
+    for (int i = wave; i < MT * 4; i += W) {
+        v4f total = part[i * 64 + lane];
+#pragma unroll
+        for (int p = 1; p < W; ++p) total += part[(p * MT * 4 + i) * 64 + lane];
+        const int64_t m = m0 + 32 * (i / 4) + r;
+        if (m < M) store_out4(out + m * out_stride, n0 + 8 * (i % 4) + 4 * h, N, total);
+    }
+}
+
+// ---- large products
+// A workgroup of WN x WM waves has WN * FN * 32 rows of w by WM * FM * 32 rows of x, a wave FN x FM results of 32 x 32 in
+// registers.  A step is the 128 elements of a group, two 32x32x64 instructions a result, whose lane l has row l % 32 and block l / 32
+// of two.  Codes come to LDS with direct loads of two steps, a pair, into one of kBuffers buffers: a pair is asked for when
+// the one kBuffers before it has been read.
+//
+// In LDS a row of a pair is 128 bytes, a line of memory, and rows follow each other as the lanes of a direct load do, eight
+// lanes a row (rows spread over distant lanes, or half lines, are more requests: 8192 cubed 383 and 291 us).  The eight blocks of
+// row r stand in the order of their number xor r / 2 % 8, so that one block of sixteen rows is in all banks once.  Scales: the
+// four bytes of a row and step are a word; a lane shifts it by its block and the instruction picks byte 0 or 2.  Rows' scales lie
+// far apart, a line each, so that they are loaded for four steps at once (a word a step: half of all requests).
 
 // What one of W waves loads of a side: of every pair eights of rows wave, wave + W, ...; of every second one four groups' scales of
 // 64 rows, if the wave is one of the first kEights / 8.
@@ -296,13 +437,11 @@ struct Rows32 {
     }
 };
 
-template <int kHalf>
-__device__ __forceinline__ v16f multiply32(const Rows32 &w, uint32_t w_scale, const Rows32 &x, uint32_t x_scale, const v16f &sum)
+// f(0), f(1), ... with the numbers known when the program is built.
+template <int... kNumbers, typename F>
+__device__ __forceinline__ void each_phase(std::integer_sequence<int, kNumbers...>, F f)
 {
-    const u32x4 p = w.codes[kHalf], q = x.codes[kHalf];
-    const v8i a = {(int)p[0], (int)p[1], (int)p[2], (int)p[3], 0, 0, 0, 0};
-    const v8i b = {(int)q[0], (int)q[1], (int)q[2], (int)q[3], 0, 0, 0, 0};
-    return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, sum, 4, 4, 2 * kHalf, (int)w_scale, 2 * kHalf, (int)x_scale);
+    (f(std::integral_constant<int, kNumbers>{}), ...);
 }
 
 // A tile of results in LDS to memory, as far as `rows` and `cols` go.
@@ -317,7 +456,7 @@ __device__ __forceinline__ void store_tile(const uint8_t *tile, uint16_t *out, i
     }
 }
 
-template <int WN, int WM, int FN, int FM>
+template <int WN, int WM, int FN, int FM, int kBuffers>
 __global__ __launch_bounds__(64 * WN * WM) void product_tiles_kernel(Global<const uint8_t> xc, Global<const uint8_t> xs,
                                                                      Global<const uint8_t> wc, Global<const uint8_t> ws,
                                                                      Global<uint16_t> out, int32_t M, int32_t N, int32_t groups,
@@ -326,7 +465,9 @@ __global__ __launch_bounds__(64 * WN * WM) void product_tiles_kernel(Global<cons
     constexpr int W = WN * WM, kEightN = WN * FN * 4, kEightM = WM * FM * 4;
     constexpr int kSideN = kEightN * 1024, kPair = kSideN + kEightM * 1024;
     constexpr int kScalesN = kEightN * 128, kScales = kScalesN + kEightM * 128;
-    __shared__ __align__(1024) uint8_t lds[2 * (kPair + kScales)];
+    constexpr int kWindows = kBuffers / 2 + 1;                      // fours of groups that the pairs in LDS are of
+    static_assert(kBuffers % 2 == 0, "a pair's place among the four groups whose scales it shares is known from its buffer");
+    __shared__ __align__(1024) uint8_t lds[kBuffers * kPair + kWindows * kScales];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int h = lane >> 5;
     const uint32_t tile_n = blockIdx.x % tiles_n, tile_m = blockIdx.x / tiles_n;
@@ -346,13 +487,13 @@ __global__ __launch_bounds__(64 * WN * WM) void product_tiles_kernel(Global<cons
     const uint32_t base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)lds;
     // Scales come four groups at a time; the last four of a row may begin inside the four before.
     auto window = [&](int step) { return (step & ~3) + 4 <= groups ? step & ~3 : groups - 4; };
-    // A part of the loads of the pair that begins at `step`; phase: step % 4, known when the program is built.
+    // A part of the loads of the pair that begins at `step`; phase: step % (2 * kBuffers), known when the program is built.
     constexpr int kParts = 4 * FM;
     auto issue = [&](int step, auto phase, int part) {
         constexpr int kPhase = decltype(phase)::value;
         const uint32_t to = base + kPhase / 2 * kPair;
-        if (kPhase == 0 && part == 0) {         // past the end, the last four again
-            const uint32_t scales = base + 2 * kPair + (uint32_t)(step / 4 % 2) * kScales;
+        if (kPhase % 4 == 0 && part == 0) {     // past the end, the last four again
+            const uint32_t scales = base + kBuffers * kPair + (uint32_t)(step / 4 % kWindows) * kScales;
             const int from = window(step);
             if (kScaleN == W || wave < kScaleN) wl.issue_scales(scales + wave * 1024, from);
             if (kBoth && kScaleM == W) {
@@ -382,7 +523,7 @@ __global__ __launch_bounds__(64 * WN * WM) void product_tiles_kernel(Global<cons
     Rows32 w[2], x[2][FM];
     static_assert(FN % 2 == 0 && FM <= FN, "a step asks for the next one's rows of x line by line");
     const int part_n = wave % WN, part_m = wave / WN;
-    auto scales = [&](int step) { return lds + 2 * kPair + (uint32_t)(step / 4 % 2) * kScales; };
+    auto scales = [&](int step) { return lds + kBuffers * kPair + (uint32_t)(step / 4 % kWindows) * kScales; };
     auto read_w = [&](Rows32 &to, int step, int phase, int i) {
         to.read(lds + phase / 2 * kPair, scales(step), part_n * FN + i, phase % 2, (step - window(step)) & 3, lane);
     };
@@ -390,17 +531,21 @@ __global__ __launch_bounds__(64 * WN * WM) void product_tiles_kernel(Global<cons
         to.read(lds + phase / 2 * kPair + kSideN, scales(step) + kScalesN, part_m * FM + j, phase % 2, (step - window(step)) & 3, lane);
     };
     using std::integral_constant;
+    constexpr int kPhases = 2 * kBuffers, kPairLoads = LoadsN::kPer + LoadsM::kPer;     // of a wave, and its scales
+    each_phase(std::make_integer_sequence<int, kBuffers - 1>{}, [&](auto pair) {
+        constexpr int kPairOf = decltype(pair)::value;
 #pragma unroll
-    for (int part = 0; part < kParts; ++part) issue(0, integral_constant<int, 0>{}, part);
+        for (int part = 0; part < kParts; ++part) issue(2 * kPairOf, integral_constant<int, 2 * kPairOf>{}, part);
+    });
 #pragma unroll
-    for (int part = 0; part < FM; ++part) issue(2, integral_constant<int, 2>{}, part);
-    asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"((LoadsN::kPer + LoadsM::kPer) / 4) : "memory");
+    for (int part = 0; part < FM; ++part) issue(kPhases - 2, integral_constant<int, kPhases - 2>{}, part);
+    asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"((kBuffers - 2) * kPairLoads + kPairLoads / 4) : "memory");
 #pragma unroll
     for (int j = 0; j < FM; ++j) read_x(x[0][j], 0, 0, j);
     read_w(w[0], 0, 0, 0);
     // What else a line has to do goes between its instructions, a little at a time: a wave issues in order.
     auto step = [&](int at, auto phase) {
-        constexpr int kPhase = decltype(phase)::value, kNow = kPhase % 2, kNext = (kPhase + 1) % 4;
+        constexpr int kPhase = decltype(phase)::value, kNow = kPhase % 2, kNext = (kPhase + 1) % kPhases;
         constexpr bool kSecond = kPhase % 2 == 1;
         uint32_t sx[FM];
 #pragma unroll
@@ -410,11 +555,11 @@ __global__ __launch_bounds__(64 * WN * WM) void product_tiles_kernel(Global<cons
             const uint32_t sw = w[i % 2].scales >> (8 * h);
             if (kSecond && i + 1 == FN) {
                 // the next pair is in LDS for all waves, and this one has been read by all: its buffer is free
-                asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+                asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((kBuffers - 2) * kPairLoads) : "memory");
             }
 #pragma unroll
             for (int j = 0; j < FM; ++j) {
-                sum[i][j] = multiply32<0>(w[i % 2], sw, x[kNow][j], sx[j], sum[i][j]);
+                sum[i][j] = multiply<0>(w[i % 2].codes[0], sw, x[kNow][j].codes[0], sx[j], sum[i][j]);
                 if (j == 0) {
                     if (i + 1 < FN) {
                         read_w(w[(i + 1) % 2], at, kPhase, i + 1);
@@ -431,35 +576,31 @@ __global__ __launch_bounds__(64 * WN * WM) void product_tiles_kernel(Global<cons
             }
 #pragma unroll
             for (int j = 0; j < FM; ++j) {
-                sum[i][j] = multiply32<1>(w[i % 2], sw, x[kNow][j], sx[j], sum[i][j]);
+                sum[i][j] = multiply<2>(w[i % 2].codes[1], sw, x[kNow][j].codes[1], sx[j], sum[i][j]);
                 // (four loads in a row instead of one an instruction: 277 us for 8192 cubed, sixteen: 298)
-                if (kSecond && i + 1 == FN) issue(at + 3, integral_constant<int, (kPhase + 3) % 4>{}, j);
-                if (!kSecond && i < 3) issue(at + 2, integral_constant<int, (kPhase + 2) % 4>{}, (i + 1) * FM + j);
+                if (kSecond && i + 1 == FN) issue(at + kPhases - 1, integral_constant<int, kPhase - 1 + !kSecond>{}, j);
+                if (!kSecond && i < 3) issue(at + kPhases - 2, integral_constant<int, (kPhase + kPhases - 2) % kPhases>{}, (i + 1) * FM + j);
                 __builtin_amdgcn_sched_barrier(0);
             }
             if (!kSecond && i + 1 == FN) {
 #pragma unroll
-                for (int part = (FN + 1) * FM; part < kParts; ++part) issue(at + 2, integral_constant<int, (kPhase + 2) % 4>{}, part);
+                for (int part = (FN + 1) * FM; part < kParts; ++part) issue(at + kPhases - 2, integral_constant<int, (kPhase + kPhases - 2) % kPhases>{}, part);
             }
         }
     };
-    // No branch inside four steps: a compiler that may moves the instructions of one past the next one's wait.
+    // No branch inside a round: a compiler that may moves the instructions of one step past the next one's wait.
     int at = 0;
-    for (; at + 4 <= groups; at += 4) {
-        step(at, integral_constant<int, 0>{});
-        step(at + 1, integral_constant<int, 1>{});
-        step(at + 2, integral_constant<int, 2>{});
-        step(at + 3, integral_constant<int, 3>{});
-    }
-    if (at < groups) step(at, integral_constant<int, 0>{});
-    if (at + 1 < groups) step(at + 1, integral_constant<int, 1>{});
-    if (at + 2 < groups) step(at + 2, integral_constant<int, 2>{});
+    for (; at + kPhases <= groups; at += kPhases)
+        each_phase(std::make_integer_sequence<int, kPhases>{}, [&](auto phase) { step(at + decltype(phase)::value, phase); });
+    each_phase(std::make_integer_sequence<int, kPhases - 1>{}, [&](auto phase) {
+        if (at + decltype(phase)::value < groups) step(at + decltype(phase)::value, phase);
+    });
     // What was loaded past the end lands, all waves have read: LDS takes the results, bf16, a row of x after the other, from where
     // they leave in rows as long as the tile.  (Stored from registers, 32 bytes a row at a time, they took 2.5 us longer a tile,
     // and twice that where a row begins at an odd element.)
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
     constexpr int kRowElems = WN * FN * 32, kRowBytes = kRowElems * 2 + 16, kRows = WM * FM * 32;
-    static_assert(kRows * kRowBytes <= (int)sizeof(lds), "the results take the codes' place");
+    static_assert(kRows * kRowBytes <= kBuffers * kPair + kWindows * kScales, "the results take the codes' place");
 #pragma unroll
     for (int j = 0; j < FM; ++j) {
         uint8_t *const row = lds + ((part_m * FM + j) * 32 + (lane & 31)) * kRowBytes;

@@ -117,6 +117,29 @@ def test_product_and_linear(M, N, K):
     assert torch.equal(again, out[:, :N])
 
 
+# One shape for each kernel and tile there is (32 x 32, 64 and 128 rows; 128 x 64; 128 x 128 alone on a CU and in pairs; 256 x 256), none
+# a whole number of tiles, with every remainder that k's groups can leave.
+TILES = [(9, 77), (50, 77), (100, 1000), (300, 1100), (600, 4100), (1100, 4130), (2111, 4101)]
+
+
+@pytest.mark.parametrize("M,N", TILES)
+@pytest.mark.parametrize("groups", (1, 2, 3, 4, 5, 6, 7, 8, 9, 10, 11, 12, 15, 21))
+def test_every_tile_with_every_remainder_of_k(M, N, groups):
+    K = groups * 128 - 37
+    g = torch.Generator(device="cuda").manual_seed(groups)
+    x, w = (torch.randn(n, K, generator=g, device="cuda").to(torch.bfloat16) for n in (M, N))
+    xq, wq = _quantize(x), _quantize(w)
+    values = []
+    for codes, scales in (xq, wq):
+        v = torch.empty(codes.shape[0], K, dtype=torch.bfloat16, device="cuda")
+        eq.equarx_mx4_dequantize(codes, scales, v)
+        values.append(v.double())
+    want = values[0] @ values[1].T.contiguous()
+    out = torch.full((M, N), 9.0, dtype=torch.bfloat16, device="cuda")
+    eq.equarx_mx4_product(*xq, *wq, K, out, eq.alloc_mx4_workspace(M, N, K))
+    assert ((out.double() - want).abs() <= _bound(*values, want)).all()
+
+
 def test_linear_takes_rows_of_any_stride():
     for gap in (1, 8):
         wide = _rows(9, 21, 700 + gap).cuda()
