@@ -107,10 +107,10 @@ AttentionPlan plan_attention(int32_t heads, int32_t q_heads, int32_t sequences, 
     p.row_tiles = (rows + per - 1) / per;
     const int64_t workgroups = p.row_tiles * heads * sequences;
     // enough workgroups for four a CU, none with fewer than four tiles of tokens
-    int64_t splits = (1024 + workgroups - 1) / workgroups;
+    int64_t splits = (512 + workgroups - 1) / workgroups;
     const int64_t most = (max_length + 255) / 256;
     if (splits > most) splits = most;
-    if (splits > 128) splits = 128;
+    if (splits > kMostSplits) splits = kMostSplits;
     if (splits * heads > kGridDim) splits = kGridDim / heads;
     if (splits < 1) splits = 1;
     p.chunk = (int32_t)(((max_length + splits - 1) / splits + 63) / 64 * 64);
@@ -129,7 +129,7 @@ int check_heads(int32_t heads, int64_t q_rows, int32_t q_heads, int32_t dim, int
     if (heads < 1 || heads > kGridDim || q_heads < 1 || q_heads % heads != 0) return EQUARX_BAD_SHAPE;
     if (q_rows < 0 || sequences < 0 || max_queries < 1 || max_length < 1 || max_length > INT32_MAX - 63) return EQUARX_BAD_SHAPE;
     if (dim != 64 && dim != 128 && dim != 256) return EQUARX_BAD_SHAPE;
-    if (q_rows > INT32_MAX || q_rows > kMostElements / ((int64_t)q_heads * dim)) return EQUARX_BAD_SHAPE;
+    if (q_rows > INT32_MAX / q_heads) return EQUARX_BAD_SHAPE;
     return EQUARX_OK;
 }
 
@@ -272,8 +272,7 @@ int equarx_cache_attention(const equarx_cache *cache, const void *q_bf16, int64_
                          Sequences{page_table + at * table_width, lengths + at, table_width}, pool);
         }
         if (plan.splits > 1) {
-            const int64_t all = q_rows * q_heads, per = 256 / (D / 4);
-            ctx.launch(join_kernel<D>, (unsigned)((all + per - 1) / per), 256, call, sequences);
+            ctx.launch(join_kernel<D>, (unsigned)(q_rows * q_heads), 256, call, sequences);
         }
     });
     return ctx.status();
