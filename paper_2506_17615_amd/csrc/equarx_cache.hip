@@ -90,27 +90,35 @@ int check_sequences(const int32_t *page_table, int64_t table_width, const int32_
 
 // ---------------------------------------------------------------- how an attention call is cut
 
+// A call goes to one of three kernels' forms.
+enum class AttentionForm { kRows, kShared, kWhole };
+
 struct AttentionPlan {
-    bool on_tokens;             // the waves of a workgroup share their rows
+    AttentionForm form;
     int rows16;                 // sixteens of rows of a wave
     int64_t row_tiles;          // of the longest query run
-    int32_t splits, chunk;
+    int32_t splits, chunk;      // kRows
 };
 
 AttentionPlan plan_attention(int32_t heads, int32_t q_heads, int32_t sequences, int64_t max_queries, int64_t max_length)
 {
-    AttentionPlan p;
+    AttentionPlan p{};
     const int64_t rows = max_queries * (q_heads / heads);
-    p.on_tokens = rows <= 32;
     p.rows16 = rows <= 16 ? 1 : 2;
-    const int64_t per = (p.on_tokens ? 1 : 4) * p.rows16 * 16;
-    p.row_tiles = (rows + per - 1) / per;
+    p.splits = 1;
+    if (rows <= 32) {
+        p.row_tiles = 1;
+        p.form = sequences > kMostShared || max_length <= 512 ? AttentionForm::kWhole : AttentionForm::kShared;
+        return p;
+    }
+    p.form = AttentionForm::kRows;
+    p.row_tiles = (rows + 127) / 128;
     const int64_t workgroups = p.row_tiles * heads * sequences;
-    // enough workgroups for four a CU, none with fewer than four tiles of tokens
+    // enough workgroups for two a CU, none with fewer than four tiles of tokens
     int64_t splits = (512 + workgroups - 1) / workgroups;
     const int64_t most = (max_length + 255) / 256;
     if (splits > most) splits = most;
-    if (splits > kMostSplits) splits = kMostSplits;
+    if (splits > 64) splits = 64;
     if (splits * heads > kGridDim) splits = kGridDim / heads;
     if (splits < 1) splits = 1;
     p.chunk = (int32_t)(((max_length + splits - 1) / splits + 63) / 64 * 64);
@@ -120,7 +128,53 @@ AttentionPlan plan_attention(int32_t heads, int32_t q_heads, int32_t sequences, 
 
 size_t attention_workspace(const AttentionPlan &p, int32_t dim, int64_t q_rows, int32_t q_heads)
 {
-    return p.splits == 1 ? 0 : (size_t)p.splits * (size_t)q_rows * (size_t)q_heads * ((size_t)dim + 2) * sizeof(float);
+    const size_t row = ((size_t)dim + 2) * sizeof(float);
+    if (p.form == AttentionForm::kShared) return (size_t)kShares * 2 * p.rows16 * 16 * row + (kMostShared + 1) * sizeof(int64_t);
+    return p.splits == 1 ? 0 : (size_t)p.splits * (size_t)q_rows * (size_t)q_heads * row;
+}
+
+// The kernels of one geometry.
+template <int D, int NB>
+void launch_attention(const AttentionPlan &plan, const AttentionCall &call, const Sequences &seqs, const Pool &pool, LaunchCtx &ctx)
+{
+    const int64_t tiles = plan.row_tiles < 65536 ? plan.row_tiles : 65536;
+    const int64_t all = call.q_rows * call.q_heads;
+    auto share = [&](auto rows16) {
+        constexpr int R = decltype(rows16)::value;
+        ctx.launch(attention_shares_kernel<D, NB, R>, (unsigned)kShares / 4, 256, call, seqs, pool);
+        // many items have few parts each: a wave joins them; few have many: four
+        if ((int64_t)call.sequences * pool.heads * 8 >= kShares) {
+            ctx.launch(join_shares_kernel<D, R, 1>, (unsigned)((all + 3) / 4), 256, call, seqs, pool);
+        } else {
+            ctx.launch(join_shares_kernel<D, R, 4>, (unsigned)all, 256, call, seqs, pool);
+        }
+    };
+    if (plan.form == AttentionForm::kShared) {
+        if (plan.rows16 == 1) {
+            share(std::integral_constant<int, 1>{});
+        } else {
+            share(std::integral_constant<int, 2>{});
+        }
+        return;
+    }
+    for (int32_t at = 0; at < call.sequences; at += kGridDim) {
+        const int32_t count = call.sequences - at < kGridDim ? call.sequences - at : kGridDim;
+        AttentionCall part = call;
+        part.q_starts += at;
+        const Sequences some{seqs.table + at * seqs.width, seqs.lengths + at, seqs.width};
+        if (plan.form == AttentionForm::kRows) {
+            ctx.launch3d(attention_rows_kernel<D, NB, 2>, (unsigned)tiles, (unsigned)(pool.heads * plan.splits), (unsigned)count, 256,
+                         part, some, pool);
+        } else {
+            ctx.launch3d(plan.rows16 == 1 ? attention_tokens_kernel<D, NB, 1> : attention_tokens_kernel<D, NB, 2>,
+                         (unsigned)tiles, (unsigned)pool.heads, (unsigned)count, 256, part, some, pool);
+        }
+    }
+    if (plan.splits > 8) {
+        ctx.launch(join_splits_kernel<D, 4>, (unsigned)all, 256, call);
+    } else if (plan.splits > 1) {
+        ctx.launch(join_splits_kernel<D, 1>, (unsigned)((all + 3) / 4), 256, call);
+    }
 }
 
 int check_heads(int32_t heads, int64_t q_rows, int32_t q_heads, int32_t dim, int32_t sequences, int32_t max_queries,
@@ -257,23 +311,10 @@ int equarx_cache_attention(const equarx_cache *cache, const void *q_bf16, int64_
     call.window = window;
     call.chunk = plan.chunk;
     call.splits = plan.splits;
-    const Pool pool = pool_of(*cache);
-    const int64_t tiles = plan.row_tiles < 65536 ? plan.row_tiles : 65536;
+    call.sequences = sequences;
     with_geometry(cache->dim, cache->block, [&](auto dim, auto block) {
         constexpr int D = decltype(dim)::value, NB = D / decltype(block)::value;
-        const auto kernel = !plan.on_tokens     ? attention_kernel<D, NB, 2, false>
-                            : plan.rows16 == 1 ? attention_kernel<D, NB, 1, true>
-                                               : attention_kernel<D, NB, 2, true>;
-        for (int32_t at = 0; at < sequences; at += kGridDim) {
-            const int32_t count = sequences - at < kGridDim ? sequences - at : kGridDim;
-            AttentionCall part = call;
-            part.q_starts += at;
-            ctx.launch3d(kernel, (unsigned)tiles, (unsigned)(cache->heads * plan.splits), (unsigned)count, 256, part,
-                         Sequences{page_table + at * table_width, lengths + at, table_width}, pool);
-        }
-        if (plan.splits > 1) {
-            ctx.launch(join_kernel<D>, (unsigned)(q_rows * q_heads), 256, call, sequences);
-        }
+        launch_attention<D, NB>(plan, call, {page_table, lengths, table_width}, pool_of(*cache), ctx);
     });
     return ctx.status();
 }

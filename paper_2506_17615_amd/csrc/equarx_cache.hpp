@@ -216,13 +216,13 @@ struct AttentionCall {
     const int32_t *q_starts;
     uint16_t *out;
     float *lse;
-    float *part;                // [splits][q_rows][q_heads][D], then the statistics, 2 each
+    float *part;                // parts of rows to be joined, sums and then statistics
     int64_t q_rows;
     int32_t q_heads, group;
     float scale;                // times log2(e)
     int32_t causal, window;
-    int32_t chunk;              // tokens of a split, a multiple of 64
-    int32_t splits;
+    int32_t chunk, splits;      // waves on rows: a split's tokens, a multiple of 64
+    int32_t sequences;
 };
 
 __device__ __forceinline__ int within(int v, int64_t most) { return v < 0 ? 0 : v < most ? v : (int)most; }
@@ -437,25 +437,161 @@ struct Rows {
     }
 };
 
-// Where a lane's keys and values of a tile are: its page and head's first slot, and its group of sixteen there.
+// Rows `first` .. first + R * 16 - 1 of a sequence and key head: row n * 16 + lane % 16 as a query and its head, past the end the last.
+struct Row {
+    int query, head;
+    __device__ __forceinline__ Row(const AttentionCall &call, int queries, int h, int row)
+    {
+        const int rows = queries * call.group;
+        if (row >= rows) row = rows - 1;
+        query = (int)((uint32_t)row / (uint32_t)call.group);
+        head = h * call.group + (row - query * call.group);
+    }
+};
+
+template <int D, int NB, int R>
+__device__ __forceinline__ void load_q(Rows<D, NB, R> &mine, const AttentionCall &call, int q0, int queries, int h, int first, int lane)
+{
+#pragma unroll
+    for (int n = 0; n < R; ++n) {
+        const Row row(call, queries, h, first + n * 16 + (lane & 15));
+        const uint16_t *const from = call.q + (q0 + row.query) * call.q_row + row.head * call.q_head + (lane >> 4) * 16;
+#pragma unroll
+        for (int j = 0; j < D / 32; ++j) mine.q[n][j] = *reinterpret_cast<const bf16x8 *>(from + (j / 2) * 64 + (j % 2) * 8);
+    }
+}
+
+// What the rows see, nothing summed yet; and where their results go.
+template <int D, int NB, int R>
+__device__ __forceinline__ void start_rows(Rows<D, NB, R> &mine, const AttentionCall &call, int queries, int length, int h, int first,
+                                           int lane)
+{
+    mine.start();
+#pragma unroll
+    for (int n = 0; n < R; ++n) {
+        const int at = length - queries + Row(call, queries, h, first + n * 16 + (lane & 15)).query;
+        mine.high[n] = call.causal ? (at < -1 ? -1 : at) : length - 1;
+        mine.low[n] = call.window && at >= call.window ? at - call.window : -1;
+    }
+}
+
+__device__ __forceinline__ int64_t place_of_row(const AttentionCall &call, int q0, const Row &row)
+{
+    return (int64_t)(q0 + row.query) * call.q_heads + row.head;
+}
+
+// The tokens that any of some consecutive rows sees, first .. last - 1 with first a multiple of 64, and those that all see.
+struct Span {
+    int first, last, all_from, all_to;
+};
+
+__device__ __forceinline__ Span span_of(const AttentionCall &call, int queries, int length, int row_first, int row_last)
+{
+    const int rows = queries * call.group;
+    Span s{0, length, 0, length};
+    if (call.causal) {
+        if (row_last >= rows) row_last = rows - 1;
+        if (row_first >= rows) row_first = rows - 1;
+        const int at_first = length - queries + (int)((uint32_t)row_first / (uint32_t)call.group);
+        const int at_last = length - queries + (int)((uint32_t)row_last / (uint32_t)call.group);
+        s.last = at_last + 1 < 0 ? 0 : at_last + 1;
+        s.all_to = at_first + 1;
+        if (call.window) {
+            if (at_first >= call.window) s.first = (at_first - call.window + 1) & ~63;
+            if (at_last >= call.window) s.all_from = at_last - call.window + 1;
+        }
+    }
+    return s;
+}
+
+// Where a lane's keys and values of the tile from token t on are: page numbers, -1 past the table; a page and head's first slot;
+// a group there.
+struct PageIds {
+    int k, v;
+    __device__ __forceinline__ PageIds(const Pool &pool, const int32_t *table, int64_t width, int t, int lane)
+    {
+        const int k_p = page_of(pool, t + 16 * ((lane & 15) >> 2)), v_p = page_of(pool, t + 16 * (lane >> 4));
+        k = k_p < width ? table[k_p] : -1;
+        v = v_p < width ? table[v_p] : -1;
+    }
+};
+
 struct Place {
     int64_t k_at, v_at;
     int k_in, v_in;
     bool there;
+    __device__ __forceinline__ Place(const Pool &pool, PageIds ids, int h, int t, int lane)
+    {
+        const int k_t = t + 16 * ((lane & 15) >> 2), v_t = t + 16 * (lane >> 4);
+        there = ids.v >= 0 && ids.v < pool.pages;
+        if (ids.k < 0 || ids.k >= pool.pages) ids.k = 0;        // loaded, not seen
+        if (!there) ids.v = 0;
+        k_at = pool.place(ids.k, h) * pool.page;
+        v_at = pool.place(ids.v, h) * pool.page;
+        k_in = k_t - page_of(pool, k_t) * pool.page;
+        v_in = v_t - page_of(pool, v_t) * pool.page;
+    }
 };
 
-// Waves of a workgroup: on the same rows and different tokens (kTokens), their results joined at the end, or on
-// different rows.
-template <int D, int NB, int R, bool kTokens>
-__global__ __launch_bounds__(256, R == 1 && D <= 128 ? 2 : 1) void attention_kernel(const AttentionCall call, const Sequences seqs,
-                                                                                    const Pool pool)
+// Takes the tiles t0, t0 + kStep, ... below `last` in.
+template <int kStep, int D, int NB, int R>
+__device__ __forceinline__ void walk(Rows<D, NB, R> &mine, const Pool &pool, const int32_t *table, int64_t width, int h, float scale,
+                                     int t0, int last, const Span &span, int lane)
 {
-    constexpr int W = 4;
-    constexpr float kNone = -__builtin_inff();
-    constexpr int kPitch = D + 4;           // of a row of results in LDS, whose statistics are behind it
-    __shared__ float joined[kTokens ? W / 2 : 1][kTokens ? R * 16 : 1][kPitch];
+    if (t0 >= last) return;
+    Tile<D, NB> tile;
+    const Place place(pool, PageIds(pool, table, width, t0, lane), h, t0, lane);
+    tile.load_k(pool, place.k_at, place.k_in, place.v_at, place.v_in, lane);
+    tile.load_v(pool, place.v_at, place.v_in, lane);
+    bool there = place.there;
+    PageIds ids(pool, table, width, t0 + kStep, lane);
+    do {
+        // past the end the next tile is one of another part, or of no page: loaded, not used
+        const Place next(pool, ids, h, t0 + kStep, lane);
+        float score[R][16];
+        mine.scores(tile, scale, score);
+        tile.load_k(pool, next.k_at, next.k_in, next.v_at, next.v_in, lane);
+        ids = PageIds(pool, table, width, t0 + 2 * kStep, lane);
+        __builtin_amdgcn_sched_barrier(0);
+        mine.add(tile, score, t0 + 16 * (lane >> 4), there, !(t0 >= span.all_from && t0 + 64 <= span.all_to && __all(there)));
+        tile.load_v(pool, next.v_at, next.v_in, lane);
+        there = next.there;
+        t0 += kStep;
+    } while (t0 < last);
+}
+
+// Row n's results, to the output or to a part: sums at `part`, statistics at `stats`.
+template <int D, int NB, int R>
+__device__ __forceinline__ void end_row(const Rows<D, NB, R> &mine, int n, const AttentionCall &call, int64_t place_out, int lane)
+{
+    const int g = lane >> 4;
+    const float inverse = ends_with(mine.total[n]);
+#pragma unroll
+    for (int t = 0; t < D / 16; ++t) {
+        const v4f o = mine.o[n][t] * inverse;
+        *reinterpret_cast<u32x2 *>(call.out + place_out * D + t * 16 + 4 * g) = u32x2{narrow_bf16x2(o[0], o[1]), narrow_bf16x2(o[2], o[3])};
+    }
+    if (call.lse && g == 0) call.lse[place_out] = log_sum(mine.base[n], mine.total[n]);
+}
+
+template <int D, int NB, int R>
+__device__ __forceinline__ void part_row(const Rows<D, NB, R> &mine, int n, float *part, float2 *stats, int lane)
+{
+    const int g = lane >> 4;
+#pragma unroll
+    for (int t = 0; t < D / 16; ++t) *reinterpret_cast<v4f *>(part + t * 16 + 4 * g) = mine.o[n][t];
+    if (g == 0) *stats = float2{mine.base[n], mine.total[n]};
+}
+
+// ---- many rows: the waves of a workgroup have different ones
+// Grid: tiles of rows, heads x splits, sequences.  Parts: [splits][q_rows][q_heads].
+
+template <int D, int NB, int R>
+__global__ __launch_bounds__(256) void attention_rows_kernel(const AttentionCall call, const Sequences seqs, const Pool pool)
+{
+    constexpr int kRows = 4 * R * 16;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int r = lane & 15, g = lane >> 4;
+    const int r = lane & 15;
     const int b = blockIdx.z, split = blockIdx.y / (uint32_t)pool.heads, h = blockIdx.y - split * pool.heads;
     const int q0 = within(call.q_starts[b], call.q_rows), queries = within(call.q_starts[b + 1], call.q_rows) - q0;
     const int length = seqs.length(b, pool.page);
@@ -463,197 +599,429 @@ __global__ __launch_bounds__(256, R == 1 && D <= 128 ? 2 : 1) void attention_ker
     int chunk = call.chunk;
     if ((int64_t)chunk * call.splits < length) chunk = (int)((uint32_t)(length + call.splits - 1) / (uint32_t)call.splits + 63 & ~63u);
     const int64_t split_from = (int64_t)split * chunk;
-    const int split_first = split_from < length ? (int)split_from : length;
-    const int split_last = split_from + chunk < length ? (int)split_from + chunk : length;
 
-    const int32_t *const table = seqs.table + b * seqs.width;
-    // page numbers of a tile from t0 on, of this lane's keys and values; -1 past the table
-    auto pages_of = [&](int t0, int &k_id, int &v_id) {
-        const int k_p = page_of(pool, t0 + 16 * (r >> 2)), v_p = page_of(pool, t0 + 16 * g);
-        k_id = k_p < seqs.width ? table[k_p] : -1;
-        v_id = v_p < seqs.width ? table[v_p] : -1;
-    };
-    auto place_of = [&](int t0, int k_id, int v_id) {
-        Place p;
-        const int k_t = t0 + 16 * (r >> 2), v_t = t0 + 16 * g;
-        p.there = v_id >= 0 && v_id < pool.pages;
-        if (k_id < 0 || k_id >= pool.pages) k_id = 0;       // loaded, not seen
-        if (!p.there) v_id = 0;
-        p.k_at = pool.place(k_id, h) * pool.page;
-        p.v_at = pool.place(v_id, h) * pool.page;
-        p.k_in = k_t - page_of(pool, k_t) * pool.page;
-        p.v_in = v_t - page_of(pool, v_t) * pool.page;
-        return p;
-    };
-
-    const int rows = queries * call.group;
-    constexpr int kRows = (kTokens ? 1 : W) * R * 16;
-    const int row_tiles = (rows + kRows - 1) / kRows;
+    const int rows = queries * call.group, row_tiles = (rows + kRows - 1) / kRows;
     for (int turn = blockIdx.x; turn < row_tiles; turn += gridDim.x) {
-        // with causal rows the last ones are the longest: they begin first
-        const int tile_row = (kTokens ? turn : row_tiles - 1 - turn) * kRows;
-        const int row0 = tile_row + (kTokens ? 0 : wave * R * 16);
-        auto query_of = [&](int row) { return (int)((uint32_t)(row < rows ? row : rows - 1) / (uint32_t)call.group); };
+        const int row0 = (row_tiles - 1 - turn) * kRows + wave * R * 16;        // with causal rows the last ones are the longest: first
         Rows<D, NB, R> mine;
-        mine.start();
-        int64_t place_out[R];
+        load_q(mine, call, q0, queries, h, row0, lane);
+        start_rows(mine, call, queries, length, h, row0, lane);
+        Span span = span_of(call, queries, length, row0, row0 + R * 16 - 1);
+        if (split_from > span.first) span.first = split_from < length ? (int)split_from : length;
+        if (split_from + chunk < span.last) span.last = (int)split_from + chunk;
+        walk<64>(mine, pool, seqs.table + b * seqs.width, seqs.width, h, call.scale, span.first, span.last, span, lane);
 #pragma unroll
         for (int n = 0; n < R; ++n) {
-            const int row = row0 + n * 16 + r < rows ? row0 + n * 16 + r : rows - 1;
-            const int i = query_of(row), member = h * call.group + (row - i * call.group);
-            const int at = length - queries + i;
-            mine.high[n] = call.causal ? (at < -1 ? -1 : at) : length - 1;
-            mine.low[n] = call.window && at >= call.window ? at - call.window : -1;
-            place_out[n] = (int64_t)(q0 + i) * call.q_heads + member;
-            const uint16_t *const from = call.q + (q0 + i) * call.q_row + member * call.q_head + g * 16;
-#pragma unroll
-            for (int j = 0; j < D / 32; ++j)
-                mine.q[n][j] = *reinterpret_cast<const bf16x8 *>(from + (j / 2) * 64 + (j % 2) * 8);
-        }
-        // what any row of the wave sees of this split, and what all of them see
-        int first = split_first, last = split_last;
-        int all_from = 0, all_to = length;
-        if (call.causal) {
-            const int at_first = length - queries + query_of(row0), at_last = length - queries + query_of(row0 + R * 16 - 1);
-            if (at_last + 1 < last) last = at_last + 1;
-            all_to = at_first + 1;
-            if (call.window && at_last >= call.window) {
-                if (at_first >= call.window && at_first - call.window + 1 > first) first = (at_first - call.window + 1) & ~63;
-                all_from = at_last - call.window + 1;
-            }
-        }
-        constexpr int kStep = (kTokens ? W : 1) * 64;
-        int t0 = first + (kTokens ? wave * 64 : 0);
-        if (t0 < last) {
-            Tile<D, NB> tile;
-            int k_id, v_id;
-            pages_of(t0, k_id, v_id);
-            Place place = place_of(t0, k_id, v_id);
-            tile.load_k(pool, place.k_at, place.k_in, place.v_at, place.v_in, lane);
-            tile.load_v(pool, place.v_at, place.v_in, lane);
-            bool there = place.there;
-            pages_of(t0 + kStep, k_id, v_id);
-            do {
-                // past the end the next tile is one of another split, or of no page: loaded, not used
-                const Place next = place_of(t0 + kStep, k_id, v_id);
-                float score[R][16];
-                mine.scores(tile, call.scale, score);
-                tile.load_k(pool, next.k_at, next.k_in, next.v_at, next.v_in, lane);
-                pages_of(t0 + 2 * kStep, k_id, v_id);
-                __builtin_amdgcn_sched_barrier(0);
-                mine.add(tile, score, t0 + 16 * g, there, !(t0 >= all_from && t0 + 64 <= all_to && __all(there)));
-                tile.load_v(pool, next.v_at, next.v_in, lane);
-                there = next.there;
-                t0 += kStep;
-            } while (t0 < last);
-        }
-#pragma unroll
-        for (int n = 0; n < R; ++n) mine.total[n] = quarters_sum(mine.total[n]);
-
-        if constexpr (kTokens) {            // join the four waves: two halves, then one
-            auto give = [&](int to) {
-#pragma unroll
-                for (int n = 0; n < R; ++n) {
-#pragma unroll
-                    for (int t = 0; t < D / 16; ++t) *reinterpret_cast<v4f *>(&joined[to][n * 16 + r][t * 16 + 4 * g]) = mine.o[n][t];
-                    if (g == 0) {
-                        joined[to][n * 16 + r][D] = mine.base[n];
-                        joined[to][n * 16 + r][D + 1] = mine.total[n];
-                    }
-                }
-            };
-            auto take = [&](int from) {
-#pragma unroll
-                for (int n = 0; n < R; ++n) {
-                    const float base = joined[from][n * 16 + r][D], total = joined[from][n * 16 + r][D + 1];
-                    const float now = __builtin_fmaxf(mine.base[n], base), reference = now == kNone ? 0.0f : now;
-                    const float fade = __builtin_amdgcn_exp2f(mine.base[n] - reference), other = __builtin_amdgcn_exp2f(base - reference);
-                    mine.base[n] = now;
-                    mine.total[n] = mine.total[n] * fade + total * other;
-#pragma unroll
-                    for (int t = 0; t < D / 16; ++t)
-                        mine.o[n][t] = mine.o[n][t] * fade + *reinterpret_cast<const v4f *>(&joined[from][n * 16 + r][t * 16 + 4 * g]) * other;
-                }
-            };
-            __syncthreads();                // the last rows' results have been read
-            if (wave >= 2) give(wave - 2);
-            __syncthreads();
-            if (wave < 2) take(wave);
-            __syncthreads();
-            if (wave == 1) give(0);
-            __syncthreads();
-            if (wave == 0) take(0);
-        }
-        if (kTokens && wave != 0) continue;
-#pragma unroll
-        for (int n = 0; n < R; ++n) {
+            mine.total[n] = quarters_sum(mine.total[n]);
             if (row0 + n * 16 + r >= rows) continue;
-            if (call.splits > 1) {
-                const int64_t at = split * call.q_rows * call.q_heads + place_out[n];
-#pragma unroll
-                for (int t = 0; t < D / 16; ++t) *reinterpret_cast<v4f *>(call.part + at * D + t * 16 + 4 * g) = mine.o[n][t];
-                if (g == 0) {
-                    float *const stats = call.part + call.splits * call.q_rows * call.q_heads * D + at * 2;
-                    stats[0] = mine.base[n];
-                    stats[1] = mine.total[n];
-                }
+            const int64_t place_out = place_of_row(call, q0, Row(call, queries, h, row0 + n * 16 + r));
+            if (call.splits == 1) {
+                end_row(mine, n, call, place_out, lane);
             } else {
-                const float inverse = ends_with(mine.total[n]);
-#pragma unroll
-                for (int t = 0; t < D / 16; ++t) {
-                    const v4f o = mine.o[n][t] * inverse;
-                    *reinterpret_cast<u32x2 *>(call.out + place_out[n] * D + t * 16 + 4 * g) = u32x2{narrow_bf16x2(o[0], o[1]), narrow_bf16x2(o[2], o[3])};
-                }
-                if (call.lse && g == 0) call.lse[place_out[n]] = log_sum(mine.base[n], mine.total[n]);
+                const int64_t all = call.q_rows * call.q_heads, at = split * all + place_out;
+                part_row(mine, n, call.part + at * D, reinterpret_cast<float2 *>(call.part + call.splits * all * D) + at, lane);
             }
         }
     }
 }
 
-// Joins the splits of an output row, a workgroup each: D / 4 lanes take a split, the others other splits, and the parts are
-// added in order.  Little is read and much waited for: what can be asked for at once is (the splits' statistics one after
-// the other: 17.5 us for 64 splits).
-constexpr int kMostSplits = 64;         // a lane each
+// ---- few rows of short sequences: the waves of a workgroup have the same ones and different tokens
+// Grid: tiles of rows, heads, sequences.
 
-template <int D>
-__global__ __launch_bounds__(256) void join_kernel(const AttentionCall call, int32_t sequences)
+template <int D, int NB, int R>
+__global__ __launch_bounds__(256) void attention_tokens_kernel(const AttentionCall call, const Sequences seqs, const Pool pool)
 {
-    constexpr int kLanes = D / 4, kParts = 256 / kLanes, kRounds = kMostSplits / kParts;
-    constexpr float kNone = -__builtin_inff();
-    __shared__ v4f part[kParts][kLanes];
-    const int64_t all = call.q_rows * call.q_heads, at = blockIdx.x;
-    const int row = (int)(blockIdx.x / (uint32_t)call.q_heads);
-    const int from = call.q_starts[0], to = call.q_starts[sequences];
-    const int mine = threadIdx.x / kLanes, lane = threadIdx.x % kLanes, split = threadIdx.x & 63;
-    const float2 stat = split < call.splits ? reinterpret_cast<const float2 *>(call.part + call.splits * all * D)[split * all + at]
-                                            : float2{kNone, 0.0f};
-    const float *const sums = call.part + at * D + lane * 4;
-    v4f o[kRounds];
+    constexpr int kRows = R * 16, kPitch = D + 4;           // of a row of results in LDS, whose statistics are behind it
+    __shared__ float joined[2][kRows][kPitch];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int r = lane & 15, g = lane >> 4;
+    const int b = blockIdx.z, h = blockIdx.y;
+    const int q0 = within(call.q_starts[b], call.q_rows), queries = within(call.q_starts[b + 1], call.q_rows) - q0;
+    const int length = seqs.length(b, pool.page);
+    const int rows = queries * call.group, tiles = (rows + kRows - 1) / kRows;
+    for (int tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
+        const int row0 = tile * kRows;
+        Rows<D, NB, R> mine;
+        load_q(mine, call, q0, queries, h, row0, lane);
+        start_rows(mine, call, queries, length, h, row0, lane);
+        const Span span = span_of(call, queries, length, row0, row0 + kRows - 1);
+        walk<256>(mine, pool, seqs.table + b * seqs.width, seqs.width, h, call.scale, span.first + wave * 64, span.last, span, lane);
 #pragma unroll
-    for (int i = 0; i < kRounds; ++i) {
-        const int s = mine + i * kParts;
-        o[i] = s < call.splits ? *reinterpret_cast<const v4f *>(sums + s * all * D) : v4f{0, 0, 0, 0};
+        for (int n = 0; n < R; ++n) mine.total[n] = quarters_sum(mine.total[n]);
+        // join the four waves: two halves, then one
+        auto give = [&](int half) {
+#pragma unroll
+            for (int n = 0; n < R; ++n) {
+                float *const row = joined[half][n * 16 + r];
+#pragma unroll
+                for (int t = 0; t < D / 16; ++t) *reinterpret_cast<v4f *>(row + t * 16 + 4 * g) = mine.o[n][t];
+                if (g == 0) {
+                    row[D] = mine.base[n];
+                    row[D + 1] = mine.total[n];
+                }
+            }
+        };
+        auto take = [&](int half) {
+#pragma unroll
+            for (int n = 0; n < R; ++n) {
+                const float *const row = joined[half][n * 16 + r];
+                const float base = row[D], now = __builtin_fmaxf(mine.base[n], base);
+                const float reference = now == -__builtin_inff() ? 0.0f : now;
+                const float fade = __builtin_amdgcn_exp2f(mine.base[n] - reference), other = __builtin_amdgcn_exp2f(base - reference);
+                mine.base[n] = now;
+                mine.total[n] = mine.total[n] * fade + row[D + 1] * other;
+#pragma unroll
+                for (int t = 0; t < D / 16; ++t)
+                    mine.o[n][t] = mine.o[n][t] * fade + *reinterpret_cast<const v4f *>(row + t * 16 + 4 * g) * other;
+            }
+        };
+        __syncthreads();                // the last rows' results have been read
+        if (wave >= 2) give(wave - 2);
+        __syncthreads();
+        if (wave < 2) take(wave);
+        __syncthreads();
+        if (wave == 1) give(0);
+        __syncthreads();
+        if (wave != 0) continue;
+        take(0);
+#pragma unroll
+        for (int n = 0; n < R; ++n) {
+            if (row0 + n * 16 + r < rows) end_row(mine, n, call, place_of_row(call, q0, Row(call, queries, h, row0 + n * 16 + r)), lane);
+        }
     }
-    loads_first();
-    if (row < from || row >= to) return;        // a row of no sequence
-    float now = stat.x;
+}
+
+// ---- few rows of any sequences: every wave has an even share of all that is to be done
+// What is to be done is counted in tiles of 64 tokens for one tile of rows and key head (an item).  Wave w has the tiles w * per ..
+// (w + 1) * per - 1 of all sequences' items in order and walks through them without a pause, asking for an item's first tile
+// while it ends the one before (with a workgroup an item and sequence, the longest took as long again as all together; with shares
+// of workgroups that began every item anew, an item's beginning took as long as 500 tokens).  The part of an item that it
+// has, if not the whole, goes to its slot 0 where the item began before, to slot 1 where it begins here; the join finds the
+// parts by the same count.
+
+constexpr int kShares = 2048;               // waves: eight a CU
+constexpr int kMostShared = 1024;           // sequences that a workgroup counts
+
+// What a workgroup knows of the sequences: before[b] tiles are of those before b, before[count] of all.
+struct Counted {
+    int64_t before[kMostShared + 1], wave_sums[4];
+    int q0[kMostShared + 1], length[kMostShared];
+};
+
+// An item's tiles, and where they begin.
+struct ItemTiles {
+    int first, tiles;
+    __device__ __forceinline__ ItemTiles(const AttentionCall &call, int queries, int length)
+    {
+        first = queries <= 0 ? 0 : span_of(call, queries, length, 0, 0).first;
+        tiles = length > first ? (length - first + 63) / 64 : 1;
+    }
+};
+
+// The whole workgroup.
+__device__ __forceinline__ void count_tiles(Counted &all, const AttentionCall &call, const Sequences &seqs, const Pool &pool, int tile_rows)
+{
+    constexpr int kPer = kMostShared / 256;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    int64_t mine[kPer], sum = 0;
+    const int per = (call.sequences + 255) / 256;           // of a thread: one up to 256 sequences
 #pragma unroll
-    for (int step = 1; step < 64; step *= 2) now = __builtin_fmaxf(now, __shfl_xor(now, step));
-    const float weight = __builtin_amdgcn_exp2f(stat.x - (now == kNone ? 0.0f : now));
-    float total = stat.y * weight;
+    for (int i = 0; i < kPer; ++i) {
+        const int b = threadIdx.x * per + i;
+        mine[i] = 0;
+        if (i < per && b < call.sequences) {
+            const int q0 = within(call.q_starts[b], call.q_rows), past = within(call.q_starts[b + 1], call.q_rows);
+            const int length = seqs.length(b, pool.page);
+            all.q0[b] = q0;
+            if (b + 1 == call.sequences) all.q0[b + 1] = past;
+            all.length[b] = length;
+            if (past > q0) {
+                const int items = ((past - q0) * call.group + tile_rows - 1) / tile_rows * pool.heads;
+                mine[i] = (int64_t)items * ItemTiles(call, past - q0, length).tiles;
+            }
+        }
+        sum += mine[i];
+    }
+    int64_t upto = sum;
 #pragma unroll
-    for (int step = 1; step < 64; step *= 2) total += __shfl_xor(total, step);
-    v4f acc = {0, 0, 0, 0};
-#pragma unroll
-    for (int i = 0; i < kRounds; ++i) acc += o[i] * __shfl(weight, mine + i * kParts);
-    part[mine][lane] = acc;
+    for (int step = 1; step < 64; step *= 2) {
+        const int64_t other = __shfl_up(upto, step);
+        if (lane >= step) upto += other;
+    }
+    if (lane == 63) all.wave_sums[wave] = upto;
     __syncthreads();
-    if (mine != 0) return;
+    int64_t at = upto - sum;
+    for (int i = 0; i < wave; ++i) at += all.wave_sums[i];
 #pragma unroll
-    for (int p = 1; p < kParts; ++p) acc += part[p][lane];
-    acc *= ends_with(total);
-    *reinterpret_cast<u32x2 *>(call.out + at * D + lane * 4) = u32x2{narrow_bf16x2(acc[0], acc[1]), narrow_bf16x2(acc[2], acc[3])};
-    if (call.lse && lane == 0) call.lse[at] = log_sum(now, total);
+    for (int i = 0; i < kPer; ++i) {
+        const int b = threadIdx.x * per + i;
+        if (i < per && b <= call.sequences) all.before[b] = at;
+        at += mine[i];
+    }
+    if (call.sequences == per * 256 && threadIdx.x == 255) all.before[call.sequences] = at;
+    __syncthreads();
+}
+
+// The tiles of a share: up to two, eight waves a CU have them; more are shared out among four, which ask for as much at a time as
+// the memory gives, and leave fewer parts (MI355X, 30 thousand tiles: 93 us against 99; 1100 tiles in eight 12.4, in four 19.8).
+__host__ __device__ inline int64_t share_of(int64_t tiles)
+{
+    const int64_t per = (tiles + kShares - 1) / kShares;
+    return per <= 2 ? per : (tiles + kShares / 2 - 1) / (kShares / 2);
+}
+
+// What the join needs of the count: before[], behind the parts' statistics.
+template <int D, int R>
+__device__ __forceinline__ int64_t *kept_count(const AttentionCall &call)
+{
+    return reinterpret_cast<int64_t *>(call.part + (int64_t)kShares * 2 * R * 16 * (D + 2));
+}
+
+// Slot `slot` of wave w: its row's place among the parts.
+template <int R>
+__device__ __forceinline__ int64_t slot_row(int w, int slot, int row) { return ((int64_t)w * 2 + slot) * (R * 16) + row; }
+template <int D, int R>
+__device__ __forceinline__ float2 *slot_stats(const AttentionCall &call)
+{
+    return reinterpret_cast<float2 *>(call.part + (int64_t)kShares * 2 * R * 16 * D);
+}
+
+// A place in a wave's walk: an item and a tile of it; all the same in every lane.
+struct Cursor {
+    int b, h, row0, t;          // sequence, key head, first row; first token of the tile
+    int q0, queries, length, first, last;       // of the sequence; tokens first .. last - 1 are the item's
+
+    __device__ __forceinline__ void enter(const Counted &all, const AttentionCall &call, int sequence)
+    {
+        b = __builtin_amdgcn_readfirstlane(sequence);
+        q0 = __builtin_amdgcn_readfirstlane(all.q0[b]);
+        queries = __builtin_amdgcn_readfirstlane(all.q0[b + 1]) - q0;
+        length = __builtin_amdgcn_readfirstlane(all.length[b]);
+        const ItemTiles item(call, queries, length);
+        first = item.first;
+        last = item.first + item.tiles * 64;
+    }
+    // The next tile; past the last item of all, one that is loaded and not used.
+    __device__ __forceinline__ void advance(const Counted &all, const AttentionCall &call, const Pool &pool, int tile_rows)
+    {
+        t += 64;
+        if (t < last) return;
+        t = first;
+        if (++h < pool.heads) return;
+        h = 0;
+        row0 += tile_rows;
+        if (row0 < queries * call.group) return;
+        row0 = 0;
+        int next = b + 1;
+        while (next < call.sequences && all.q0[next + 1] <= all.q0[next]) ++next;       // without queries: no items
+        if (next >= call.sequences) return;
+        enter(all, call, next);
+        t = first;
+    }
+};
+
+template <int D, int NB, int R>
+__global__ __launch_bounds__(256, R == 1 && D <= 128 ? 2 : 1) void attention_shares_kernel(const AttentionCall call,
+                                                                                           const Sequences seqs, const Pool pool)
+{
+    constexpr int kRows = R * 16;
+    __shared__ Counted all;
+    const int lane = threadIdx.x & 63, share = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
+    const int r = lane & 15, g = lane >> 4;
+    count_tiles(all, call, seqs, pool, kRows);
+    const int64_t total = all.before[call.sequences], per = share_of(total), from = share * per;
+    if (blockIdx.x == 0) {
+        for (int b = threadIdx.x; b <= call.sequences; b += 256) kept_count<D, R>(call)[b] = all.before[b];
+    }
+    if (from >= total) return;
+    int left = __builtin_amdgcn_readfirstlane((int)(total - from < per ? total - from : per));
+    Cursor at;                          // what is computed
+    {
+        int b = 0, past = call.sequences;       // before[b] <= from < before[past]
+        while (past - b > 1) {
+            const int middle = (b + past) / 2;
+            if (all.before[middle] <= from) {
+                b = middle;
+            } else {
+                past = middle;
+            }
+        }
+        at.enter(all, call, b);
+        const int64_t mine = from - all.before[b];
+        const int tiles = (at.last - at.first) / 64;
+        const int item = __builtin_amdgcn_readfirstlane((int)(mine / tiles));
+        at.t = at.first + __builtin_amdgcn_readfirstlane((int)(mine - (int64_t)item * tiles)) * 64;
+        const int row_tile = item / pool.heads;
+        at.h = item - row_tile * pool.heads;
+        at.row0 = row_tile * kRows;
+    }
+    auto ids_of = [&](const Cursor &c) { return PageIds(pool, seqs.table + c.b * seqs.width, seqs.width, c.t, lane); };
+    Rows<D, NB, R> mine;
+    Tile<D, NB> tile;
+    load_q(mine, call, at.q0, at.queries, at.h, at.row0, lane);
+    bool there;
+    {
+        const Place place(pool, ids_of(at), at.h, at.t, lane);
+        tile.load_k(pool, place.k_at, place.k_in, place.v_at, place.v_in, lane);
+        tile.load_v(pool, place.v_at, place.v_in, lane);
+        there = place.there;
+    }
+    Cursor next = at;                   // what is loaded
+    next.advance(all, call, pool, kRows);
+    PageIds ids = ids_of(next);
+    start_rows(mine, call, at.queries, at.length, at.h, at.row0, lane);
+    Span span = span_of(call, at.queries, at.length, at.row0, at.row0 + kRows - 1);
+    bool begun_here = at.t == at.first;
+    for (;;) {
+        const Place place(pool, ids, next.h, next.t, lane);
+        float score[R][16];
+        mine.scores(tile, call.scale, score);
+        tile.load_k(pool, place.k_at, place.k_in, place.v_at, place.v_in, lane);
+        const bool item_ends = at.t + 64 >= at.last, ends = item_ends || left == 1;
+        if (ends) load_q(mine, call, next.q0, next.queries, next.h, next.row0, lane);
+        Cursor after = next;
+        after.advance(all, call, pool, kRows);
+        ids = ids_of(after);
+        __builtin_amdgcn_sched_barrier(0);
+        mine.add(tile, score, at.t + 16 * g, there, !(at.t >= span.all_from && at.t + 64 <= span.all_to && __all(there)));
+        tile.load_v(pool, place.v_at, place.v_in, lane);
+        there = place.there;
+        if (ends) {
+#pragma unroll
+            for (int n = 0; n < R; ++n) {
+                mine.total[n] = quarters_sum(mine.total[n]);
+                const int row = at.row0 + n * 16 + r;
+                if (row >= at.queries * call.group) continue;
+                if (begun_here && item_ends) {
+                    end_row(mine, n, call, place_of_row(call, at.q0, Row(call, at.queries, at.h, row)), lane);
+                } else {
+                    const int64_t place_in = slot_row<R>(share, begun_here ? 1 : 0, n * 16 + r);
+                    part_row(mine, n, call.part + place_in * D, slot_stats<D, R>(call) + place_in, lane);
+                }
+            }
+            if (left == 1) return;
+            start_rows(mine, call, next.queries, next.length, next.h, next.row0, lane);
+            span = span_of(call, next.queries, next.length, next.row0, next.row0 + kRows - 1);
+            begun_here = true;
+        }
+        --left;
+        at = next;
+        next = after;
+    }
+}
+
+// ---- joining parts
+// An output row and head has W of a workgroup's four waves: D / 4 lanes take a part, the others other parts, and the sums are added in
+// order.  Little is read and much waited for: what can be asked for at once is (one part's statistics after the
+// other's: 17.5 us for 64).
+
+template <int D, int W>
+struct Joiner {
+    static constexpr int kLanes = D / 4, kParts = W * 64 / kLanes, kRounds = 64 / kParts < 8 ? 64 / kParts : 8;
+    float now = -__builtin_inff(), total = 0.0f;
+    v4f acc = {0, 0, 0, 0};
+
+    // `count` parts, those that this row's first wave begins with: part i's statistics are at stat_of(i), its sums at sums_of(i)
+    template <typename Stat, typename Sums>
+    __device__ __forceinline__ void join(int count, Stat stat_of, Sums sums_of)
+    {
+        const int thread = threadIdx.x % (W * 64), mine = thread / kLanes, lane = thread % kLanes;
+        for (int at = 0; at < count; at += 64) {        // 64 parts at a time, a lane has one's statistics
+            const int part = at + (threadIdx.x & 63);
+            const float2 stat = part < count ? *stat_of(part) : float2{-__builtin_inff(), 0.0f};
+            v4f o[kRounds];
+            auto load = [&](int from) {
+#pragma unroll
+                for (int i = 0; i < kRounds; ++i) {
+                    const int p = at + from + mine + i * kParts;
+                    o[i] = p < count ? *reinterpret_cast<const v4f *>(sums_of(p) + lane * 4) : v4f{0, 0, 0, 0};
+                }
+            };
+            load(0);
+            loads_first();
+            float most = __builtin_fmaxf(stat.x, now);
+#pragma unroll
+            for (int step = 1; step < 64; step *= 2) most = __builtin_fmaxf(most, __shfl_xor(most, step));
+            const float reference = most == -__builtin_inff() ? 0.0f : most;
+            const float weight = __builtin_amdgcn_exp2f(stat.x - reference), fade = __builtin_amdgcn_exp2f(now - reference);
+            float sum = stat.y * weight;
+#pragma unroll
+            for (int step = 1; step < 64; step *= 2) sum += __shfl_xor(sum, step);
+            total = total * fade + sum;
+            acc *= fade;
+            now = most;
+            for (int from = 0;;) {
+#pragma unroll
+                for (int i = 0; i < kRounds; ++i) acc += o[i] * __shfl(weight, (from + mine + i * kParts) & 63);
+                from += kRounds * kParts;
+                if (from >= 64 || at + from >= count) break;
+                load(from);
+            }
+        }
+    }
+    // The whole workgroup, rows that have nothing to join among it.
+    __device__ __forceinline__ void end(v4f (&shared)[256], const AttentionCall &call, int64_t at, bool write)
+    {
+        const int thread = threadIdx.x % (W * 64);
+        shared[threadIdx.x] = acc;
+        __syncthreads();
+        if (!write || thread >= kLanes) return;
+#pragma unroll
+        for (int p = 1; p < kParts; ++p) acc += shared[threadIdx.x + p * kLanes];
+        acc *= ends_with(total);
+        *reinterpret_cast<u32x2 *>(call.out + at * D + thread * 4) = u32x2{narrow_bf16x2(acc[0], acc[1]), narrow_bf16x2(acc[2], acc[3])};
+        if (call.lse && thread == 0) call.lse[at] = log_sum(now, total);
+    }
+};
+
+// The splits of attention_rows_kernel.
+template <int D, int W>
+__global__ __launch_bounds__(256) void join_splits_kernel(const AttentionCall call)
+{
+    __shared__ v4f shared[256];
+    const int64_t all = call.q_rows * call.q_heads, at = (int64_t)blockIdx.x * (4 / W) + threadIdx.x / (W * 64);
+    const int row = (int)((uint32_t)at / (uint32_t)call.q_heads);
+    const bool write = at < all && row >= call.q_starts[0] && row < call.q_starts[call.sequences];     // not a row of no sequence
+    Joiner<D, W> joiner;
+    const float2 *const stats = reinterpret_cast<const float2 *>(call.part + call.splits * all * D) + at;
+    joiner.join(write ? call.splits : 0, [&](int s) { return stats + s * all; },
+                [&](int s) { return call.part + (s * all + at) * D; });
+    joiner.end(shared, call, at, write);
+}
+
+// The shares of attention_shares_kernel, where a row's item is of more than one: otherwise the wave that had it wrote it.
+template <int D, int R, int W>
+__global__ __launch_bounds__(256) void join_shares_kernel(const AttentionCall call, const Sequences seqs, const Pool pool)
+{
+    __shared__ v4f shared[256];
+    const int lane = threadIdx.x & 63;
+    const int64_t at = (int64_t)blockIdx.x * (4 / W) + threadIdx.x / (W * 64);
+    const int row = (int)((uint32_t)at / (uint32_t)call.q_heads), head = (int)at - row * call.q_heads;
+    // the row's sequence, by the wave: the last one that begins with it or before, and has it
+    int b = -1;
+    for (int from = 0; from < call.sequences; from += 64) {
+        const int i = from + lane < call.sequences ? from + lane : call.sequences - 1;
+        const uint64_t has = __ballot(row >= call.q_starts[i] && row < call.q_starts[i + 1] && at < call.q_rows * call.q_heads);
+        if (has) b = from + __builtin_ctzll(has);
+    }
+    if (b >= call.sequences) b = call.sequences - 1;
+    int count = 0, first = 0, mine = 0;
+    if (b >= 0) {
+        const int64_t *const before = kept_count<D, R>(call);
+        const int q0 = within(call.q_starts[b], call.q_rows), queries = within(call.q_starts[b + 1], call.q_rows) - q0;
+        const int tiles = ItemTiles(call, queries, seqs.length(b, pool.page)).tiles;
+        const int64_t per = share_of(before[call.sequences]);
+        const int h = head / call.group;
+        mine = (row - q0) * call.group + head - h * call.group;
+        const int64_t from = before[b] + ((int64_t)(mine / (R * 16)) * pool.heads + h) * tiles;
+        first = (int)(from / per);
+        count = (int)((from + tiles - 1) / per) - first + 1;
+        if (count == 1) count = 0;
+    }
+    Joiner<D, W> joiner;
+    auto place = [&](int p) { return slot_row<R>(first + p, p == 0 ? 1 : 0, mine % (R * 16)); };
+    joiner.join(count, [&](int p) { return slot_stats<D, R>(call) + place(p); }, [&](int p) { return call.part + place(p) * D; });
+    joiner.end(shared, call, at, count > 0);
 }
 
 }  // namespace cache
