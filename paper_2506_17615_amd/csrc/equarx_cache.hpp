@@ -911,24 +911,27 @@ __global__ __launch_bounds__(256, R == 1 && D <= 128 ? 2 : 1) void attention_sha
 }
 
 // ---- joining parts
-// An output row and head has W of a workgroup's four waves: D / 4 lanes take a part, the others other parts, and the sums are added in
-// order.  Little is read and much waited for: what can be asked for at once is (one part's statistics after the
-// other's: 17.5 us for 64).
+// An output row and head has W of a workgroup's four waves, which take 64 parts each at a time; in a wave D / 4 lanes take a part, the
+// others other parts, and the sums are added in order.  Little is read and much waited for: what can be asked for at once is (one
+// part's statistics after the other's: 17.5 us for 64).
 
 template <int D, int W>
 struct Joiner {
-    static constexpr int kLanes = D / 4, kParts = W * 64 / kLanes, kRounds = 64 / kParts < 8 ? 64 / kParts : 8;
+    static constexpr int kLanes = D / 4, kParts = 64 / kLanes, kRounds = 64 / kParts < 8 ? 64 / kParts : 8;
+    struct Shared {
+        v4f acc[256];
+        float2 stats[4];
+    };
     float now = -__builtin_inff(), total = 0.0f;
     v4f acc = {0, 0, 0, 0};
 
-    // `count` parts, those that this row's first wave begins with: part i's statistics are at stat_of(i), its sums at sums_of(i)
+    // `count` parts: part i's statistics are at stat_of(i), its sums at sums_of(i)
     template <typename Stat, typename Sums>
     __device__ __forceinline__ void join(int count, Stat stat_of, Sums sums_of)
     {
-        const int thread = threadIdx.x % (W * 64), mine = thread / kLanes, lane = thread % kLanes;
-        for (int at = 0; at < count; at += 64) {        // 64 parts at a time, a lane has one's statistics
-            const int part = at + (threadIdx.x & 63);
-            const float2 stat = part < count ? *stat_of(part) : float2{-__builtin_inff(), 0.0f};
+        const int thread = threadIdx.x & 63, mine = thread / kLanes, lane = thread % kLanes;
+        for (int at = threadIdx.x % (W * 64) / 64 * 64; at < count; at += W * 64) {
+            const float2 stat = at + thread < count ? *stat_of(at + thread) : float2{-__builtin_inff(), 0.0f};
             v4f o[kRounds];
             auto load = [&](int from) {
 #pragma unroll
@@ -960,17 +963,29 @@ struct Joiner {
         }
     }
     // The whole workgroup, rows that have nothing to join among it.
-    __device__ __forceinline__ void end(v4f (&shared)[256], const AttentionCall &call, int64_t at, bool write)
+    __device__ __forceinline__ void end(Shared &shared, const AttentionCall &call, int64_t at, bool write)
     {
-        const int thread = threadIdx.x % (W * 64);
-        shared[threadIdx.x] = acc;
+        const int thread = threadIdx.x % (W * 64), wave = threadIdx.x / 64, first = wave / W * W;
+        shared.acc[threadIdx.x] = acc;
+        if (threadIdx.x % 64 == 0) shared.stats[wave] = float2{now, total};
         __syncthreads();
         if (!write || thread >= kLanes) return;
+        float most = shared.stats[first].x;
 #pragma unroll
-        for (int p = 1; p < kParts; ++p) acc += shared[threadIdx.x + p * kLanes];
+        for (int w = 1; w < W; ++w) most = __builtin_fmaxf(most, shared.stats[first + w].x);
+        const float reference = most == -__builtin_inff() ? 0.0f : most;
+        acc = v4f{0, 0, 0, 0};
+        total = 0.0f;
+#pragma unroll
+        for (int w = 0; w < W; ++w) {
+            const float weight = __builtin_amdgcn_exp2f(shared.stats[first + w].x - reference);
+            total += shared.stats[first + w].y * weight;
+#pragma unroll
+            for (int p = 0; p < kParts; ++p) acc += shared.acc[(first + w) * 64 + p * kLanes + thread] * weight;
+        }
         acc *= ends_with(total);
         *reinterpret_cast<u32x2 *>(call.out + at * D + thread * 4) = u32x2{narrow_bf16x2(acc[0], acc[1]), narrow_bf16x2(acc[2], acc[3])};
-        if (call.lse && thread == 0) call.lse[at] = log_sum(now, total);
+        if (call.lse && thread == 0) call.lse[at] = log_sum(most, total);
     }
 };
 
@@ -978,7 +993,7 @@ struct Joiner {
 template <int D, int W>
 __global__ __launch_bounds__(256) void join_splits_kernel(const AttentionCall call)
 {
-    __shared__ v4f shared[256];
+    __shared__ typename Joiner<D, W>::Shared shared;
     const int64_t all = call.q_rows * call.q_heads, at = (int64_t)blockIdx.x * (4 / W) + threadIdx.x / (W * 64);
     const int row = (int)((uint32_t)at / (uint32_t)call.q_heads);
     const bool write = at < all && row >= call.q_starts[0] && row < call.q_starts[call.sequences];     // not a row of no sequence
@@ -993,7 +1008,7 @@ __global__ __launch_bounds__(256) void join_splits_kernel(const AttentionCall ca
 template <int D, int R, int W>
 __global__ __launch_bounds__(256) void join_shares_kernel(const AttentionCall call, const Sequences seqs, const Pool pool)
 {
-    __shared__ v4f shared[256];
+    __shared__ typename Joiner<D, W>::Shared shared;
     const int lane = threadIdx.x & 63;
     const int64_t at = (int64_t)blockIdx.x * (4 / W) + threadIdx.x / (W * 64);
     const int row = (int)((uint32_t)at / (uint32_t)call.q_heads), head = (int)at - row * call.q_heads;
