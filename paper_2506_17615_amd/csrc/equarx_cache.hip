@@ -163,7 +163,7 @@ void launch_attention(const AttentionPlan &plan, const AttentionCall &call, cons
         part.q_starts += at;
         const Sequences some{seqs.table + at * seqs.width, seqs.lengths + at, seqs.width};
         if (plan.form == AttentionForm::kRows) {
-            ctx.launch3d(attention_rows_kernel<D, NB, 2>, (unsigned)tiles, (unsigned)(pool.heads * plan.splits), (unsigned)count, 256,
+            ctx.launch3d(attention_rows_kernel<D, NB>, (unsigned)tiles, (unsigned)(pool.heads * plan.splits), (unsigned)count, 256,
                          part, some, pool);
         } else {
             ctx.launch3d(plan.rows16 == 1 ? attention_tokens_kernel<D, NB, 1> : attention_tokens_kernel<D, NB, 2>,

@@ -291,11 +291,14 @@ struct Tile {
     }
 };
 
-// v of lane kLane of this lane's sixteen.
+// A block with this is jumped over where it is not due; else the compiler makes selects of it, for every tile.
+__device__ __forceinline__ void stay_a_branch() { asm volatile(""); }
+
+// v of lane kLane of this lane's sixteen: a part of the product that takes it.
 template <int kLane>
 __device__ __forceinline__ float of_lane(float v)
 {
-    return __uint_as_float((uint32_t)__builtin_amdgcn_mov_dpp((int)__float_as_uint(v), 0x150 + kLane, 0xf, 0xf, false));
+    return __uint_as_float((uint32_t)__builtin_amdgcn_mov_dpp((int)__float_as_uint(v), 0x150 + kLane, 0xf, 0xf, true));
 }
 
 template <int... kNumbers, typename F>
@@ -356,7 +359,7 @@ struct Rows {
                 for (int n = 0; n < R; ++n) {
                     float sum = dot[n][0][i] * of_lane<4 * s + i>(ks[0]);
 #pragma unroll
-                    for (int m = 1; m < NB; ++m) sum = __builtin_fmaf(dot[n][m][i], of_lane<4 * s + i>(ks[m]), sum);
+                    for (int m = 1; m < NB; ++m) sum += dot[n][m][i] * of_lane<4 * s + i>(ks[m]);
                     score[n][4 * s + i] = sum;
                 }
             });
@@ -374,6 +377,7 @@ struct Rows {
             int from = 0;               // seen: 0 <= token - from < count, counted from this lane's first
             uint32_t count = 16;
             if (masked) {
+                stay_a_branch();
                 const int lo = low[n] + 1 - first, hi = high[n] + 1 - first;
                 from = lo < 0 ? 0 : lo < 16 ? lo : 16;
                 const int to = hi < 0 ? 0 : hi < 16 ? hi : 16;
@@ -583,18 +587,100 @@ __device__ __forceinline__ void part_row(const Rows<D, NB, R> &mine, int n, floa
     if (g == 0) *stats = float2{mine.base[n], mine.total[n]};
 }
 
-// ---- many rows: the waves of a workgroup have different ones
+// ---- many rows: the waves of a workgroup have 32 different ones each
+// Here the matrix unit and what comes between its instructions are the bound, so codes are widened once for a workgroup: wave w takes
+// the keys and values of sixteen tokens of 64, as bf16 they wait in LDS (two buffers: the next tile's are written, and the one
+// after that asked for, while this one's are used) in the order in which the lanes of a 32x32x16 instruction read them.
+// (2 x 2048 rows of 32 heads at the end of 8192 tokens, blocks of 64: every wave widening all for itself, 16x16x32, 1055 us; this 663.)
+//
+// As above with 32 for 16: the tokens of an instruction's rows are chosen so that S^T leaves lane (row c = l % 32, half h = l / 32)
+// with 16 consecutive tokens 16 h .. of the 32, row 8 j + 4 h + i being token 16 h + 4 j + i, and O^T += V^T P^T takes eight of
+// these as they are.
 // Grid: tiles of rows, heads x splits, sequences.  Parts: [splits][q_rows][q_heads].
 
-template <int D, int NB, int R>
-__global__ __launch_bounds__(256) void attention_rows_kernel(const AttentionCall call, const Sequences seqs, const Pool pool)
+typedef float v16f __attribute__((ext_vector_type(16)));
+
+template <int D, int NB>
+struct RowsTile {
+    static constexpr int kKeys = D * 128, kBytes = 2 * kKeys;       // of bf16, a tile's keys and then its values
+    static constexpr int kPieces = D / 64;                          // of 16 codes, a lane's keys and its values
+
+    // What a wave's lane has of a tile on the way: lane l 1/4 of the keys of token l / 4 of the wave's sixteen, and the sixteen values
+    // of elements l, l + 64, ...; and one token's scales, number l % 16 of either group of its half.
+    u32x4 k[kPieces], v[kPieces];
+    float ks[2][NB], vs[2][NB];
+    bool there[2];
+
+    __device__ __forceinline__ void load(const Pool &pool, const int32_t *table, int64_t width, int h, int t, int wave, int lane)
+    {
+        auto page_at = [&](int token, bool &exists) {       // first slot of a token's page and this head; any one if there is none
+            const int p = page_of(pool, token), id = p < width ? table[p] : -1;
+            exists = id >= 0 && id < pool.pages;
+            return pool.place(exists ? id : 0, h) * pool.page;
+        };
+        auto in_page = [&](int token) { return token - page_of(pool, token) * pool.page; };
+        bool exists;
+        const int mine = t + 16 * wave;
+        const int64_t at = page_at(mine, exists) + in_page(mine);
+        const int8_t *const keys = pool.kc + (at + (lane >> 2)) * D + (lane & 3) * (D / 4);
+        const int8_t *const values = pool.vc + at * D + lane * 16;
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) {
+            k[i] = *reinterpret_cast<const u32x4 *>(keys + 16 * i);
+            v[i] = *reinterpret_cast<const u32x4 *>(values + 1024 * i);
+        }
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+            const int group = t + 32 * b + 16 * (lane >> 5);
+            const int64_t page = page_at(group, there[b]) * NB + in_page(group) + (lane & 15);
+#pragma unroll
+            for (int m = 0; m < NB; ++m) {
+                ks[b][m] = pool.ks[page + (int64_t)m * pool.page];
+                vs[b][m] = pool.vs[page + (int64_t)m * pool.page];
+            }
+        }
+    }
+
+    // The codes, widened, into a buffer.  Keys: fragment (32 tokens, 16 elements) is 1 KB, lane after lane.  Values: fragment (32
+    // elements, 32 tokens, 16 of them) the same.
+    __device__ __forceinline__ void store(uint8_t *buffer, int wave, int lane) const
+    {
+        const int token = lane >> 2, quarter = lane & 3, place = 8 * (token >> 2) + 4 * (wave & 1) + (token & 3);
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) {
+            uint8_t *const keys = buffer + (wave >> 1) * (D * 64) + (quarter * kPieces + i) * 1024 + place * 16;
+            *reinterpret_cast<bf16x8 *>(keys) = widen_codes(k[i].x, k[i].y);
+            *reinterpret_cast<bf16x8 *>(keys + 512) = widen_codes(k[i].z, k[i].w);
+            uint8_t *const values = buffer + kKeys + ((2 * i + (lane >> 5)) * 4 + (wave >> 1) * 2) * 1024 + ((wave & 1) * 32 + (lane & 31)) * 16;
+            *reinterpret_cast<bf16x8 *>(values) = widen_codes(v[i].x, v[i].y);
+            *reinterpret_cast<bf16x8 *>(values + 1024) = widen_codes(v[i].z, v[i].w);
+        }
+    }
+};
+
+__device__ __forceinline__ float halves_max(float v)
 {
-    constexpr int kRows = 4 * R * 16;
+    auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __builtin_fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float halves_sum(float v)
+{
+    auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+template <int D, int NB>
+__global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void attention_rows_kernel(const AttentionCall call, const Sequences seqs,
+                                                                               const Pool pool)
+{
+    constexpr int kRows = 128;
+    __shared__ __align__(16) uint8_t lds[2][RowsTile<D, NB>::kBytes];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int r = lane & 15;
+    const int r = lane & 31, half = lane >> 5;
     const int b = blockIdx.z, split = blockIdx.y / (uint32_t)pool.heads, h = blockIdx.y - split * pool.heads;
     const int q0 = within(call.q_starts[b], call.q_rows), queries = within(call.q_starts[b + 1], call.q_rows) - q0;
     const int length = seqs.length(b, pool.page);
+    const int32_t *const table = seqs.table + b * seqs.width;
     // this split's tokens: whole tiles; a sequence longer than the host knew has longer splits
     int chunk = call.chunk;
     if ((int64_t)chunk * call.splits < length) chunk = (int)((uint32_t)(length + call.splits - 1) / (uint32_t)call.splits + 63 & ~63u);
@@ -602,25 +688,170 @@ __global__ __launch_bounds__(256) void attention_rows_kernel(const AttentionCall
 
     const int rows = queries * call.group, row_tiles = (rows + kRows - 1) / kRows;
     for (int turn = blockIdx.x; turn < row_tiles; turn += gridDim.x) {
-        const int row0 = (row_tiles - 1 - turn) * kRows + wave * R * 16;        // with causal rows the last ones are the longest: first
-        Rows<D, NB, R> mine;
-        load_q(mine, call, q0, queries, h, row0, lane);
-        start_rows(mine, call, queries, length, h, row0, lane);
-        Span span = span_of(call, queries, length, row0, row0 + R * 16 - 1);
+        const int tile_row = (row_tiles - 1 - turn) * kRows;        // with causal rows the last ones are the longest: first
+        const int row0 = tile_row + wave * 32;
+        const Row row(call, queries, h, row0 + r);
+        bf16x8 q[D / 16];
+        {
+            const uint16_t *const from = call.q + (q0 + row.query) * call.q_row + row.head * call.q_head + half * 8;
+#pragma unroll
+            for (int j = 0; j < D / 16; ++j) q[j] = *reinterpret_cast<const bf16x8 *>(from + 16 * j);
+        }
+        const int at = length - queries + row.query;
+        const int high = call.causal ? (at < -1 ? -1 : at) : length - 1;        // seen: low < token <= high
+        const int low = call.window && at >= call.window ? at - call.window : -1;
+        // what any row of the workgroup sees of this split, and what all of the wave's see
+        Span span = span_of(call, queries, length, tile_row, tile_row + kRows - 1);
+        const Span mine = span_of(call, queries, length, row0, row0 + 31);
         if (split_from > span.first) span.first = split_from < length ? (int)split_from : length;
         if (split_from + chunk < span.last) span.last = (int)split_from + chunk;
-        walk<64>(mine, pool, seqs.table + b * seqs.width, seqs.width, h, call.scale, span.first, span.last, span, lane);
+
+        v16f o[D / 32];
 #pragma unroll
-        for (int n = 0; n < R; ++n) {
-            mine.total[n] = quarters_sum(mine.total[n]);
-            if (row0 + n * 16 + r >= rows) continue;
-            const int64_t place_out = place_of_row(call, q0, Row(call, queries, h, row0 + n * 16 + r));
-            if (call.splits == 1) {
-                end_row(mine, n, call, place_out, lane);
-            } else {
-                const int64_t all = call.q_rows * call.q_heads, at = split * all + place_out;
-                part_row(mine, n, call.part + at * D, reinterpret_cast<float2 *>(call.part + call.splits * all * D) + at, lane);
+        for (int t = 0; t < D / 32; ++t) o[t] = v16f{0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
+        float base = -__builtin_inff(), total = 0.0f;
+        RowsTile<D, NB> next;
+        int cur = 0;
+        if (span.first < span.last) {
+            __syncthreads();                    // the last rows' tiles have been read
+            next.load(pool, table, seqs.width, h, span.first, wave, lane);
+            next.store(lds[0], wave, lane);
+        }
+        for (int t0 = span.first; t0 < span.last; t0 += 64) {
+            float ks[2][NB], vs[2][NB];
+            bool there[2];
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                there[i] = next.there[i];
+#pragma unroll
+                for (int m = 0; m < NB; ++m) {
+                    ks[i][m] = next.ks[i][m] * call.scale;
+                    vs[i][m] = next.vs[i][m];
+                }
             }
+            __syncthreads();                    // this tile is there for all, and the other buffer read by all
+            const bool more = t0 + 64 < span.last;
+            if (more) next.load(pool, table, seqs.width, h, t0 + 64, wave, lane);
+            const uint8_t *const tile = lds[cur];
+            if (t0 < mine.last && t0 + 64 > mine.first) {
+                const bool masked = !(t0 >= mine.all_from && t0 + 64 <= mine.all_to && __all(there[0] && there[1]));
+                float score[2][16];
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    v16f dot[NB];
+#pragma unroll
+                    for (int m = 0; m < NB; ++m) dot[m] = v16f{0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
+#pragma unroll
+                    for (int j = 0; j < D / 16; ++j) {
+                        const bf16x8 k = *reinterpret_cast<const bf16x8 *>(tile + i * (D * 64) + j * 1024 + lane * 16);
+                        constexpr int kPer = D / 16 / NB;
+                        dot[j / kPer] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, q[j], dot[j / kPer], 0, 0, 0);
+                    }
+                    each_of(std::make_integer_sequence<int, 16>{}, [&](auto token) {
+                        constexpr int t = decltype(token)::value;
+                        float sum = dot[0][t] * of_lane<t>(ks[i][0]);
+#pragma unroll
+                        for (int m = 1; m < NB; ++m) sum += dot[m][t] * of_lane<t>(ks[i][m]);
+                        score[i][t] = sum;
+                    });
+                }
+                int from[2] = {0, 0};               // seen: 0 <= token - from < count, counted from this lane's first of a block
+                uint32_t count[2] = {16, 16};
+                if (masked) {
+                    stay_a_branch();
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const int first = t0 + 32 * i + 16 * half, lo = low + 1 - first, hi = high + 1 - first;
+                        from[i] = lo < 0 ? 0 : lo < 16 ? lo : 16;
+                        const int to = hi < 0 ? 0 : hi < 16 ? hi : 16;
+                        count[i] = there[i] && to > from[i] ? to - from[i] : 0;
+#pragma unroll
+                        for (int t = 0; t < 16; ++t) score[i][t] = (uint32_t)(t - from[i]) < count[i] ? score[i][t] : -__builtin_inff();
+                    }
+                }
+                float most = score[0][0];
+#pragma unroll
+                for (int t = 1; t < 16; ++t) most = __builtin_fmaxf(most, score[0][t]);
+#pragma unroll
+                for (int t = 0; t < 16; ++t) most = __builtin_fmaxf(most, score[1][t]);
+                most = halves_max(most);
+                if (__any(most > base + kSlack)) {
+                    const float now = __builtin_fmaxf(base, most);
+                    const float fade = now == -__builtin_inff() ? 1.0f : __builtin_amdgcn_exp2f(base - now);
+                    base = now;
+                    total *= fade;
+#pragma unroll
+                    for (int t = 0; t < D / 32; ++t) o[t] *= fade;
+                }
+                const float reference = base == -__builtin_inff() ? 0.0f : base;
+                float sums[2] = {0.0f, 0.0f};
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int t = 0; t < 16; ++t) {
+                        score[i][t] = __builtin_amdgcn_exp2f(score[i][t] - reference);
+                        sums[t % 2] += score[i][t];
+                    }
+                total += sums[0] + sums[1];
+                // block by block of the values' elements: one block's products are registers enough
+                each_of(std::make_integer_sequence<int, NB>{}, [&](auto number) {
+                    constexpr int m = decltype(number)::value, kPer = D / 32 / NB;
+                    bf16x8 p[4];
+                    each_of(std::make_integer_sequence<int, 2>{}, [&](auto block) {
+                        constexpr int i = decltype(block)::value;
+                        float e[16];
+                        each_of(std::make_integer_sequence<int, 16>{}, [&](auto token) {
+                            constexpr int t = decltype(token)::value;
+                            e[t] = score[i][t] * of_lane<t>(vs[i][m]);
+                        });
+                        if (masked) {           // what is not seen may have any scale
+                            asm volatile("" : "+v"(from[i]), "+v"(count[i]));       // compared again, not kept
+#pragma unroll
+                            for (int t = 0; t < 16; ++t) e[t] = (uint32_t)(t - from[i]) < count[i] ? e[t] : 0.0f;
+                        }
+#pragma unroll
+                        for (int j = 0; j < 2; ++j) {
+                            const u32x4 w = {narrow_bf16x2(e[8 * j], e[8 * j + 1]), narrow_bf16x2(e[8 * j + 2], e[8 * j + 3]),
+                                             narrow_bf16x2(e[8 * j + 4], e[8 * j + 5]), narrow_bf16x2(e[8 * j + 6], e[8 * j + 7])};
+                            p[2 * i + j] = __builtin_bit_cast(bf16x8, w);
+                        }
+                    });
+#pragma unroll
+                    for (int t = m * kPer; t < (m + 1) * kPer; ++t) {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const bf16x8 v = *reinterpret_cast<const bf16x8 *>(tile + RowsTile<D, NB>::kKeys + (t * 4 + i) * 1024 + lane * 16);
+                            o[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, p[i], o[t], 0, 0, 0);
+                        }
+                    }
+                });
+            }
+            cur ^= 1;
+            if (more) next.store(lds[cur], wave, lane);
+        }
+        total = halves_sum(total);
+        if (row0 + r >= rows) continue;
+        const int64_t place_out = place_of_row(call, q0, row);
+        if (call.splits == 1) {
+            const float inverse = ends_with(total);
+#pragma unroll
+            for (int t = 0; t < D / 32; ++t) {
+                const v16f done = o[t] * inverse;
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    *reinterpret_cast<u32x2 *>(call.out + place_out * D + t * 32 + 8 * j + 4 * half) =
+                        u32x2{narrow_bf16x2(done[4 * j], done[4 * j + 1]), narrow_bf16x2(done[4 * j + 2], done[4 * j + 3])};
+            }
+            if (call.lse && half == 0) call.lse[place_out] = log_sum(base, total);
+        } else {
+            const int64_t all = call.q_rows * call.q_heads, part = split * all + place_out;
+#pragma unroll
+            for (int t = 0; t < D / 32; ++t)
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    *reinterpret_cast<v4f *>(call.part + part * D + t * 32 + 8 * j + 4 * half) =
+                        v4f{o[t][4 * j], o[t][4 * j + 1], o[t][4 * j + 2], o[t][4 * j + 3]};
+            if (half == 0) reinterpret_cast<float2 *>(call.part + call.splits * all * D)[part] = float2{base, total};
         }
     }
 }
