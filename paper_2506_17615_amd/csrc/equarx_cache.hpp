@@ -602,27 +602,34 @@ typedef float v16f __attribute__((ext_vector_type(16)));
 
 template <int D, int NB>
 struct RowsTile {
-    static constexpr int kKeys = D * 128, kBytes = 2 * kKeys;       // of bf16, a tile's keys and then its values
+    // A tile in LDS: the keys of bf16, the values, then scales [keys, values][block][token] and whether each sixteen tokens have
+    // a page.
+    static constexpr int kKeys = D * 128, kScales = 2 * kKeys, kThere = kScales + 2 * NB * 256, kBytes = kThere + 16;
     static constexpr int kPieces = D / 64;                          // of 16 codes, a lane's keys and its values
+    static constexpr int kLoads = NB < 4 ? 1 : 2;                   // of scales, a lane's: 16 tokens' are 32 NB
 
-    // What a wave's lane has of a tile on the way: lane l 1/4 of the keys of token l / 4 of the wave's sixteen, and the sixteen values
-    // of elements l, l + 64, ...; and one token's scales, number l % 16 of either group of its half.
+    // What a wave's lane has of the wave's sixteen tokens on the way: lane l 1/4 of the keys of token l / 4, and the sixteen
+    // values of elements l, l + 64, ...; and scales of token l % 16.  They are in one page, found a tile ahead.
     u32x4 k[kPieces], v[kPieces];
-    float ks[2][NB], vs[2][NB];
-    bool there[2];
+    float scale[kLoads];
+    bool there;
+    int id;
 
-    __device__ __forceinline__ void load(const Pool &pool, const int32_t *table, int64_t width, int h, int t, int wave, int lane)
+    static __device__ __forceinline__ bool of_values(int i, int lane) { return NB == 1 ? lane >> 4 & 1 : NB == 2 ? lane >> 5 : i; }
+    static __device__ __forceinline__ int block_of(int lane) { return (lane >> 4) & (NB - 1); }
+
+    __device__ __forceinline__ void find(const Pool &pool, const int32_t *table, int64_t width, int t)
     {
-        auto page_at = [&](int token, bool &exists) {       // first slot of a token's page and this head; any one if there is none
-            const int p = page_of(pool, token), id = p < width ? table[p] : -1;
-            exists = id >= 0 && id < pool.pages;
-            return pool.place(exists ? id : 0, h) * pool.page;
-        };
-        auto in_page = [&](int token) { return token - page_of(pool, token) * pool.page; };
-        bool exists;
-        const int mine = t + 16 * wave;
-        const int64_t at = page_at(mine, exists) + in_page(mine);
-        const int8_t *const keys = pool.kc + (at + (lane >> 2)) * D + (lane & 3) * (D / 4);
+        const int p = page_of(pool, t);
+        id = p < width ? table[p] : -1;
+    }
+
+    __device__ __forceinline__ void load(const Pool &pool, int h, int t, int lane)
+    {
+        const int page = __builtin_amdgcn_readfirstlane(id), in = t - page_of(pool, t) * pool.page;
+        there = page >= 0 && page < pool.pages;
+        const int64_t first = pool.place(there ? page : 0, h) * pool.page, at = first + in;      // no page: any one's, not seen
+        const int8_t *const keys = pool.kc + at * D + (lane >> 2) * D + (lane & 3) * (D / 4);
         const int8_t *const values = pool.vc + at * D + lane * 16;
 #pragma unroll
         for (int i = 0; i < kPieces; ++i) {
@@ -630,20 +637,13 @@ struct RowsTile {
             v[i] = *reinterpret_cast<const u32x4 *>(values + 1024 * i);
         }
 #pragma unroll
-        for (int b = 0; b < 2; ++b) {
-            const int group = t + 32 * b + 16 * (lane >> 5);
-            const int64_t page = page_at(group, there[b]) * NB + in_page(group) + (lane & 15);
-#pragma unroll
-            for (int m = 0; m < NB; ++m) {
-                ks[b][m] = pool.ks[page + (int64_t)m * pool.page];
-                vs[b][m] = pool.vs[page + (int64_t)m * pool.page];
-            }
-        }
+        for (int i = 0; i < kLoads; ++i)
+            scale[i] = (of_values(i, lane) ? pool.vs : pool.ks)[first * NB + in + block_of(lane) * pool.page + (lane & 15)];
     }
 
-    // The codes, widened, into a buffer.  Keys: fragment (32 tokens, 16 elements) is 1 KB, lane after lane.  Values: fragment (32
-    // elements, 32 tokens, 16 of them) the same.
-    __device__ __forceinline__ void store(uint8_t *buffer, int wave, int lane) const
+    // The codes, widened, into a buffer; the keys' scales with the call's.  Keys: fragment (32 tokens, 16 elements) is 1 KB, lane
+    // after lane.  Values: fragment (32 elements, 32 tokens, 16 of them) the same.
+    __device__ __forceinline__ void store(uint8_t *buffer, float key_scale, int wave, int lane) const
     {
         const int token = lane >> 2, quarter = lane & 3, place = 8 * (token >> 2) + 4 * (wave & 1) + (token & 3);
 #pragma unroll
@@ -655,6 +655,13 @@ struct RowsTile {
             *reinterpret_cast<bf16x8 *>(values) = widen_codes(v[i].x, v[i].y);
             *reinterpret_cast<bf16x8 *>(values + 1024) = widen_codes(v[i].z, v[i].w);
         }
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            const bool values = of_values(i, lane);
+            reinterpret_cast<float *>(buffer + kScales)[(values * NB + block_of(lane)) * 64 + 16 * wave + (lane & 15)] =
+                values ? scale[i] : scale[i] * key_scale;
+        }
+        if (lane == 0) reinterpret_cast<int32_t *>(buffer + kThere)[wave] = there;
     }
 };
 
@@ -714,25 +721,29 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void attention_rows_kernel(c
         int cur = 0;
         if (span.first < span.last) {
             __syncthreads();                    // the last rows' tiles have been read
-            next.load(pool, table, seqs.width, h, span.first, wave, lane);
-            next.store(lds[0], wave, lane);
+            next.find(pool, table, seqs.width, span.first + 16 * wave);
+            next.load(pool, h, span.first + 16 * wave, lane);
+            next.store(lds[0], call.scale, wave, lane);
+            next.find(pool, table, seqs.width, span.first + 16 * wave + 64);
         }
         for (int t0 = span.first; t0 < span.last; t0 += 64) {
+            __syncthreads();                    // this tile is there for all, and the other buffer read by all
+            // past the end the next tile is one of another part, or of no page: loaded, not used
+            next.load(pool, h, t0 + 64 + 16 * wave, lane);
+            next.find(pool, table, seqs.width, t0 + 128 + 16 * wave);
+            const uint8_t *const tile = lds[cur];
             float ks[2][NB], vs[2][NB];
             bool there[2];
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-                there[i] = next.there[i];
+                const float *const scales = reinterpret_cast<const float *>(tile + RowsTile<D, NB>::kScales) + 32 * i + 16 * half + (lane & 15);
 #pragma unroll
                 for (int m = 0; m < NB; ++m) {
-                    ks[i][m] = next.ks[i][m] * call.scale;
-                    vs[i][m] = next.vs[i][m];
+                    ks[i][m] = scales[m * 64];
+                    vs[i][m] = scales[(NB + m) * 64];
                 }
+                there[i] = reinterpret_cast<const int32_t *>(tile + RowsTile<D, NB>::kThere)[2 * i + half];
             }
-            __syncthreads();                    // this tile is there for all, and the other buffer read by all
-            const bool more = t0 + 64 < span.last;
-            if (more) next.load(pool, table, seqs.width, h, t0 + 64, wave, lane);
-            const uint8_t *const tile = lds[cur];
             if (t0 < mine.last && t0 + 64 > mine.first) {
                 const bool masked = !(t0 >= mine.all_from && t0 + 64 <= mine.all_to && __all(there[0] && there[1]));
                 float score[2][16];
@@ -827,7 +838,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void attention_rows_kernel(c
                 });
             }
             cur ^= 1;
-            if (more) next.store(lds[cur], wave, lane);
+            if (t0 + 64 < span.last) next.store(lds[cur], call.scale, wave, lane);
         }
         total = halves_sum(total);
         if (row0 + r >= rows) continue;
