@@ -57,9 +57,10 @@ __device__ __forceinline__ u32x4 transpose4(uint32_t a, uint32_t b, uint32_t c, 
 }
 
 // ---------------------------------------------------------------- writing
-// A lane has eight elements of four consecutive tokens of the call, dim / 8 lanes a head.  Keys are written eight bytes at a
-// time; values four tokens together where the four lie in one group of sixteen slots from a multiple of four on, and byte
-// by byte where they do not.
+// A lane has eight elements of T = 4 consecutive tokens of the call, or of one; dim / 8 lanes a head.  Keys are written eight
+// bytes at a time.  An element's value codes of sixteen slots are sixteen bytes: where a wave's tokens are whole such groups
+// its quarters, four tokens each, exchange words and write them whole; else four tokens are written together where they lie
+// in one group from a multiple of four on, and byte by byte where they do not.
 
 // Q_B of eight bf16 numbers, a block being the 8 * G elements of G lanes; a NaN scale where the block is not finite.
 template <int G>
@@ -75,20 +76,30 @@ __device__ __forceinline__ u32x2 quantize_finite(const u32x4 &x, float &scale)
     return codes;
 }
 
-template <int D, int B>
+// Word i of quarter q of a wave to word q of quarter i.
+__device__ __forceinline__ u32x4 exchange_quarters(const u32x4 &w)
+{
+    const auto a = __builtin_amdgcn_permlane32_swap(w.x, w.z, false, false), b = __builtin_amdgcn_permlane32_swap(w.y, w.w, false, false);
+    const auto lo = __builtin_amdgcn_permlane16_swap(a[0], b[0], false, false), hi = __builtin_amdgcn_permlane16_swap(a[1], b[1], false, false);
+    return u32x4{lo[0], lo[1], hi[0], hi[1]};
+}
+
+template <int D, int B, int T>
 __global__ __launch_bounds__(256) void write_kernel(Global<const uint16_t> k, Global<const uint16_t> v,
                                                     Global<const int64_t> slots, int64_t k_row, int64_t v_row,
                                                     int32_t tokens, int64_t k_head, int64_t v_head, const Pool pool)
 {
     constexpr int kLanes = D / 8, kBlocks = D / B, G = B / 8;
     const int h = blockIdx.y;
-    const int t0 = (blockIdx.x * (256 / kLanes) + threadIdx.x / kLanes) * 4;
+    int part = threadIdx.x / kLanes;
+    if (T == 4 && D == 64) part = (part & ~7) + (part >> 1 & 3) + (part & 1) * 4;       // a quarter's tokens: of two groups
+    const int t0 = (blockIdx.x * (256 / kLanes) + part) * T;
     const int d = threadIdx.x % kLanes * 8;
     const int64_t space = pool.pages * pool.page;
-    u32x4 kx[4], vx[4];
-    int64_t slot[4];
+    u32x4 kx[T], vx[T];
+    int64_t slot[T];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < T; ++i) {
         const int t = t0 + i < tokens ? t0 + i : tokens - 1;
         slot[i] = t0 + i < tokens ? slots[t] : -1;
         if (slot[i] >= space) slot[i] = -1;
@@ -96,11 +107,11 @@ __global__ __launch_bounds__(256) void write_kernel(Global<const uint16_t> k, Gl
         vx[i] = *reinterpret_cast<const u32x4 *>(v + t * v_row + h * v_head + d);
     }
     loads_first();
-    u32x2 vw[4];
-    int64_t at[4];
-    int in_page[4];
+    u32x2 vw[T];
+    int64_t at[T];
+    int in_page[T];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < T; ++i) {
         float ks, vs;
         const u32x2 kw = quantize_finite<G>(kx[i], ks);
         vw[i] = quantize_finite<G>(vx[i], vs);
@@ -116,20 +127,35 @@ __global__ __launch_bounds__(256) void write_kernel(Global<const uint16_t> k, Gl
             }
         }
     }
-    const bool together = slot[0] >= 0 && (slot[0] & 3) == 0 && slot[1] == slot[0] + 1 && slot[2] == slot[0] + 2 &&
-                          slot[3] == slot[0] + 3;
-    if (together) {
-        int8_t *const to = pool.vc + at[0] * pool.page * D + (int64_t)(in_page[0] & ~15) * D + d * 16 + (in_page[0] & 15);
+    if constexpr (T == 4) {
+        const bool together = slot[0] >= 0 && (slot[0] & 3) == 0 && slot[1] == slot[0] + 1 && slot[2] == slot[0] + 2 &&
+                              slot[3] == slot[0] + 3;
+        int8_t *const group = pool.vc + at[0] * pool.page * D + (int64_t)(in_page[0] & ~15) * D;
+        u32x4 w[2];
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            const u32x4 w = transpose4(vw[0][j], vw[1][j], vw[2][j], vw[3][j]);
+        for (int j = 0; j < 2; ++j) w[j] = transpose4(vw[0][j], vw[1][j], vw[2][j], vw[3][j]);
+        if constexpr (D <= 128) {
+            // this lane's tokens follow those of the quarters before it, from a group's first on
+            const int quarter = threadIdx.x >> 4 & 3;
+            const int64_t first = __shfl(slot[0], threadIdx.x & 15);
+            if (__all(together && (first & 15) == 0 && slot[0] == first + 4 * quarter)) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) *reinterpret_cast<uint32_t *>(to + (4 * j + i) * 16) = w[i];
+                for (int j = 0; j < 2; ++j)
+                    *reinterpret_cast<u32x4 *>(group + (d + 4 * j + quarter) * 16) = exchange_quarters(w[j]);
+                return;
+            }
         }
-        return;
+        if (together) {
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    *reinterpret_cast<uint32_t *>(group + d * 16 + (in_page[0] & 15) + (4 * j + i) * 16) = w[j][i];
+            return;
+        }
     }
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < T; ++i) {
         if (slot[i] < 0) continue;
         int8_t *const to = pool.vc + at[i] * pool.page * D + (int64_t)(in_page[i] & ~15) * D + d * 16 + (in_page[i] & 15);
 #pragma unroll
@@ -591,7 +617,7 @@ __device__ __forceinline__ void part_row(const Rows<D, NB, R> &mine, int n, floa
 // Here the matrix unit and what comes between its instructions are the bound, so codes are widened once for a workgroup: wave w takes
 // the keys and values of sixteen tokens of 64, as bf16 they wait in LDS (two buffers: the next tile's are written, and the one
 // after that asked for, while this one's are used) in the order in which the lanes of a 32x32x16 instruction read them.
-// (2 x 2048 rows of 32 heads at the end of 8192 tokens, blocks of 64: every wave widening all for itself, 16x16x32, 1055 us; this 663.)
+// (2 x 2048 rows of 32 heads at the end of 8192 tokens, blocks of 64: every wave widening all for itself, 16x16x32, 1055 us; this 575.)
 //
 // As above with 32 for 16: the tokens of an instruction's rows are chosen so that S^T leaves lane (row c = l % 32, half h = l / 32)
 // with 16 consecutive tokens 16 h .. of the 32, row 8 j + 4 h + i being token 16 h + 4 j + i, and O^T += V^T P^T takes eight of
