@@ -100,13 +100,15 @@ struct AttentionPlan {
     int32_t splits, chunk;      // kRows
 };
 
-AttentionPlan plan_attention(int32_t heads, int32_t q_heads, int32_t sequences, int64_t max_queries, int64_t max_length)
+AttentionPlan plan_attention(int32_t heads, int32_t dim, int32_t q_heads, int32_t sequences, int64_t max_queries, int64_t max_length)
 {
     AttentionPlan p{};
     const int64_t rows = max_queries * (q_heads / heads);
     p.rows16 = rows <= 16 ? 1 : 2;
     p.splits = 1;
-    if (rows <= 32) {
+    // A wave holds 32 rows of heads up to 128; of 256 their sums spill: 24 rows of 8 sequences of up to 4096 tokens, blocks of
+    // 64: 78 us, and 62 with many rows' kernel.
+    if (rows <= (dim <= 128 ? 32 : 16)) {
         p.row_tiles = 1;
         p.form = sequences > kMostShared || max_length <= 512 ? AttentionForm::kWhole : AttentionForm::kShared;
         return p;
@@ -114,11 +116,14 @@ AttentionPlan plan_attention(int32_t heads, int32_t q_heads, int32_t sequences, 
     p.form = AttentionForm::kRows;
     p.row_tiles = (rows + 127) / 128;
     const int64_t workgroups = p.row_tiles * heads * sequences;
-    // enough workgroups for two a CU, none with fewer than four tiles of tokens
-    int64_t splits = (512 + workgroups - 1) / workgroups;
+    // as many workgroups as the CUs hold at once, two each and one with heads of 256, none with fewer than four tiles of tokens:
+    // 5 queries of 8 heads after 131072 tokens 27 us in 256 splits, 65 in 64; twice as many workgroups, 202 for 192 us (512
+    // queries of 32 heads after 16384)
+    const int64_t held = dim <= 128 ? 512 : 256;
+    int64_t splits = (held + workgroups - 1) / workgroups;
     const int64_t most = (max_length + 255) / 256;
     if (splits > most) splits = most;
-    if (splits > 64) splits = 64;
+    if (splits > 256) splits = 256;
     if (splits * heads > kGridDim) splits = kGridDim / heads;
     if (splits < 1) splits = 1;
     p.chunk = (int32_t)(((max_length + splits - 1) / splits + 63) / 64 * 64);
@@ -150,12 +155,15 @@ void launch_attention(const AttentionPlan &plan, const AttentionCall &call, cons
         }
     };
     if (plan.form == AttentionForm::kShared) {
-        if (plan.rows16 == 1) {
-            share(std::integral_constant<int, 1>{});
-        } else {
-            share(std::integral_constant<int, 2>{});
+        if (plan.rows16 == 1) share(std::integral_constant<int, 1>{});
+        if constexpr (D <= 128) {
+            if (plan.rows16 == 2) share(std::integral_constant<int, 2>{});
         }
         return;
+    }
+    auto tokens_kernel = attention_tokens_kernel<D, NB, 1>;
+    if constexpr (D <= 128) {
+        if (plan.rows16 == 2) tokens_kernel = attention_tokens_kernel<D, NB, 2>;
     }
     for (int32_t at = 0; at < call.sequences; at += kGridDim) {
         const int32_t count = call.sequences - at < kGridDim ? call.sequences - at : kGridDim;
@@ -166,8 +174,7 @@ void launch_attention(const AttentionPlan &plan, const AttentionCall &call, cons
             ctx.launch3d(attention_rows_kernel<D, NB>, (unsigned)tiles, (unsigned)(pool.heads * plan.splits), (unsigned)count, 256,
                          part, some, pool);
         } else {
-            ctx.launch3d(plan.rows16 == 1 ? attention_tokens_kernel<D, NB, 1> : attention_tokens_kernel<D, NB, 2>,
-                         (unsigned)tiles, (unsigned)pool.heads, (unsigned)count, 256, part, some, pool);
+            ctx.launch3d(tokens_kernel, (unsigned)tiles, (unsigned)pool.heads, (unsigned)count, 256, part, some, pool);
         }
     }
     if (plan.splits > 8) {
@@ -218,7 +225,7 @@ int equarx_cache_write(const equarx_cache *cache, const void *k_bf16, int64_t k_
                          static_cast<const uint16_t *>(k_bf16), static_cast<const uint16_t *>(v_bf16), slots, k_row_stride,
                          v_row_stride, (int32_t)tokens, k_head_stride, v_head_stride, pool_of(*cache));
         };
-        // Four tokens a lane once that gives every CU a workgroup: 16384 tokens of 8 heads of 128 in 20 us, one a lane 44; 64
+        // Four tokens a lane once that gives every CU a workgroup: 16384 tokens of 8 heads of 128 in 20 us, one a lane 43; 64
         // tokens in no order, as a decode step has them, one a lane 3.8 us, four 8 to 10.
         constexpr int kTokens = 256 / (D / 8) * 4;
         if ((tokens + kTokens - 1) / kTokens * cache->heads < 256)
@@ -268,7 +275,7 @@ size_t equarx_cache_attention_workspace_bytes(int32_t heads, int32_t dim, int64_
                                               int32_t max_queries, int64_t max_length)
 {
     if (check_heads(heads, q_rows, q_heads, dim, sequences, max_queries, max_length) != EQUARX_OK || sequences == 0) return 0;
-    return attention_workspace(plan_attention(heads, q_heads, sequences, max_queries, max_length), dim, q_rows, q_heads);
+    return attention_workspace(plan_attention(heads, dim, q_heads, sequences, max_queries, max_length), dim, q_rows, q_heads);
 }
 
 int equarx_cache_attention(const equarx_cache *cache, const void *q_bf16, int64_t q_rows, int32_t q_heads,
@@ -292,7 +299,7 @@ int equarx_cache_attention(const equarx_cache *cache, const void *q_bf16, int64_
     if (misaligned(q_starts, sizeof(int32_t)) || misaligned(out_bf16, kAlign) || misaligned(lse, kAlign) ||
         misaligned(workspace, kWorkspaceAlign))
         return EQUARX_MISALIGNED;
-    const AttentionPlan plan = plan_attention(cache->heads, q_heads, sequences, max_queries, max_length);
+    const AttentionPlan plan = plan_attention(cache->heads, cache->dim, q_heads, sequences, max_queries, max_length);
     const size_t need = attention_workspace(plan, cache->dim, q_rows, q_heads);
     if (need > 0 && !workspace) return EQUARX_NULL_POINTER;
     if (workspace_bytes < need) return EQUARX_WORKSPACE_TOO_SMALL;

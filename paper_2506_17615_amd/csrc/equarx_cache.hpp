@@ -770,7 +770,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void attention_rows_kernel(c
                 }
                 there[i] = reinterpret_cast<const int32_t *>(tile + RowsTile<D, NB>::kThere)[2 * i + half];
             }
-            if (t0 < mine.last && t0 + 64 > mine.first) {
+            if (row0 < rows && t0 < mine.last && t0 + 64 > mine.first) {
                 const bool masked = !(t0 >= mine.all_from && t0 + 64 <= mine.all_to && __all(there[0] && there[1]));
                 float score[2][16];
 #pragma unroll
