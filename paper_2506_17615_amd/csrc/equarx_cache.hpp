@@ -232,9 +232,10 @@ __global__ __launch_bounds__(256) void read_kernel(Global<uint16_t> k_out, Globa
 //            from 0 to 3: after the four, the tokens 16 g .. 16 g + 15 in order.
 //   sums     O^T += V^T P^T takes a lane's P as it is: quarter g has 8 consecutive tokens of its 16 per instruction, and the 16
 //            codes of one element of v for those tokens are 16 consecutive bytes of the cache.
-// A code is exact in bf16; scales join in fp32, the keys' on the scores, the values' on the probabilities before these are
-// rounded to bf16 (up to 2^-8 of each summand, as any attention that feeds matrix instructions has it).  Running maximum and sum per
-// row; the sum stays split over the quarters until the end.
+// A code is exact in bf16; scales join in fp32, the keys' on the scores, the values' on the probabilities.  These products
+// go to the matrix instructions as sums of two bf16: rounded to one, 2^-9 of each, their error is as large as that of the result's
+// own rounding, and f16 has not the range for the small ones.  Running maximum and sum per row; the sum stays split over the
+// quarters until the end.
 
 struct AttentionCall {
     const uint16_t *q;
@@ -283,6 +284,20 @@ __device__ __forceinline__ bf16x8 widen_codes(uint32_t a, uint32_t b)
     widen_i8x8(u32x2{a, b}, f);
     const u32x4 w = {narrow_bf16x2(f[0], f[1]), narrow_bf16x2(f[2], f[3]), narrow_bf16x2(f[4], f[5]), narrow_bf16x2(f[6], f[7])};
     return __builtin_bit_cast(bf16x8, w);
+}
+
+// Eight numbers as the sums of two bf16, the first their upper halves: to 2^-16 of each.
+__device__ __forceinline__ void split_in_two(const float *e, bf16x8 &upper, bf16x8 &rest)
+{
+    u32x4 u, r;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t a = __float_as_uint(e[2 * i]), b = __float_as_uint(e[2 * i + 1]);
+        u[i] = __builtin_amdgcn_perm(b, a, 0x07060302u);
+        r[i] = narrow_bf16x2(e[2 * i] - __uint_as_float(a & 0xffff0000u), e[2 * i + 1] - __uint_as_float(b & 0xffff0000u));
+    }
+    upper = __builtin_bit_cast(bf16x8, u);
+    rest = __builtin_bit_cast(bf16x8, r);
 }
 
 // What a wave has of 64 tokens, each part asked for as soon as its registers are free.  A lane's scales are those of one token, its
@@ -397,7 +412,7 @@ struct Rows {
     // some token.
     __device__ __forceinline__ void add(const Tile<D, NB> &tile, float (&score)[R][16], int first, bool there, bool masked)
     {
-        bf16x8 p[R][NB][2];
+        bf16x8 p[R][NB][2], rest[R][NB][2];
 #pragma unroll
         for (int n = 0; n < R; ++n) {
             int from = 0;               // seen: 0 <= token - from < count, counted from this lane's first
@@ -444,11 +459,7 @@ struct Rows {
                     for (int t = 0; t < 16; ++t) e[t] = (uint32_t)(t - from) < count ? e[t] : 0.0f;
                 }
 #pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    const u32x4 w = {narrow_bf16x2(e[8 * j], e[8 * j + 1]), narrow_bf16x2(e[8 * j + 2], e[8 * j + 3]),
-                                     narrow_bf16x2(e[8 * j + 4], e[8 * j + 5]), narrow_bf16x2(e[8 * j + 6], e[8 * j + 7])};
-                    p[n][m][j] = __builtin_bit_cast(bf16x8, w);
-                }
+                for (int j = 0; j < 2; ++j) split_in_two(e + 8 * j, p[n][m][j], rest[n][m][j]);
             });
         }
         // codes are widened as they are used: early, they would be twice the registers
@@ -461,6 +472,8 @@ struct Rows {
             for (int n = 0; n < R; ++n) {
                 o[n][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a0, p[n][t / kPer][0], o[n][t], 0, 0, 0);
                 o[n][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a1, p[n][t / kPer][1], o[n][t], 0, 0, 0);
+                o[n][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a0, rest[n][t / kPer][0], o[n][t], 0, 0, 0);
+                o[n][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a1, rest[n][t / kPer][1], o[n][t], 0, 0, 0);
             }
         }
         __builtin_amdgcn_sched_barrier(0);
@@ -617,7 +630,8 @@ __device__ __forceinline__ void part_row(const Rows<D, NB, R> &mine, int n, floa
 // Here the matrix unit and what comes between its instructions are the bound, so codes are widened once for a workgroup: wave w takes
 // the keys and values of sixteen tokens of 64, as bf16 they wait in LDS (two buffers: the next tile's are written, and the one
 // after that asked for, while this one's are used) in the order in which the lanes of a 32x32x16 instruction read them.
-// (2 x 2048 rows of 32 heads at the end of 8192 tokens, blocks of 64: every wave widening all for itself, 16x16x32, 1055 us; this 575.)
+// (2 x 2048 rows of 32 heads at the end of 8192 tokens, blocks of 64: every wave widening all for itself, 16x16x32, 1055 us;
+// this 575, and 720 with probabilities as two bf16.)
 //
 // As above with 32 for 16: the tokens of an instruction's rows are chosen so that S^T leaves lane (row c = l % 32, half h = l / 32)
 // with 16 consecutive tokens 16 h .. of the 32, row 8 j + 4 h + i being token 16 h + 4 j + i, and O^T += V^T P^T takes eight of
@@ -779,10 +793,11 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void attention_rows_kernel(c
 #pragma unroll
                     for (int m = 0; m < NB; ++m) dot[m] = v16f{0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
 #pragma unroll
-                    for (int j = 0; j < D / 16; ++j) {
-                        const bf16x8 k = *reinterpret_cast<const bf16x8 *>(tile + i * (D * 64) + j * 1024 + lane * 16);
+                    for (int n = 0; n < D / 16; ++n) {
                         constexpr int kPer = D / 16 / NB;
-                        dot[j / kPer] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, q[j], dot[j / kPer], 0, 0, 0);
+                        const int m = n % NB, j = m * kPer + n / NB;
+                        const bf16x8 k = *reinterpret_cast<const bf16x8 *>(tile + i * (D * 64) + j * 1024 + lane * 16);
+                        dot[m] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, q[j], dot[m], 0, 0, 0);
                     }
                     each_of(std::make_integer_sequence<int, 16>{}, [&](auto token) {
                         constexpr int t = decltype(token)::value;
@@ -833,7 +848,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void attention_rows_kernel(c
                 // block by block of the values' elements: one block's products are registers enough
                 each_of(std::make_integer_sequence<int, NB>{}, [&](auto number) {
                     constexpr int m = decltype(number)::value, kPer = D / 32 / NB;
-                    bf16x8 p[4];
+                    bf16x8 p[4], rest[4];
                     each_of(std::make_integer_sequence<int, 2>{}, [&](auto block) {
                         constexpr int i = decltype(block)::value;
                         float e[16];
@@ -847,19 +862,20 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void attention_rows_kernel(c
                             for (int t = 0; t < 16; ++t) e[t] = (uint32_t)(t - from[i]) < count[i] ? e[t] : 0.0f;
                         }
 #pragma unroll
-                        for (int j = 0; j < 2; ++j) {
-                            const u32x4 w = {narrow_bf16x2(e[8 * j], e[8 * j + 1]), narrow_bf16x2(e[8 * j + 2], e[8 * j + 3]),
-                                             narrow_bf16x2(e[8 * j + 4], e[8 * j + 5]), narrow_bf16x2(e[8 * j + 6], e[8 * j + 7])};
-                            p[2 * i + j] = __builtin_bit_cast(bf16x8, w);
-                        }
+                        for (int j = 0; j < 2; ++j) split_in_two(e + 8 * j, p[2 * i + j], rest[2 * i + j]);
                     });
+                    // no product after one on the same sums, where there are others
 #pragma unroll
-                    for (int t = m * kPer; t < (m + 1) * kPer; ++t) {
+                    for (int i = 0; i < 4; ++i) {
+                        bf16x8 v[kPer];
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const bf16x8 v = *reinterpret_cast<const bf16x8 *>(tile + RowsTile<D, NB>::kKeys + (t * 4 + i) * 1024 + lane * 16);
-                            o[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, p[i], o[t], 0, 0, 0);
+                        for (int t = 0; t < kPer; ++t) {
+                            v[t] = *reinterpret_cast<const bf16x8 *>(tile + RowsTile<D, NB>::kKeys + ((m * kPer + t) * 4 + i) * 1024 + lane * 16);
+                            o[m * kPer + t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v[t], p[i], o[m * kPer + t], 0, 0, 0);
                         }
+#pragma unroll
+                        for (int t = 0; t < kPer; ++t)
+                            o[m * kPer + t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v[t], rest[i], o[m * kPer + t], 0, 0, 0);
                     }
                 });
             }
