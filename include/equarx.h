@@ -417,9 +417,10 @@ int equarx_mx4_dequantize(const uint8_t *codes, const uint8_t *scales, int64_t r
  * equarx_mx4_linear takes x as bf16 [M][K] (row m at x + m * x_stride) and
  * quantizes it as equarx_mx4_quantize does: same bits as the two calls.
  *
- *   workspace   device, equarx_mx4_workspace_bytes(M, N, K) bytes for either
- *               call, 256-byte aligned (may be NULL where that is 0); nothing
- *               in it needs clearing.
+ *   workspace   of equarx_mx4_linear: device, equarx_mx4_workspace_bytes(M, N, K)
+ *               bytes, 256-byte aligned (may be NULL where that is 0); x's packed
+ *               rows, and nothing in it needs clearing.  equarx_mx4_product takes
+ *               the same arguments and does not use them.
  * No output may overlap another buffer of the call (EQUARX_BAD_SHAPE).
  */
 int equarx_mx4_product(const uint8_t *x_codes, const uint8_t *x_scales, const uint8_t *w_codes, const uint8_t *w_scales,
@@ -498,7 +499,7 @@ int equarx_cache_read(const equarx_cache *cache, const int32_t *page_table, int6
  *   out = sum_t exp(s_t - lse) v_t
  * over the tokens t that the row sees, with k and v the codes times their scales,
  * unrounded.  Sums and statistics are fp32; the products exp(..) * v scale
- * are rounded to bf16 before they meet the codes.
+ * meet the codes as sums of two bf16, to 2^-16 of each.
  *
  *   flags    EQUARX_CAUSAL: query i of n sees token t of L if t <= L - n + i
  *            (its own token is in the cache already); without it, all.
@@ -510,6 +511,8 @@ int equarx_cache_read(const equarx_cache *cache, const int32_t *page_table, int6
  *   max_queries, max_length   the longest query run and sequence, as far as
  *            the host knows (>= 1): they size the launch and choose how a long context
  *            is split, and hence the order of the sums; larger actual values cost time, not correctness.
+ *   q_rows * q_heads is at most 2^31 - 128 (EQUARX_BAD_SHAPE); a sequence's tokens from 2^31 - 65536
+ *            on are not seen.
  *   workspace  equarx_cache_attention_workspace_bytes(...) bytes, 256-byte
  *            aligned (may be NULL where that is 0); nothing in it needs clearing.
  */

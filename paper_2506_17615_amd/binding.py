@@ -652,6 +652,8 @@ def alloc_cache(pages: int, heads: int, page: int, dim: int, block: int, device=
 
 def _need_cache(cache):
     """The C structure of a Cache whose tensors have the shapes they should have."""
+    if not isinstance(cache, (tuple, list)) or len(cache) != 4 or not all(isinstance(t, torch.Tensor) for t in cache):
+        raise ValueError("cache: need the four tensors of a Cache")
     kc, ks, vc, vs = cache
     good = kc.dim() == 4 and ks.dim() == 4 and ks.shape[2] > 0 and kc.shape[3] % ks.shape[2] == 0
     if good:

@@ -190,7 +190,7 @@ int check_heads(int32_t heads, int64_t q_rows, int32_t q_heads, int32_t dim, int
     if (heads < 1 || heads > kGridDim || q_heads < 1 || q_heads % heads != 0) return EQUARX_BAD_SHAPE;
     if (q_rows < 0 || sequences < 0 || max_queries < 1 || max_length < 1 || max_length > INT32_MAX - 63) return EQUARX_BAD_SHAPE;
     if (dim != 64 && dim != 128 && dim != 256) return EQUARX_BAD_SHAPE;
-    if (q_rows > INT32_MAX / q_heads) return EQUARX_BAD_SHAPE;
+    if (q_rows > (INT32_MAX - 127) / q_heads) return EQUARX_BAD_SHAPE;      // a kernel rounds up to its 128 rows
     return EQUARX_OK;
 }
 

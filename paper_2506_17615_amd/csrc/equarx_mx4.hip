@@ -141,15 +141,15 @@ void launch_product(const Product &p, LaunchCtx &ctx)
     }
 }
 
-// The parts of a workspace: x's codes and scales where the call quantizes x itself.
+// The workspace of a linear call: x's codes, and from `scales` on its scales; none where the product's kernel packs x.
 struct Workspace {
-    size_t codes, scales, bytes;
+    size_t scales, bytes;
 };
 
 Workspace plan_workspace(int64_t M, int64_t K)
 {
-    Workspace w;
-    w.codes = 0;
+    Workspace w{};
+    if (K == 0 || packs_itself(M, K)) return w;
     w.scales = round_up(code_bytes(M, K), kWorkspaceAlign);
     w.bytes = w.scales + round_up(scale_bytes(M, K), kWorkspaceAlign);
     return w;
@@ -219,8 +219,8 @@ size_t equarx_mx4_workspace_bytes(int64_t M, int64_t N, int64_t K)
 }
 
 int equarx_mx4_product(const uint8_t *x_codes, const uint8_t *x_scales, const uint8_t *w_codes, const uint8_t *w_scales,
-                       int64_t M, int64_t N, int64_t K, void *out_bf16, int64_t out_stride, void *workspace,
-                       size_t workspace_bytes, void *stream)
+                       int64_t M, int64_t N, int64_t K, void *out_bf16, int64_t out_stride, void * /*workspace*/,
+                       size_t /*workspace_bytes*/, void *stream)
 {
     LaunchCtx ctx(stream);
     if (int st = check_product(M, N, K, out_stride)) return st;
@@ -228,18 +228,14 @@ int equarx_mx4_product(const uint8_t *x_codes, const uint8_t *x_scales, const ui
     if (!out_bf16) return EQUARX_NULL_POINTER;
     if (K > 0 && (!x_codes || !x_scales || !w_codes || !w_scales)) return EQUARX_NULL_POINTER;
     if (misaligned(out_bf16, kAlign) || misaligned(x_codes, kAlign) || misaligned(x_scales, kAlign) ||
-        misaligned(w_codes, kAlign) || misaligned(w_scales, kAlign) || misaligned(workspace, kWorkspaceAlign))
+        misaligned(w_codes, kAlign) || misaligned(w_scales, kAlign))
         return EQUARX_MISALIGNED;
-    const size_t need = K > 0 ? plan_workspace(M, K).bytes : 0;
-    if (need > 0 && !workspace) return EQUARX_NULL_POINTER;
-    if (workspace_bytes < need) return EQUARX_WORKSPACE_TOO_SMALL;
     Aliasing mem;
     mem.reads(x_codes, code_bytes(M, K));
     mem.reads(x_scales, scale_bytes(M, K));
     mem.reads(w_codes, code_bytes(N, K));
     mem.reads(w_scales, scale_bytes(N, K));
     mem.writes(out_bf16, row_bytes(M, N, out_stride));
-    mem.writes(workspace, need);
     if (int st = mem.check()) return st;
     launch_product({x_codes, x_scales, w_codes, w_scales, static_cast<uint16_t *>(out_bf16), M, N, K, out_stride, 0}, ctx);
     return ctx.status();
@@ -259,7 +255,7 @@ int equarx_mx4_linear(const void *x_bf16, int64_t x_stride, const uint8_t *w_cod
         misaligned(w_scales, kAlign) || misaligned(workspace, kWorkspaceAlign))
         return EQUARX_MISALIGNED;
     const Workspace plan = plan_workspace(M, K);
-    const size_t need = K > 0 ? plan.bytes : 0;
+    const size_t need = plan.bytes;
     if (need > 0 && !workspace) return EQUARX_NULL_POINTER;
     if (workspace_bytes < need) return EQUARX_WORKSPACE_TOO_SMALL;
     Aliasing mem;
