@@ -60,7 +60,8 @@ __device__ __forceinline__ u32x4 transpose4(uint32_t a, uint32_t b, uint32_t c, 
 // A lane has eight elements of T = 4 consecutive tokens of the call, or of one; dim / 8 lanes a head.  Keys are written eight
 // bytes at a time.  An element's value codes of sixteen slots are sixteen bytes: where a wave's tokens are whole such groups
 // its quarters, four tokens each, exchange words and write them whole; else four tokens are written together where they lie
-// in one group from a multiple of four on, and byte by byte where they do not.
+// in one group from a multiple of four on, and byte by byte where they do not.  Memory is the bound: 16384 tokens of 8 heads of 128
+// in 19.8 us (5.2 TB/s), 23.0 without the exchange.
 
 // Q_B of eight bf16 numbers, a block being the 8 * G elements of G lanes; a NaN scale where the block is not finite.
 template <int G>
@@ -164,7 +165,8 @@ __global__ __launch_bounds__(256) void write_kernel(Global<const uint16_t> k, Gl
 }
 
 // ---------------------------------------------------------------- reading back
-// A lane has eight elements of four tokens from a multiple of four on, dim / 8 lanes a head.
+// A lane has eight elements of four tokens from a multiple of four on, dim / 8 lanes a head.  Memory is the bound: the tokens
+// above back in 19.0 us (5.4 TB/s).
 
 __device__ __forceinline__ u32x4 read_back(const u32x2 &codes, float scale)
 {
@@ -250,6 +252,7 @@ struct AttentionCall {
     int32_t causal, window;
     int32_t chunk, splits;      // waves on rows: a split's tokens, a multiple of 64
     int32_t sequences;
+    int32_t tiles_last;         // waves on rows: the grid's third dimension is tiles of rows, not sequences
 };
 
 __device__ __forceinline__ int within(int v, int64_t most) { return v < 0 ? 0 : v < most ? v : (int)most; }
@@ -631,12 +634,14 @@ __device__ __forceinline__ void part_row(const Rows<D, NB, R> &mine, int n, floa
 // the keys and values of sixteen tokens of 64, as bf16 they wait in LDS (two buffers: the next tile's are written, and the one
 // after that asked for, while this one's are used) in the order in which the lanes of a 32x32x16 instruction read them.
 // (2 x 2048 rows of 32 heads at the end of 8192 tokens, blocks of 64: every wave widening all for itself, 16x16x32, 1055 us;
-// this 575, and 720 with probabilities as two bf16.)
+// this 629, 0.60 PFLOP/s, of which 130 are for probabilities as two bf16.  Two thirds of the cycles issue vector instructions -- 620
+// a wave and tile, the exponentials four times as long as others --, a third have a matrix instruction under way, and few both.)
 //
 // As above with 32 for 16: the tokens of an instruction's rows are chosen so that S^T leaves lane (row c = l % 32, half h = l / 32)
 // with 16 consecutive tokens 16 h .. of the 32, row 8 j + 4 h + i being token 16 h + 4 j + i, and O^T += V^T P^T takes eight of
 // these as they are.
-// Grid: tiles of rows, heads x splits, sequences.  Parts: [splits][q_rows][q_heads].
+// Grid: heads x splits, then sequences and tiles of rows in either order: tiles of one head, which read the same tokens, are on one
+// XCD as a rule.  Parts: [splits][q_rows][q_heads].
 
 typedef float v16f __attribute__((ext_vector_type(16)));
 
@@ -724,7 +729,8 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void attention_rows_kernel(c
     __shared__ __align__(16) uint8_t lds[2][RowsTile<D, NB>::kBytes];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int r = lane & 31, half = lane >> 5;
-    const int b = blockIdx.z, split = blockIdx.y / (uint32_t)pool.heads, h = blockIdx.y - split * pool.heads;
+    const int b = call.tiles_last ? blockIdx.y : blockIdx.z, split = blockIdx.x / (uint32_t)pool.heads, h = blockIdx.x - split * pool.heads;
+    const int first_turn = call.tiles_last ? blockIdx.z : blockIdx.y, turns = call.tiles_last ? gridDim.z : gridDim.y;
     const int q0 = within(call.q_starts[b], call.q_rows), queries = within(call.q_starts[b + 1], call.q_rows) - q0;
     const int length = seqs.length(b, pool.page);
     const int32_t *const table = seqs.table + b * seqs.width;
@@ -734,7 +740,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void attention_rows_kernel(c
     const int64_t split_from = (int64_t)split * chunk;
 
     const int rows = queries * call.group, row_tiles = (rows + kRows - 1) / kRows;
-    for (int turn = blockIdx.x; turn < row_tiles; turn += gridDim.x) {
+    for (int turn = first_turn; turn < row_tiles; turn += turns) {
         const int tile_row = (row_tiles - 1 - turn) * kRows;        // with causal rows the last ones are the longest: first
         const int row0 = tile_row + wave * 32;
         const Row row(call, queries, h, row0 + r);

@@ -285,3 +285,10 @@ def test_written_then_attended_on_another_stream_and_in_a_graph():
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(out, want)
+
+
+def test_more_workgroups_than_are_held_at_once():
+    """70 sequences of 8 heads: launched sequence after sequence."""
+    lengths = [35 + 11 * (i % 9) for i in range(70)]
+    r, table = _filled(31, lengths, 16, 8, 64, 64)
+    _attend(r, table, lengths, [33 + i % 3 for i in range(70)], 1)
