@@ -504,7 +504,7 @@ int equarx_cache_read(const equarx_cache *cache, const int32_t *page_table, int6
  *   flags    EQUARX_CAUSAL: query i of n sees token t of L if t <= L - n + i
  *            (its own token is in the cache already); without it, all.
  *   window   0, or with EQUARX_CAUSAL also t > L - n + i - window.
- * A row that sees nothing has out 0 and lse -inf.
+ * A row that sees nothing has out 0 and lse -inf; one that sees tokens, all with the score -inf, has out NaN and lse -inf.
  *
  *   out [q_rows][q_heads][dim] bf16, lse fp32 [q_rows][q_heads] or NULL; rows of
  *   no sequence are not written.

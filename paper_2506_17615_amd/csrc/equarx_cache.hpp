@@ -257,9 +257,12 @@ struct AttentionCall {
 
 __device__ __forceinline__ int within(int v, int64_t most) { return v < 0 ? 0 : v < most ? v : (int)most; }
 
-// The factor that ends a row: 1 / its sum, 0 for a row that saw nothing (whose sum is 0, where any token seen adds up to 1
-// at least, or to NaN), and its log sum of exponentials.
-__device__ __forceinline__ float ends_with(float total) { return total == 0.0f ? 0.0f : 1.0f / total; }
+// A row's maximum is -inf until it sees a token, and kLeast at least from then on: so a row that saw nothing is told from one all of
+// whose scores are -inf.  The first is zeros; the second's sums stay 0, and its result is 0 / 0.
+constexpr float kLeast = -3.402823466e38f;
+
+// The factor that ends a row, and its log sum of exponentials.
+__device__ __forceinline__ float ends_with(float top, float total) { return top == -__builtin_inff() ? 0.0f : 1.0f / total; }
 __device__ __forceinline__ float log_sum(float top, float total)
 {
     return total == 0.0f ? -__builtin_inff() : (top + __builtin_log2f(total)) * 0.69314718056f;
@@ -420,18 +423,20 @@ struct Rows {
         for (int n = 0; n < R; ++n) {
             int from = 0;               // seen: 0 <= token - from < count, counted from this lane's first
             uint32_t count = 16;
+            float least = kLeast;
             if (masked) {
                 stay_a_branch();
                 const int lo = low[n] + 1 - first, hi = high[n] + 1 - first;
                 from = lo < 0 ? 0 : lo < 16 ? lo : 16;
                 const int to = hi < 0 ? 0 : hi < 16 ? hi : 16;
                 count = there && to > from ? to - from : 0;
+                least = count ? kLeast : -__builtin_inff();
 #pragma unroll
                 for (int t = 0; t < 16; ++t) score[n][t] = (uint32_t)(t - from) < count ? score[n][t] : -__builtin_inff();
             }
-            float most = __builtin_fmaxf(score[n][0], score[n][1]);
+            float most = least;
 #pragma unroll
-            for (int t = 2; t < 16; t += 2) most = __builtin_fmaxf(__builtin_fmaxf(score[n][t], score[n][t + 1]), most);
+            for (int t = 0; t < 16; t += 2) most = __builtin_fmaxf(__builtin_fmaxf(score[n][t], score[n][t + 1]), most);
             most = quarters_max(most);
             if (__any(most > base[n] + kSlack)) {
                 const float now = __builtin_fmaxf(base[n], most);
@@ -611,7 +616,7 @@ template <int D, int NB, int R>
 __device__ __forceinline__ void end_row(const Rows<D, NB, R> &mine, int n, const AttentionCall &call, int64_t place_out, int lane)
 {
     const int g = lane >> 4;
-    const float inverse = ends_with(mine.total[n]);
+    const float inverse = ends_with(mine.base[n], mine.total[n]);
 #pragma unroll
     for (int t = 0; t < D / 16; ++t) {
         const v4f o = mine.o[n][t] * inverse;
@@ -815,6 +820,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void attention_rows_kernel(c
                 }
                 int from[2] = {0, 0};               // seen: 0 <= token - from < count, counted from this lane's first of a block
                 uint32_t count[2] = {16, 16};
+                float most = kLeast;
                 if (masked) {
                     stay_a_branch();
 #pragma unroll
@@ -826,12 +832,12 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void attention_rows_kernel(c
 #pragma unroll
                         for (int t = 0; t < 16; ++t) score[i][t] = (uint32_t)(t - from[i]) < count[i] ? score[i][t] : -__builtin_inff();
                     }
+                    most = (count[0] | count[1]) != 0 ? kLeast : -__builtin_inff();
                 }
-                float most = score[0][0];
 #pragma unroll
-                for (int t = 1; t < 16; ++t) most = __builtin_fmaxf(most, score[0][t]);
+                for (int i = 0; i < 2; ++i)
 #pragma unroll
-                for (int t = 0; t < 16; ++t) most = __builtin_fmaxf(most, score[1][t]);
+                    for (int t = 0; t < 16; ++t) most = __builtin_fmaxf(most, score[i][t]);
                 most = halves_max(most);
                 if (__any(most > base + kSlack)) {
                     const float now = __builtin_fmaxf(base, most);
@@ -892,7 +898,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void attention_rows_kernel(c
         if (row0 + r >= rows) continue;
         const int64_t place_out = place_of_row(call, q0, row);
         if (call.splits == 1) {
-            const float inverse = ends_with(total);
+            const float inverse = ends_with(base, total);
 #pragma unroll
             for (int t = 0; t < D / 32; ++t) {
                 const v16f done = o[t] * inverse;
@@ -1273,7 +1279,7 @@ struct Joiner {
 #pragma unroll
             for (int p = 0; p < kParts; ++p) acc += shared.acc[(first + w) * 64 + p * kLanes + thread] * weight;
         }
-        acc *= ends_with(total);
+        acc *= ends_with(most, total);
         *reinterpret_cast<u32x2 *>(call.out + at * D + thread * 4) = u32x2{narrow_bf16x2(acc[0], acc[1]), narrow_bf16x2(acc[2], acc[3])};
         if (call.lse && thread == 0) call.lse[at] = log_sum(most, total);
     }
