@@ -514,7 +514,10 @@ int equarx_cache_read(const equarx_cache *cache, const int32_t *page_table, int6
  *   q_rows * q_heads is at most 2^31 - 128 (EQUARX_BAD_SHAPE); a sequence's tokens from 2^31 - 65536
  *            on are not seen.
  *   workspace  equarx_cache_attention_workspace_bytes(...) bytes, 256-byte
- *            aligned (may be NULL where that is 0); nothing in it needs clearing.
+ *            aligned (may be NULL where that is 0); nothing in it needs clearing.  A call with fewer sequences, or
+ *            a shorter longest run, may need MORE: there a context is split into more parts.  For a workspace that
+ *            serves calls of several sizes ..._most_workspace_bytes(...) is enough for all of up to q_rows rows,
+ *            sequences and max_length tokens, with any max_queries that is at least q_rows / sequences of the call.
  */
 #define EQUARX_CAUSAL 1u
 int equarx_cache_attention(const equarx_cache *cache, const void *q_bf16, int64_t q_rows, int32_t q_heads,
@@ -524,6 +527,8 @@ int equarx_cache_attention(const equarx_cache *cache, const void *q_bf16, int64_
                            void *out_bf16, float *lse, void *workspace, size_t workspace_bytes, void *stream);
 size_t equarx_cache_attention_workspace_bytes(int32_t heads, int32_t dim, int64_t q_rows, int32_t q_heads,
                                               int32_t sequences, int32_t max_queries, int64_t max_length);
+size_t equarx_cache_attention_most_workspace_bytes(int32_t heads, int32_t dim, int64_t q_rows, int32_t q_heads,
+                                                   int32_t sequences, int64_t max_length);
 
 /* Bytes of workspace equarx_reduce_quantized needs (0 for invalid arguments). */
 size_t equarx_workspace_bytes(int32_t P, int64_t n, int32_t block);

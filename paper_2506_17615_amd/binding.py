@@ -113,6 +113,7 @@ SIGNATURES = {
     "equarx_cache_attention": (ctypes.c_int, [ctypes.POINTER(_CCache), _vp, _i64, _i32, _i64, _i64, _vp, _vp, _i64, _vp, _i32,
                                               ctypes.c_float, _i32, _i64, ctypes.c_uint32, _i32, _vp, _vp, _vp, _sz, _vp]),
     "equarx_cache_attention_workspace_bytes": (_sz, [_i32, _i32, _i64, _i32, _i32, _i32, _i64]),
+    "equarx_cache_attention_most_workspace_bytes": (_sz, [_i32, _i32, _i64, _i32, _i32, _i64]),
     "equarx_workspace_bytes": (_sz, [_i32, _i64, _i32]),
     "equarx_num_blocks": (_i64, [_i64, _i32]),
     "equarx_wire_row_codes": (_i64, [_i64]),
@@ -713,10 +714,15 @@ def equarx_cache_read(cache: Cache, page_table, lengths, starts, k_out, v_out, m
                                     k_out.shape[0], _ptr(k_out), _ptr(v_out), _stream()), "equarx_cache_read")
 
 
-def alloc_cache_attention_workspace(cache: Cache, q_rows: int, q_heads: int, sequences: int, max_queries: int, max_length: int,
+def alloc_cache_attention_workspace(cache: Cache, q_rows: int, q_heads: int, sequences: int, max_queries, max_length: int,
                                     device="cuda") -> torch.Tensor:
+    """For calls of these sizes; with max_queries None for all calls of up to so many rows, sequences and tokens, whose max_queries
+    is at least their rows per sequence (a call of fewer sequences may need more than one of all)."""
     heads, dim = cache[0].shape[1], cache[0].shape[3]
-    nbytes = load().equarx_cache_attention_workspace_bytes(heads, dim, q_rows, q_heads, sequences, max_queries, max_length)
+    if max_queries is None:
+        nbytes = load().equarx_cache_attention_most_workspace_bytes(heads, dim, q_rows, q_heads, sequences, max_length)
+    else:
+        nbytes = load().equarx_cache_attention_workspace_bytes(heads, dim, q_rows, q_heads, sequences, max_queries, max_length)
     return torch.empty(max(int(nbytes), 256), dtype=torch.uint8, device=device)
 
 

@@ -90,6 +90,9 @@ int check_sequences(const int32_t *page_table, int64_t table_width, const int32_
 
 // ---------------------------------------------------------------- how an attention call is cut
 
+// Sequences up to here are not shared out.
+constexpr int64_t kShortest = 512;
+
 // A call goes to one of three kernels' forms.
 enum class AttentionForm { kRows, kShared, kWhole };
 
@@ -101,47 +104,84 @@ struct AttentionPlan {
     bool tiles_last;
 };
 
+// A wave of the kernels for few rows holds 32 rows of heads up to 128; of 256 their sums spill: 24 rows of 8 sequences of up to 4096
+// tokens, blocks of 64: 78 us, and 62 with many rows' kernel.
+inline int64_t few_rows(int32_t dim) { return dim <= 128 ? 32 : 16; }
+
+// Many rows, by workgroups of 128: as many workgroups as the CUs hold at once, two each and one with heads of 256.
+inline int64_t held_at_once(int32_t dim) { return dim <= 128 ? 512 : 256; }
+
+// Splits of the tokens for so many workgroups of rows: as many as are held at once, none with fewer than four tiles of tokens: 5
+// queries of 8 heads after 131072 tokens 27 us in 256 splits, 65 in 64; twice as many workgroups, 202 for 192 us (512 queries
+// of 32 heads after 16384).  No more for more workgroups, no fewer for more tokens.
+inline int64_t splits_for(int64_t workgroups, int32_t heads, int32_t dim, int64_t max_length)
+{
+    const int64_t held = held_at_once(dim), most = (max_length + 255) / 256;
+    int64_t splits = (held + workgroups - 1) / workgroups;
+    if (splits > most) splits = most;
+    if (splits > 256) splits = 256;
+    if (splits * heads > kGridDim) splits = kGridDim / heads;
+    return splits < 1 ? 1 : splits;
+}
+
 AttentionPlan plan_attention(int32_t heads, int32_t dim, int32_t q_heads, int32_t sequences, int64_t max_queries, int64_t max_length)
 {
     AttentionPlan p{};
     const int64_t rows = max_queries * (q_heads / heads);
     p.rows16 = rows <= 16 ? 1 : 2;
     p.splits = 1;
-    // A wave holds 32 rows of heads up to 128; of 256 their sums spill: 24 rows of 8 sequences of up to 4096 tokens, blocks of
-    // 64: 78 us, and 62 with many rows' kernel.
-    if (rows <= (dim <= 128 ? 32 : 16)) {
+    if (rows <= few_rows(dim)) {
         p.row_tiles = 1;
-        p.form = sequences > kMostShared || max_length <= 512 ? AttentionForm::kWhole : AttentionForm::kShared;
+        p.form = sequences > kMostShared || max_length <= kShortest ? AttentionForm::kWhole : AttentionForm::kShared;
         return p;
     }
     p.form = AttentionForm::kRows;
     p.row_tiles = (rows + 127) / 128;
     const int64_t workgroups = p.row_tiles * heads * sequences;
-    // as many workgroups as the CUs hold at once, two each and one with heads of 256, none with fewer than four tiles of tokens:
-    // 5 queries of 8 heads after 131072 tokens 27 us in 256 splits, 65 in 64; twice as many workgroups, 202 for 192 us (512
-    // queries of 32 heads after 16384)
-    const int64_t held = dim <= 128 ? 512 : 256;
-    int64_t splits = (held + workgroups - 1) / workgroups;
-    const int64_t most = (max_length + 255) / 256;
-    if (splits > most) splits = most;
-    if (splits > 256) splits = 256;
-    if (splits * heads > kGridDim) splits = kGridDim / heads;
-    if (splits < 1) splits = 1;
+    const int64_t splits = splits_for(workgroups, heads, dim, max_length);
     p.chunk = (int32_t)(((max_length + splits - 1) / splits + 63) / 64 * 64);
     p.splits = (int32_t)((max_length + p.chunk - 1) / p.chunk);
     // Long workgroups should be launched first, and a CU have long ones and short ones.  Tiles are launched longest first; where
     // their lengths differ most within a sequence, or all are held at once, tile after tile over all sequences (8 prompts of 1024
     // tokens, 16 heads of 64: 50 us for 65), else sequence after sequence (2 x 2048 queries of 32 heads of 128 after 8192 and
     // 5120 tokens: 629 us for 752).
-    p.tiles_last = workgroups * p.splits <= held || max_queries * 2 > max_length;
+    p.tiles_last = workgroups * p.splits <= held_at_once(dim) || max_queries * 2 > max_length;
     return p;
+}
+
+inline size_t part_bytes(int32_t dim) { return ((size_t)dim + 2) * sizeof(float); }
+inline size_t shares_bytes(int rows16, int32_t dim)
+{
+    return (size_t)kShares * 2 * rows16 * 16 * part_bytes(dim) + (kMostShared + 1) * sizeof(int64_t);
+}
+inline size_t splits_bytes(int64_t splits, int64_t q_rows, int32_t q_heads, int32_t dim)
+{
+    return splits == 1 ? 0 : (size_t)splits * (size_t)q_rows * (size_t)q_heads * part_bytes(dim);
 }
 
 size_t attention_workspace(const AttentionPlan &p, int32_t dim, int64_t q_rows, int32_t q_heads)
 {
-    const size_t row = ((size_t)dim + 2) * sizeof(float);
-    if (p.form == AttentionForm::kShared) return (size_t)kShares * 2 * p.rows16 * 16 * row + (kMostShared + 1) * sizeof(int64_t);
-    return p.splits == 1 ? 0 : (size_t)p.splits * (size_t)q_rows * (size_t)q_heads * row;
+    return p.form == AttentionForm::kShared ? shares_bytes(p.rows16, dim) : splits_bytes(p.splits, q_rows, q_heads, dim);
+}
+
+// What no call of up to so many rows, sequences and tokens needs more than, as long as its rows are at most its sequences times its
+// longest run.  Fewer sequences or shorter runs may need more: fewer workgroups of rows are cut into more splits.
+size_t most_attention_workspace(int32_t heads, int32_t dim, int64_t q_rows, int32_t q_heads, int32_t sequences, int64_t max_length)
+{
+    const int64_t group = q_heads / heads, few = few_rows(dim), held = held_at_once(dim);
+    size_t most = 0;
+    if (group <= few && max_length > kShortest) most = shares_bytes(few / group * group <= 16 ? 1 : 2, dim);
+    for (int64_t s = 1; s <= sequences && s * heads < held; ++s) {
+        // tiles of rows of the longest run, which is as long as that allows; from `held` workgroups on there is one split
+        for (int64_t tiles = 1; tiles * s * heads < held; ++tiles) {
+            const int64_t longest = tiles * 128 / group;
+            if (longest * group <= (tiles - 1) * 128) continue;         // none of so many
+            const int64_t rows = s * longest < q_rows ? s * longest : q_rows;
+            const size_t bytes = splits_bytes(splits_for(tiles * s * heads, heads, dim, max_length), rows, q_heads, dim);
+            if (bytes > most) most = bytes;
+        }
+    }
+    return most;
 }
 
 // The kernels of one geometry.
@@ -283,6 +323,13 @@ size_t equarx_cache_attention_workspace_bytes(int32_t heads, int32_t dim, int64_
 {
     if (check_heads(heads, q_rows, q_heads, dim, sequences, max_queries, max_length) != EQUARX_OK || sequences == 0) return 0;
     return attention_workspace(plan_attention(heads, dim, q_heads, sequences, max_queries, max_length), dim, q_rows, q_heads);
+}
+
+size_t equarx_cache_attention_most_workspace_bytes(int32_t heads, int32_t dim, int64_t q_rows, int32_t q_heads, int32_t sequences,
+                                                   int64_t max_length)
+{
+    if (check_heads(heads, q_rows, q_heads, dim, sequences, 1, max_length) != EQUARX_OK || sequences == 0 || q_rows == 0) return 0;
+    return most_attention_workspace(heads, dim, q_rows, q_heads, sequences, max_length);
 }
 
 int equarx_cache_attention(const equarx_cache *cache, const void *q_bf16, int64_t q_rows, int32_t q_heads,

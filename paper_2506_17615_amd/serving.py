@@ -19,7 +19,7 @@ def pack(weights: torch.Tensor):
 
 
 class ShardedAttention:
-    """Weights, caches and buffers of a layer for calls of up to max_tokens new tokens.
+    """Weights, caches and buffers of a layer for calls of up to max_tokens new tokens, of up to `sequences` sequences.
 
     w_qkv bf16 [(heads + 2 * kv_heads) * dim, hidden], heads of q before those of k and v; w_o bf16 [hidden, heads * dim].
     """
@@ -42,11 +42,9 @@ class ShardedAttention:
         new = lambda *shape: torch.empty(shape, dtype=torch.bfloat16, device="cuda")
         self.qkv, self.attended = new(shards, max_tokens, rows), new(shards, max_tokens, self.heads, dim)
         self.partials = new(shards, max_tokens, hidden)
-        # one workspace serves every call in turn; attention's depends on how long the longest query run is
-        sizes = [eq.alloc_cache_attention_workspace(self.caches[0], max_tokens, self.heads, sequences, queries, max_length, device="meta")
-                 for queries in range(1, max_tokens + 1)]
-        sizes += [eq.alloc_mx4_workspace(tokens, r, k, device="meta") for tokens in range(1, max_tokens + 1)
-                  for r, k in ((rows, hidden), (hidden, self.heads * dim))]
+        # one workspace serves every call in turn, of the largest size that any has
+        sizes = [eq.alloc_cache_attention_workspace(self.caches[0], max_tokens, self.heads, sequences, None, max_length, device="meta")]
+        sizes += [eq.alloc_mx4_workspace(max_tokens, r, k, device="meta") for r, k in ((rows, hidden), (hidden, self.heads * dim))]
         self.workspace = torch.empty(max(s.numel() for s in sizes), dtype=torch.uint8, device="cuda")
 
     def __call__(self, x, slots, q_starts, page_table, lengths, max_queries, out):
@@ -56,6 +54,7 @@ class ShardedAttention:
         if not 1 <= tokens <= self.max_tokens:
             raise ValueError(f"x: need 1 to {self.max_tokens} tokens")
         nq, nk = self.heads * self.dim, self.kv_heads * self.dim
+        max_queries = max(max_queries, -(-tokens // max(page_table.shape[0], 1)))      # no run can be shorter than the mean
         for p in range(self.shards):
             qkv, attended, cache = self.qkv[p, :tokens], self.attended[p, :tokens], self.caches[p]
             eq.equarx_mx4_linear(x, *self.w_qkv[p], qkv, self.workspace)
