@@ -22,6 +22,7 @@ class ShardedAttention:
     """Weights, caches and buffers of a layer for calls of up to max_tokens new tokens, of up to `sequences` sequences.
 
     w_qkv bf16 [(heads + 2 * kv_heads) * dim, hidden], heads of q before those of k and v; w_o bf16 [hidden, heads * dim].
+    Its calls share the buffers and the workspace: they go to one stream, or to streams that wait for each other.
     """
 
     def __init__(self, w_qkv, w_o, shards, heads, kv_heads, dim, pages, page, max_tokens, sequences, max_length, block=64,
@@ -75,6 +76,19 @@ def slots_of(page_table, page, lengths, new):
     return torch.cat(rows)
 
 
+def captured(step):
+    """A graph of step: run once on a stream of its own, after what the current one has been given, then captured."""
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(stream):
+        step()
+    torch.cuda.current_stream().wait_stream(stream)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    return graph
+
+
 def main():
     shards, heads, kv_heads, dim, hidden, page = 8, 32, 16, 128, 5376, 64
     prompts, steps = [700, 1500, 64, 1], 32
@@ -113,13 +127,7 @@ def main():
         slots = device_table[rows, last // page].long() * page + last % page
         layer(token, slots, one, device_table, lengths, 1, step_out)
 
-    stream = torch.cuda.Stream()
-    with torch.cuda.stream(stream):
-        step()
-    torch.cuda.current_stream().wait_stream(stream)
-    graph = torch.cuda.CUDAGraph()
-    with torch.cuda.graph(graph):
-        step()
+    graph = captured(step)
     us = timed(graph.replay, steps - 2)
     print(f"decode of {len(prompts)} sequences: {us:.0f} us a step and layer")
 
