@@ -184,6 +184,14 @@ size_t most_attention_workspace(int32_t heads, int32_t dim, int64_t q_rows, int3
     return most;
 }
 
+// f(first, count) in pieces whose threads a grid can hold, 256 a row at most.
+template <typename F>
+void in_launches(int64_t rows, F f)
+{
+    constexpr int64_t kPiece = (int64_t)1 << 22;
+    for (int64_t at = 0; at < rows; at += kPiece) f(at, rows - at < kPiece ? rows - at : kPiece);
+}
+
 // The kernels of one geometry.
 template <int D, int NB>
 void launch_attention(const AttentionPlan &plan, const AttentionCall &call, const Sequences &seqs, const Pool &pool, LaunchCtx &ctx)
@@ -194,11 +202,13 @@ void launch_attention(const AttentionPlan &plan, const AttentionCall &call, cons
         constexpr int R = decltype(rows16)::value;
         ctx.launch(attention_shares_kernel<D, NB, R>, (unsigned)kShares / 4, 256, call, seqs, pool);
         // many items have few parts each: a wave joins them; few have many: four
-        if ((int64_t)call.sequences * pool.heads * 8 >= kShares) {
-            ctx.launch(join_shares_kernel<D, R, 1>, (unsigned)((all + 3) / 4), 256, call, seqs, pool);
-        } else {
-            ctx.launch(join_shares_kernel<D, R, 4>, (unsigned)all, 256, call, seqs, pool);
-        }
+        in_launches(all, [&](int64_t first, int64_t rows) {
+            if ((int64_t)call.sequences * pool.heads * 8 >= kShares) {
+                ctx.launch(join_shares_kernel<D, R, 1>, (unsigned)((rows + 3) / 4), 256, call, seqs, pool, first);
+            } else {
+                ctx.launch(join_shares_kernel<D, R, 4>, (unsigned)rows, 256, call, seqs, pool, first);
+            }
+        });
     };
     if (plan.form == AttentionForm::kShared) {
         if (plan.rows16 == 1) share(std::integral_constant<int, 1>{});
@@ -224,11 +234,14 @@ void launch_attention(const AttentionPlan &plan, const AttentionCall &call, cons
             ctx.launch3d(tokens_kernel, (unsigned)tiles, (unsigned)pool.heads, (unsigned)count, 256, part, some, pool);
         }
     }
-    if (plan.splits > 8) {
-        ctx.launch(join_splits_kernel<D, 4>, (unsigned)all, 256, call);
-    } else if (plan.splits > 1) {
-        ctx.launch(join_splits_kernel<D, 1>, (unsigned)((all + 3) / 4), 256, call);
-    }
+    if (plan.splits == 1) return;
+    in_launches(all, [&](int64_t first, int64_t rows) {
+        if (plan.splits > 8) {
+            ctx.launch(join_splits_kernel<D, 4>, (unsigned)rows, 256, call, first);
+        } else {
+            ctx.launch(join_splits_kernel<D, 1>, (unsigned)((rows + 3) / 4), 256, call, first);
+        }
+    });
 }
 
 int check_heads(int32_t heads, int64_t q_rows, int32_t q_heads, int32_t dim, int32_t sequences, int32_t max_queries,

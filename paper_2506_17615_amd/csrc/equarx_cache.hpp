@@ -1285,12 +1285,12 @@ struct Joiner {
     }
 };
 
-// The splits of attention_rows_kernel.
+// The splits of attention_rows_kernel, for output rows and heads from `first` on.
 template <int D, int W>
-__global__ __launch_bounds__(256) void join_splits_kernel(const AttentionCall call)
+__global__ __launch_bounds__(256) void join_splits_kernel(const AttentionCall call, int64_t first)
 {
     __shared__ typename Joiner<D, W>::Shared shared;
-    const int64_t all = call.q_rows * call.q_heads, at = (int64_t)blockIdx.x * (4 / W) + threadIdx.x / (W * 64);
+    const int64_t all = call.q_rows * call.q_heads, at = first + (int64_t)blockIdx.x * (4 / W) + threadIdx.x / (W * 64);
     const int row = (int)((uint32_t)at / (uint32_t)call.q_heads);
     const bool write = at < all && row >= call.q_starts[0] && row < call.q_starts[call.sequences];     // not a row of no sequence
     Joiner<D, W> joiner;
@@ -1302,11 +1302,12 @@ __global__ __launch_bounds__(256) void join_splits_kernel(const AttentionCall ca
 
 // The shares of attention_shares_kernel, where a row's item is of more than one: otherwise the wave that had it wrote it.
 template <int D, int R, int W>
-__global__ __launch_bounds__(256) void join_shares_kernel(const AttentionCall call, const Sequences seqs, const Pool pool)
+__global__ __launch_bounds__(256) void join_shares_kernel(const AttentionCall call, const Sequences seqs, const Pool pool,
+                                                          int64_t first_row)
 {
     __shared__ typename Joiner<D, W>::Shared shared;
     const int lane = threadIdx.x & 63;
-    const int64_t at = (int64_t)blockIdx.x * (4 / W) + threadIdx.x / (W * 64);
+    const int64_t at = first_row + (int64_t)blockIdx.x * (4 / W) + threadIdx.x / (W * 64);
     const int row = (int)((uint32_t)at / (uint32_t)call.q_heads), head = (int)at - row * call.q_heads;
     // the row's sequence, by the wave: the last one that begins with it or before, and has it
     int b = -1;
