@@ -470,7 +470,7 @@ typedef struct equarx_cache {
  * Quantize `tokens` new tokens into their slots: k and v bf16, element
  * [t][h][d] at t * row_stride + h * head_stride + d, strides multiples of 8 in
  * elements; slots int64 [tokens] on the device, slots outside the pool are
- * skipped.  Two tokens of one call must not share a slot.
+ * skipped.  Two tokens of one call must not share a slot.  At most 2^30 tokens (EQUARX_BAD_SHAPE).
  */
 int equarx_cache_write(const equarx_cache *cache, const void *k_bf16, int64_t k_row_stride, int64_t k_head_stride,
                        const void *v_bf16, int64_t v_row_stride, int64_t v_head_stride, int64_t tokens,

@@ -79,6 +79,14 @@ void with_geometry(int32_t dim, int32_t block, F f)
 #undef EQUARX_GEOMETRY
 }
 
+// f(first, count) in pieces whose threads a grid can hold, 256 a row at most.
+template <typename F>
+void in_launches(int64_t rows, F f)
+{
+    constexpr int64_t kPiece = (int64_t)1 << 22;
+    for (int64_t at = 0; at < rows; at += kPiece) f(at, rows - at < kPiece ? rows - at : kPiece);
+}
+
 int check_sequences(const int32_t *page_table, int64_t table_width, const int32_t *lengths, int32_t sequences, Aliasing &mem)
 {
     if (!page_table || !lengths) return EQUARX_NULL_POINTER;
@@ -184,14 +192,6 @@ size_t most_attention_workspace(int32_t heads, int32_t dim, int64_t q_rows, int3
     return most;
 }
 
-// f(first, count) in pieces whose threads a grid can hold, 256 a row at most.
-template <typename F>
-void in_launches(int64_t rows, F f)
-{
-    constexpr int64_t kPiece = (int64_t)1 << 22;
-    for (int64_t at = 0; at < rows; at += kPiece) f(at, rows - at < kPiece ? rows - at : kPiece);
-}
-
 // The kernels of one geometry.
 template <int D, int NB>
 void launch_attention(const AttentionPlan &plan, const AttentionCall &call, const Sequences &seqs, const Pool &pool, LaunchCtx &ctx)
@@ -281,9 +281,12 @@ int equarx_cache_write(const equarx_cache *cache, const void *k_bf16, int64_t k_
         constexpr int D = decltype(dim)::value, B = decltype(block)::value;
         auto with = [&](auto each) {
             constexpr int T = decltype(each)::value, kTokens = 256 / (D / 8) * T;
-            ctx.launch2d(write_kernel<D, B, T>, (unsigned)((tokens + kTokens - 1) / kTokens), (unsigned)cache->heads, 256,
-                         static_cast<const uint16_t *>(k_bf16), static_cast<const uint16_t *>(v_bf16), slots, k_row_stride,
-                         v_row_stride, (int32_t)tokens, k_head_stride, v_head_stride, pool_of(*cache));
+            in_launches(tokens, [&](int64_t at, int64_t count) {
+                ctx.launch2d(write_kernel<D, B, T>, (unsigned)((count + kTokens - 1) / kTokens), (unsigned)cache->heads, 256,
+                             static_cast<const uint16_t *>(k_bf16) + at * k_row_stride,
+                             static_cast<const uint16_t *>(v_bf16) + at * v_row_stride, slots + at, k_row_stride, v_row_stride,
+                             (int32_t)count, k_head_stride, v_head_stride, pool_of(*cache));
+            });
         };
         // Four tokens a lane once that gives every CU a workgroup: 16384 tokens of 8 heads of 128 in 20 us, one a lane 43; 64
         // tokens in no order, as a decode step has them, one a lane 3.8 us, four 8 to 10.

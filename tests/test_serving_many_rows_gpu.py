@@ -2,7 +2,6 @@
 import pytest
 import torch
 
-import serving_ref as ref
 from paper_2506_17615_amd import binding as eq
 
 pytestmark = pytest.mark.gpu
@@ -45,3 +44,19 @@ def test_rows_of_no_sequence(heads, sequences, queries, max_length, rows):
     (out, lse), (far_out, far_lse) = answers
     assert torch.equal(out, far_out) and torch.equal(lse, far_lse)
     assert (out != 9).any(dim=-1).all() and torch.isfinite(lse).all() and (lse != 9).all()
+
+
+@pytest.mark.parametrize("dim", (64, 256))
+def test_tokens_that_are_all_written(dim):
+    """2^29 + 5 tokens, all of one key and value; a few of them have slots."""
+    tokens, page = (1 << 29) + 5, 16
+    cache, want = (eq.alloc_cache(2, 1, page, dim, 64) for _ in range(2))
+    k, v = (torch.randn(1, 1, dim, generator=torch.Generator().manual_seed(i)).to(torch.bfloat16).cuda() for i in (1, 2))
+    slots = torch.full((tokens,), -1, dtype=torch.int64, device="cuda")
+    places = [0, 1, (1 << 22) - 1, 1 << 22, (1 << 28) + 3, (1 << 29) - 1, 1 << 29, tokens - 1]
+    for slot, t in enumerate(places):
+        slots[t] = 3 * slot
+    eq.equarx_cache_write(cache, k.expand(tokens, 1, dim), v.expand(tokens, 1, dim), slots)
+    few = len(places)
+    eq.equarx_cache_write(want, k.repeat(few, 1, 1), v.repeat(few, 1, 1), 3 * torch.arange(few, device="cuda"))
+    assert all(torch.equal(a, b) for a, b in zip(cache, want)) and cache.k_codes.any()
