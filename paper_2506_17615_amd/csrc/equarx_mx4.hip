@@ -59,18 +59,23 @@ struct Product {
 // Does a workgroup of the kernel for few rows pack x itself?
 inline bool packs_itself(int64_t M, int64_t K) { return M <= kMostQuantizedRows && M * groups_of(K) * kGroup <= kMostQuantized; }
 
+constexpr int64_t kPieceN = (int64_t)1 << 26;           // rows of w in one launch, at most
+
 template <int WN, int WM, int FN, int FM, int kBuffers>
 void launch_tiles(const Product &p, LaunchCtx &ctx)
 {
     constexpr int64_t kN = WN * FN * 32, kM = WM * FM * 32;
-    const int64_t tiles_n = (p.N + kN - 1) / kN;
-    const int64_t most = (kGridThreads / (64 * WN * WM)) / tiles_n * kM;        // rows of x in one launch
-    for (int64_t at = 0; at < p.M; at += most) {
-        const int64_t m = p.M - at < most ? p.M - at : most, tiles_m = (m + kM - 1) / kM;
-        const int64_t groups = groups_of(p.K);
-        ctx.launch(product_tiles_kernel<WN, WM, FN, FM, kBuffers>, (unsigned)(tiles_n * tiles_m), 64 * WN * WM, p.xc + at * groups * 64,
-                   p.xs + at * groups * 4, p.wc, p.ws, p.out + at * p.out_stride, (int32_t)m, (int32_t)p.N, (int32_t)groups,
-                   p.out_stride, (uint32_t)tiles_n, (uint32_t)tiles_m);
+    const int64_t groups = groups_of(p.K);
+    for (int64_t n = 0; n < p.N; n += kPieceN) {
+        const int64_t N = p.N - n < kPieceN ? p.N - n : kPieceN, tiles_n = (N + kN - 1) / kN;
+        const int64_t most = (kGridThreads / (64 * WN * WM)) / tiles_n * kM;    // rows of x in one launch: 31 tiles at least
+        for (int64_t at = 0; at < p.M; at += most) {
+            const int64_t m = p.M - at < most ? p.M - at : most, tiles_m = (m + kM - 1) / kM;
+            ctx.launch(product_tiles_kernel<WN, WM, FN, FM, kBuffers>, (unsigned)(tiles_n * tiles_m), 64 * WN * WM,
+                       p.xc + at * groups * 64, p.xs + at * groups * 4, p.wc + n * groups * 64, p.ws + n * groups * 4,
+                       p.out + at * p.out_stride + n, (int32_t)m, (int32_t)N, (int32_t)groups, p.out_stride, (uint32_t)tiles_n,
+                       (uint32_t)tiles_m);
+        }
     }
 }
 
@@ -78,7 +83,7 @@ template <int MT, bool kQuantize>
 void launch_rows(const Product &p, LaunchCtx &ctx)
 {
     const int64_t groups = groups_of(p.K);
-    constexpr int64_t kPieceN = (int64_t)1 << 26, kPieceM = (int64_t)32768 * 32 * MT;      // of one launch
+    constexpr int64_t kPieceM = (int64_t)32768 * 32 * MT;       // rows of x in one launch
     for (int64_t n = 0; n < p.N; n += kPieceN) {
         const int64_t N = p.N - n < kPieceN ? p.N - n : kPieceN;
         for (int64_t m = 0; m < p.M; m += kPieceM) {
