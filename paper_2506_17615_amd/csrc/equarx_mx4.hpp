@@ -206,16 +206,13 @@ constexpr int kMostQuantized = 1 << 15;             // elements of x that a work
 constexpr int kMostQuantizedRows = 32;
 
 template <int MT, bool kQuantize>
-constexpr int kRowsDepth = MT == 4 ? 6 : 8;
-
-template <int MT, bool kQuantize>
 __global__ __launch_bounds__(256) void product_rows_kernel(Global<const uint8_t> xc, Global<const uint8_t> xs,
                                                            Global<const uint8_t> wc, Global<const uint8_t> ws, Global<uint16_t> out,
                                                            int32_t M, int32_t N, int32_t groups, int64_t out_stride,
                                                            int64_t x_stride, int32_t K)
 {
     constexpr int W = 4, kSides = kQuantize ? 1 : 1 + MT;           // of 32 rows each, w first
-    constexpr int kDepth = kRowsDepth<MT, kQuantize>;
+    constexpr int kDepth = MT == 4 ? 6 : 8;
     constexpr int kPair = kSides * 4096, kScales = (kSides * 512 + 1023) / 1024 * 1024;     // bytes of codes; of four groups' scales
     constexpr int kWindows = kDepth / 2 + 1;                        // fours of groups that the pairs in flight are of
     constexpr int kScalesAt = kDepth * kPair, kXAt = kScalesAt + kWindows * kScales;
