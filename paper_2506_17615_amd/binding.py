@@ -698,7 +698,10 @@ def equarx_cache_write(cache: Cache, k, v, slots) -> None:
 def equarx_cache_read(cache: Cache, page_table, lengths, starts, k_out, v_out, max_length=None) -> None:
     """Sequences back as bf16: token t of sequence b to row starts[b] + t of k_out and v_out [rows, heads, dim]."""
     if max_length is None:
-        max_length = page_table.shape[-1] * cache[0].shape[2]
+        try:
+            max_length = page_table.shape[-1] * cache[0].shape[2]           # what the table can hold
+        except (AttributeError, TypeError, IndexError):
+            max_length = 0                                                  # no table or no cache: refused below
     status = _native.equarx_cache_read(cache, page_table, lengths, starts, k_out, v_out, max_length)
     if status >= 0:
         return _check(status, "equarx_cache_read")
