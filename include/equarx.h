@@ -60,9 +60,9 @@ extern "C" {
 typedef enum equarx_status {
     EQUARX_OK = 0,
     EQUARX_NULL_POINTER = 1,        /* a required pointer is NULL */
-    EQUARX_BAD_SHAPE = 2,           /* n < 0, P < 1, P > EQUARX_MAX_PARTIALS, or overlap that is not allowed */
-    EQUARX_BAD_BLOCK = 3,           /* block not in {32, 64, 128, 256, 512} */
-    EQUARX_MISALIGNED = 4,          /* a data pointer is not 16-byte aligned */
+    EQUARX_BAD_SHAPE = 2,           /* n < 0, P < 1, P > EQUARX_MAX_PARTIALS, another size or stride out of range, or overlap that is not allowed */
+    EQUARX_BAD_BLOCK = 3,           /* block not in {32, 64, 128, 256, 512}, or not one of the cache's */
+    EQUARX_MISALIGNED = 4,          /* a data pointer is not 16-byte aligned, or a stride of the cache calls no multiple of 8 elements */
     EQUARX_WORKSPACE_TOO_SMALL = 5, /* workspace_bytes (or the static array) < what the call needs */
     EQUARX_DEVICE_ERROR = 6         /* a kernel launch of this call returned a HIP error */
 } equarx_status;

@@ -1028,12 +1028,12 @@ const char *equarx_status_string(int status)
     switch (status) {
         case EQUARX_OK: return "ok";
         case EQUARX_NULL_POINTER: return "a required pointer is NULL";
-        case EQUARX_BAD_SHAPE: return "bad shape: n < 0, P out of range, or forbidden overlap of buffers";
-        case EQUARX_BAD_BLOCK: return "block size must be 32, 64, 128, 256 or 512";
-        case EQUARX_MISALIGNED: return "a data pointer is not 16-byte aligned";
+        case EQUARX_BAD_SHAPE: return "bad shape: n, P, a dimension or a stride out of range, or forbidden overlap of buffers";
+        case EQUARX_BAD_BLOCK: return "block size must be 32, 64, 128, 256 or 512 (of a cache 64, 128 or 256, and at most its dim)";
+        case EQUARX_MISALIGNED: return "a data pointer or a stride is not aligned to 16 bytes";
         case EQUARX_WORKSPACE_TOO_SMALL:
             return "workspace (the caller's, or the static array of equarx_reduce_quantized_static) is smaller than the "
-                   "call needs: see equarx_workspace_bytes() / equarx_variant_workspace_bytes()";
+                   "call needs: see the call's equarx_..._workspace_bytes()";
         case EQUARX_DEVICE_ERROR: return "the HIP runtime reported an error at kernel launch";
         default: return "unknown status";
     }

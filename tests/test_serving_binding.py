@@ -22,3 +22,10 @@ def test_reading_back_without_a_length_is_refused_like_any_call(name, bad):
         eq.equarx_cache_read(**args)
     with pytest.raises(ValueError):
         eq.equarx_cache_read(**args, max_length=16)
+
+
+def test_an_error_names_what_a_serving_call_may_have_wrong():
+    """Not the reduction's arguments and queries alone: these statuses come from every call."""
+    text = {s: eq.status_string(s) for s in (eq.STATUS_BAD_SHAPE, eq.STATUS_BAD_BLOCK, eq.STATUS_MISALIGNED, eq.STATUS_WORKSPACE_TOO_SMALL)}
+    assert "stride" in text[eq.STATUS_BAD_SHAPE] and "stride" in text[eq.STATUS_MISALIGNED] and "cache" in text[eq.STATUS_BAD_BLOCK]
+    assert "the call's equarx_..._workspace_bytes()" in text[eq.STATUS_WORKSPACE_TOO_SMALL]
