@@ -509,8 +509,12 @@ int equarx_cache_read(const equarx_cache *cache, const int32_t *page_table, int6
  *   out [q_rows][q_heads][dim] bf16, lse fp32 [q_rows][q_heads] or NULL; rows of
  *   no sequence are not written.
  *   max_queries, max_length   the longest query run and sequence, as far as
- *            the host knows (>= 1): they size the launch and choose how a long context
- *            is split, and hence the order of the sums; larger actual values cost time, not correctness.
+ *            the host knows (>= 1): they size the launch and choose how a call and a long context
+ *            are split, and hence the order of the sums; larger actual values cost time, not correctness.
+ *            A call takes one way, by max_queries: single tokens beside long chunks are faster in a call of their own.
+ *   Equal arguments and contents give equal bits.  With few rows (max_queries * q_heads / heads up to 32, 16 for dim
+ *            256) sequences are cut into shares by the lengths of all, so that the bits of one may change with
+ *            the lengths of others.
  *   q_rows * q_heads is at most 2^31 - 128 (EQUARX_BAD_SHAPE); a sequence's tokens from 2^31 - 65536
  *            on are not seen.
  *   workspace  equarx_cache_attention_workspace_bytes(...) bytes, 256-byte

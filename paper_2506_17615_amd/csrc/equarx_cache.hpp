@@ -640,7 +640,8 @@ __device__ __forceinline__ void part_row(const Rows<D, NB, R> &mine, int n, floa
 // after that asked for, while this one's are used) in the order in which the lanes of a 32x32x16 instruction read them.
 // (2 x 2048 rows of 32 heads at the end of 8192 tokens, blocks of 64: every wave widening all for itself, 16x16x32, 1055 us;
 // this 629, 0.60 PFLOP/s, of which 130 are for probabilities as two bf16.  Two thirds of the cycles issue vector instructions -- 620
-// a wave and tile, the exponentials four times as long as others --, a third have a matrix instruction under way, and few both.)
+// a wave and tile, the exponentials four times as long as others --, a third have a matrix instruction under way, and few both.  Of
+// the LDS cycles a third are conflicts: the four lanes of a token store quarters of its keys that lie in the same banks.)
 //
 // As above with 32 for 16: the tokens of an instruction's rows are chosen so that S^T leaves lane (row c = l % 32, half h = l / 32)
 // with 16 consecutive tokens 16 h .. of the 32, row 8 j + 4 h + i being token 16 h + 4 j + i, and O^T += V^T P^T takes eight of

@@ -195,7 +195,8 @@ constexpr int64_t kMostK = (int64_t)1 << 24;
 // A workgroup has 32 rows of w and MT * 32 rows of x, and walks over all of k; what bounds it is reading w once, so what counts is
 // bytes in flight.  Pairs of groups, 128 bytes of every row, come to LDS with direct loads, kDepth - 1 pairs ahead of their turn (a lane
 // that loads its row's bytes into registers itself has its neighbours on other lines: 64 rows of x by 5376 x 5376 15.4 us; this way
-// 10.2 with the packing of x, two launches of 2.1 us that do nothing among them, and one row by 5376 x 4096 6.0 us).
+// 10.2 with the packing of x, two launches of 2.1 us that do nothing among them, and one row by 5376 x 4096 6.0 us).  With N / 32
+// workgroups, 168 of these, 88 of the 256 CUs have none.
 // In a pair wave q of the four has the blocks 2 q and 2 q + 1 of all rows, one instruction for 32 rows of x; the waves' sums are added
 // in order at the end.  LDS: a row is its 128 bytes, block b of row r in place b xor r / 2 % 8, which spreads sixteen rows' block
 // over all banks; of scales four groups' 16 bytes a row, every second pair.
@@ -380,12 +381,13 @@ __global__ __launch_bounds__(256) void product_rows_kernel(Global<const uint8_t>
 //
 // In LDS a row of a pair is 128 bytes, a line of memory, and rows follow each other as the lanes of a direct load do, eight
 // lanes a row (rows spread over distant lanes, or half lines, are more requests: 8192 cubed 383 and 291 us).  The eight blocks of
-// row r stand in the order of their number xor r / 2 % 8, so that one block of sixteen rows is in all banks once.  Scales: the
+// row r stand in the order of their number xor r / 2 % 8, so that one block of sixteen rows is in all banks once (a third of the LDS
+// cycles are counted as conflicts all the same; the words of scales, 16 bytes apart, are a sixth of those at most).  Scales: the
 // four bytes of a row and step are a word; a lane shifts it by its block and the instruction picks byte 0 or 2.  Rows' scales lie
 // far apart, a line each, so that they are loaded for four steps at once (a word a step: half of all requests).
 //
 // 8192 cubed: 274 us, 4.0 PFLOP/s, where the instruction alone on such operands does 6.6 with the clock that the power leaves it; the
-// matrix unit is busy for 54 % of the cycles, the rest are the codes' way to LDS, which takes about as long as they, and 30 us
+// matrix unit is busy for 56 to 57 % of the cycles, the rest are the codes' way to LDS, which takes about as long as they, and 30 us
 // of results on their way out that nothing runs beside.
 
 // What one of W waves loads of a side: of every pair eights of rows wave, wave + W, ...; of every second one four groups' scales of
