@@ -282,8 +282,9 @@ def _codes(v):
     """[..., block] fp32 -> codes (as fp32) and scales [..., 1]."""
     top = v.abs().amax(dim=-1, keepdim=True)
     alive = top >= 127.0 * 2.0 ** -126
-    scale = torch.where(alive, top / 127.0, 0.0)
-    inverse = torch.where(alive, 127.0 / torch.where(alive, top, 1.0), 0.0)
+    most = torch.full_like(top, 127.0)                          # by tensors: a number is multiplied by as its reciprocal
+    scale = torch.where(alive, top / most, 0.0)
+    inverse = torch.where(alive, most / torch.where(alive, top, 1.0), 0.0)
     return torch.round(v * inverse), scale
 
 
