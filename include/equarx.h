@@ -371,6 +371,54 @@ int equarx_reduce_variant_hops_strided(const void *const *partials_bf16, int32_t
                                        void *stream);
 
 /*
+ * Root-mean-square norm of rows, with the residual stream's addition before it:
+ *
+ *   h = bf16(x + residual), stored to residual (without a residual h = x)
+ *   y = fl32(fl32(h * i) * g),  i = fl32(1 / sqrt(mean over the row of h^2 + eps)),
+ *   g = weight, fl32(1 + weight) with EQUARX_NORM_ONE_PLUS, or 1 without a weight.
+ * The mean is taken in 64 bits: results do not depend on how a row is divided.  y
+ * goes to any of three outputs, rounded once for each:
+ *   out_bf16              bf16, row i at out_bf16 + i * out_stride;
+ *   codes, scales         the form of equarx_quantize, blocks of `block` elements
+ *                         (EQUARX_BAD_BLOCK) that divide a row (EQUARX_BAD_SHAPE):
+ *                         int8 [rows][cols], fp32 [rows][cols / block].  A block with a NaN or an
+ *                         infinity has scale NaN;
+ *   mx4_codes, mx4_scales the packed rows of equarx_mx4_quantize (below).
+ * NULL where an output is not wanted; codes and scales of a form go together, and one
+ * of the forms is wanted (EQUARX_NULL_POINTER).
+ *
+ *   x_bf16 [rows][cols]   row i at x_bf16 + i * x_stride; residual, in and out, the
+ *                         same with its stride, or NULL.  Strides count elements,
+ *                         are at least cols and need be a multiple of nothing.
+ *   weight_bf16 [cols]    or NULL.
+ *   rows up to 2^31 - 1, cols up to EQUARX_NORM_MAX_COLS, every tensor up to 2^40 elements;
+ *   eps >= 0 and finite (EQUARX_BAD_SHAPE): with 0, a row of zeros has NaN outputs.
+ * out_bf16 may BE x_bf16 (the same stride).  No workspace.
+ *
+ * equarx_norm_reduced norms the rows of a quantized reduction: x is what
+ * equarx_reduce_fused(partials_bf16, P, rows * cols, block) writes, the same bits, and never
+ * reaches memory.  The partials are contiguous [rows][cols]; cols is a multiple of
+ * the reduction's block (EQUARX_BAD_SHAPE).  out_bf16 may BE one of the partials (out_stride == cols).
+ */
+#define EQUARX_NORM_ONE_PLUS 1u
+#define EQUARX_NORM_MAX_COLS 32768
+typedef struct equarx_norm_outputs {
+    void *out_bf16;
+    int64_t out_stride;
+    int8_t *codes;
+    float *scales;
+    uint8_t *mx4_codes;
+    uint8_t *mx4_scales;
+    int32_t block;
+} equarx_norm_outputs;
+
+int equarx_norm(const void *x_bf16, int64_t x_stride, void *residual_bf16, int64_t residual_stride, const void *weight_bf16,
+                int64_t rows, int64_t cols, double eps, uint32_t flags, const equarx_norm_outputs *outputs, void *stream);
+int equarx_norm_reduced(const void *const *partials_bf16, int32_t P, int32_t block, void *residual_bf16, int64_t residual_stride,
+                        const void *weight_bf16, int64_t rows, int64_t cols, double eps, uint32_t flags,
+                        const equarx_norm_outputs *outputs, void *stream);
+
+/*
  * Microscaled 4-bit numbers and their product: the row-parallel layers whose
  * partial sums the calls above reduce.
  *

@@ -77,6 +77,12 @@ class _CCache(ctypes.Structure):
                 ("dim", ctypes.c_int32), ("block", ctypes.c_int32)]
 
 
+class _CNormOutputs(ctypes.Structure):
+    """equarx_norm_outputs of include/equarx.h."""
+    _fields_ = [("out_bf16", ctypes.c_void_p), ("out_stride", ctypes.c_int64), ("codes", ctypes.c_void_p), ("scales", ctypes.c_void_p),
+                ("mx4_codes", ctypes.c_void_p), ("mx4_scales", ctypes.c_void_p), ("block", ctypes.c_int32)]
+
+
 # name -> (restype, argtypes); SIGNATURES mirrors include/equarx.h, DEVTOOLS_SIGNATURES include/equarx_devtools.h
 _vp, _i64, _i32, _sz = ctypes.c_void_p, ctypes.c_int64, ctypes.c_int32, ctypes.c_size_t
 SIGNATURES = {
@@ -102,6 +108,10 @@ SIGNATURES = {
     "equarx_reduce_variant_strided": (ctypes.c_int, [ctypes.POINTER(_vp), _i32, _i64, _i32, ctypes.c_uint32, _vp, _vp]),
     "equarx_reduce_variant_hops_strided": (ctypes.c_int, [ctypes.POINTER(_vp), _i32, _i64, _i32, ctypes.c_uint32, _vp, _vp,
                                                           _sz, _vp]),
+    "equarx_norm": (ctypes.c_int, [_vp, _i64, _vp, _i64, _vp, _i64, _i64, ctypes.c_double, ctypes.c_uint32,
+                                   ctypes.POINTER(_CNormOutputs), _vp]),
+    "equarx_norm_reduced": (ctypes.c_int, [ctypes.POINTER(_vp), _i32, _i32, _vp, _i64, _vp, _i64, _i64, ctypes.c_double, ctypes.c_uint32,
+                                           ctypes.POINTER(_CNormOutputs), _vp]),
     "equarx_mx4_row_blocks": (_i64, [_i64]),
     "equarx_mx4_quantize": (ctypes.c_int, [_vp, _i64, _i64, _i64, _vp, _vp, _vp]),
     "equarx_mx4_dequantize": (ctypes.c_int, [_vp, _vp, _i64, _i64, _vp, _i64, _vp]),
@@ -758,6 +768,73 @@ def equarx_cache_attention(cache: Cache, q, q_starts, page_table, lengths, out, 
                                          width, _ptr(lengths), sequences, float(scale), max_queries, max_length,
                                          1 if causal else 0, window, _ptr(out), _ptr(lse), _ptr(workspace), nbytes, _stream()),
            "equarx_cache_attention")
+
+
+def _need_here(*tensors) -> None:
+    """The tensors' device is the current one, on whose stream the call is made."""
+    here = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.device.index != here:
+            raise ValueError(f"a tensor of {t.device}: need tensors of the current device, cuda:{here}")
+
+
+def _norm_call(rows: int, cols: int, weight, eps, residual, out, codes, scales, codes_block, mx4_codes, mx4_scales, one_plus):
+    """The arguments of a norm from `residual` on, checked."""
+    strides = []
+    for t, what in ((residual, "residual"), (out, "out")):
+        strides.append(cols if t is None else _need_rows(t, 2, what)[0])
+        if t is not None and tuple(t.shape) != (rows, cols):
+            raise ValueError(f"{what}: need [{rows}, {cols}]")
+    if weight is not None:
+        _need(weight, torch.bfloat16, cols, "weight")
+        if weight.numel() != cols:
+            raise ValueError(f"weight: need {cols} elements")
+    if not isinstance(codes_block, int):
+        raise ValueError("codes_block: need an int")
+    if codes is not None or scales is not None:
+        _need(codes, torch.int8, rows * cols, "codes")
+        _need(scales, torch.float32, num_blocks(rows * cols, codes_block) if codes_block in BLOCK_SIZES else 0, "scales")
+    if mx4_codes is not None or mx4_scales is not None:
+        _need_packed(mx4_codes, mx4_scales, rows, cols, "mx4")
+    _need_here(weight, residual, out, codes, scales, mx4_codes, mx4_scales)
+    outputs = _CNormOutputs(_ptr(out), strides[1], _ptr(codes), _ptr(scales), _ptr(mx4_codes), _ptr(mx4_scales), codes_block)
+    return (_ptr(residual), strides[0], _ptr(weight), rows, cols, float(eps), 1 if one_plus else 0, ctypes.byref(outputs), _stream())
+
+
+def equarx_norm(x, weight=None, eps: float = 1e-6, residual=None, out=None, codes=None, scales=None, codes_block: int = 0,
+                mx4_codes=None, mx4_scales=None, one_plus: bool = False) -> None:
+    """Root-mean-square norm of bf16 x [rows, cols]: residual (if given) <- x + residual, whose norm times weight (or 1 + weight) goes
+    to any of out (bf16), codes and scales (int8, blocks of codes_block), mx4_codes and mx4_scales (packed rows)."""
+    status = _native.equarx_norm(x, weight, eps, residual, out, codes, scales, codes_block, mx4_codes, mx4_scales, one_plus)
+    if status >= 0:
+        return _check(status, "equarx_norm")
+    stride, _ = _need_rows(x, 2, "x_bf16")
+    _need_here(x)
+    call = _norm_call(*x.shape, weight, eps, residual, out, codes, scales, codes_block, mx4_codes, mx4_scales, one_plus)
+    _check(load().equarx_norm(_ptr(x), stride, *call), "equarx_norm")
+
+
+def equarx_norm_reduced(partials, block: int, weight=None, eps: float = 1e-6, residual=None, out=None, codes=None, scales=None,
+                        codes_block: int = 0, mx4_codes=None, mx4_scales=None, one_plus: bool = False) -> None:
+    """equarx_norm of what equarx_reduce_fused(partials, block) writes, in one launch; partials bf16 [rows, cols]."""
+    status = _native.equarx_norm_reduced(partials, block, weight, eps, residual, out, codes, scales, codes_block, mx4_codes, mx4_scales,
+                                         one_plus)
+    if status >= 0:
+        return _check(status, "equarx_norm_reduced")
+    P = len(partials)
+    rows, cols = 0, 0
+    for i, p in enumerate(partials):
+        if not isinstance(p, torch.Tensor) or p.dim() != 2:
+            raise ValueError("partial: need [rows, cols]")
+        if i == 0:
+            rows, cols = p.shape
+        _need(p, torch.bfloat16, rows * cols, "partial")
+        if tuple(p.shape) != (rows, cols):
+            raise ValueError("partials differ in shape")
+    _need_here(*partials)
+    call = _norm_call(rows, cols, weight, eps, residual, out, codes, scales, codes_block, mx4_codes, mx4_scales, one_plus)
+    table = (_vp * max(P, 1))(*[p.data_ptr() for p in partials])
+    _check(load().equarx_norm_reduced(table, P, block, *call), "equarx_norm_reduced")
 
 
 def equarx_calib_copy(src: torch.Tensor, dst: torch.Tensor) -> None:

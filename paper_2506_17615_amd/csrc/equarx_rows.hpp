@@ -1,0 +1,62 @@
+// Rows of bf16 at any stride, eight elements a lane, and the packed 4-bit format's scale: what the kernels over rows share.
+#pragma once
+
+#include "equarx_device.hpp"
+
+namespace equarx {
+
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+// 16 bytes at any even address: rows of any stride are read and written whole where they lie
+typedef u32x4 u32x4_anywhere __attribute__((aligned(2)));
+
+// n / d for n < 2^31 by a multiplication, d fixed for a launch (Granlund and Montgomery's round-up form).
+struct Divisor {
+    uint32_t magic, shift, d;
+    explicit Divisor(uint32_t by) : magic(0), shift(0), d(by)
+    {
+        while (((uint64_t)1 << shift) < d) ++shift;
+        magic = (uint32_t)((((((uint64_t)1 << shift) - d) << 32) / d) + 1);
+    }
+    __device__ __forceinline__ uint32_t of(uint32_t n) const { return (__umulhi(n, magic) + n) >> shift; }
+};
+
+// ---------------------------------------------------------------- rows of bf16
+
+// Elements [col, col + 8) of a row of `cols`; zeros past its end.
+__device__ __forceinline__ u32x4 load_row8(const uint16_t *row, int64_t col, int64_t cols)
+{
+    if (col + 8 <= cols) return *reinterpret_cast<const u32x4_anywhere *>(row + col);
+    uint32_t e[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) e[i] = col + i < cols ? row[col + i] : 0;
+    return u32x4{e[0] | e[1] << 16, e[2] | e[3] << 16, e[4] | e[5] << 16, e[6] | e[7] << 16};
+}
+
+__device__ __forceinline__ void store_row8(uint16_t *row, int64_t col, int64_t cols, const u32x4 &v)
+{
+    if (col + 8 <= cols) {
+        *reinterpret_cast<u32x4_anywhere *>(row + col) = v;
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        if (col + i < cols) row[col + i] = (uint16_t)(v[i / 2] >> (16 * (i & 1)));
+    }
+}
+
+namespace mx4 {
+
+constexpr int kBlock = 32, kGroup = 128;
+
+// The scale byte of a block whose largest magnitude has the bf16 pattern `top`.
+__device__ __forceinline__ uint32_t scale_byte(uint32_t top)
+{
+    const uint32_t e = top >> 7;
+    return e == 255 ? 255 : e > 2 ? e - 2 : 0;
+}
+
+// 2^(byte - 127) as the instructions take it: they read the exponent field alone.
+__device__ __forceinline__ float scale_of(uint32_t byte) { return __uint_as_float(byte << 23); }
+
+}  // namespace mx4
+}  // namespace equarx

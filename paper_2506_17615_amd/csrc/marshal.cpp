@@ -34,7 +34,8 @@ struct Library {
     X(equarx_dequantize_strided) X(equarx_reduce_stage_strided) X(equarx_reduce_quantized_strided)                   \
     X(equarx_reduce_fused_strided) X(equarx_reduce_variant_strided) X(equarx_reduce_variant_hops_strided)            \
     X(equarx_mx4_quantize) X(equarx_mx4_dequantize) X(equarx_mx4_product) X(equarx_mx4_linear)                       \
-    X(equarx_cache_write) X(equarx_cache_read) X(equarx_cache_attention)
+    X(equarx_cache_write) X(equarx_cache_read) X(equarx_cache_attention)                                             \
+    X(equarx_norm) X(equarx_norm_reduced)
 #define X(name) decltype(&::name) name;
     EQUARX_CALLS(X)
 #undef X
@@ -313,11 +314,13 @@ int reduce_flat(PyObject *const *a)
 struct Rows {
     void *ptr = nullptr;
     int64_t size[3] = {0, 0, 0}, row = 0, head = 0;
+    const at::Tensor *tensor = nullptr;
 
     bool of(PyObject *o, int dims)
     {
         if (!THPVariable_CheckExact(o)) return false;
         const at::Tensor &t = THPVariable_Unpack(o);
+        tensor = &t;
         if (!t.defined() || !t.is_cuda() || !t.has_storage() || t.scalar_type() != kBF16 || t.dim() != dims) return false;
         if (t.numel() == 0) return false;
         for (int i = 0; i < dims; ++i) size[i] = t.size(i);
@@ -491,6 +494,77 @@ int cache_attention(PyObject *const *a)
                 a[9] == Py_True ? EQUARX_CAUSAL : 0u, (int32_t)window, out.ptr, static_cast<float *>(lse.ptr), ws.ptr, ws.bytes);
 }
 
+// ---------------------------------------------------------------- norms
+
+// On the device whose stream the call is made on?
+bool here(const at::Tensor *t) { return !t || t->device().index() == c10::hip::getCurrentHIPStream().device_index(); }
+
+// The arguments of a norm of [rows][cols] from `weight` on: weight, eps, residual, out, codes, scales, their block, packed codes and
+// scales, whether 1 is added to the weight.
+struct Norm {
+    Buffer weight, codes, scales;
+    Rows residual, out;
+    PackedRows packed;
+    double eps = 0;
+    uint32_t flags = 0;
+    equarx_norm_outputs to{};
+
+    bool of(PyObject *const *a, int64_t rows, int64_t cols)
+    {
+        auto sized = [&](const Rows &r) { return r.size[0] == rows && r.size[1] == cols && here(r.tensor); };
+        if (a[0] != Py_None && (!weight.of(a[0], kBF16) || weight.count != cols || !here(weight.t))) return false;
+        if (!PyFloat_CheckExact(a[1]) || !PyBool_Check(a[9])) return false;
+        eps = PyFloat_AS_DOUBLE(a[1]);
+        flags = a[9] == Py_True ? EQUARX_NORM_ONE_PLUS : 0u;
+        if (a[2] != Py_None && (!residual.of(a[2], 2) || !sized(residual))) return false;
+        if (a[3] != Py_None && (!out.of(a[3], 2) || !sized(out))) return false;
+        if (a[4] != Py_None || a[5] != Py_None) {
+            if (!a_block(a[6], to.block) || !codes.of(a[4], kInt8, rows * cols) || !here(codes.t)) return false;
+            if (!scales.of(a[5], kFloat, blocks(rows * cols, to.block)) || !here(scales.t)) return false;
+        } else {
+            long long unused;
+            if (!integer(a[6], 0, INT32_MAX, unused)) return false;
+        }
+        if (a[7] != Py_None || a[8] != Py_None) {
+            if (!packed.of(a[7], a[8], cols) || packed.rows != rows || !here(plain(a[7])) || !here(plain(a[8]))) return false;
+        }
+        to.out_bf16 = out.ptr;
+        to.out_stride = out.row;
+        to.codes = static_cast<int8_t *>(codes.ptr);
+        to.scales = static_cast<float *>(scales.ptr);
+        to.mx4_codes = packed.codes;
+        to.mx4_scales = packed.scales;
+        return true;
+    }
+};
+
+int norm(PyObject *const *a)
+{
+    Rows x;
+    Norm n;
+    if (!x.of(a[0], 2) || !here(x.tensor) || !n.of(a + 1, x.size[0], x.size[1])) return kNotPlain;
+    return call(lib.equarx_norm, x.ptr, x.row, n.residual.ptr, n.residual.row, n.weight.ptr, x.size[0], x.size[1], n.eps, n.flags, &n.to);
+}
+
+int norm_reduced(PyObject *const *a)
+{
+    Buffers x;
+    Norm n;
+    int64_t count = -1;
+    int32_t block;
+    if (!x.of(a[0], kBF16, count) || count == 0 || !a_block(a[1], block)) return kNotPlain;
+    int64_t rows = 0, cols = 0;
+    for (int32_t i = 0; i < x.count; ++i) {
+        const at::Tensor &t = THPVariable_Unpack(PySequence_Fast_GET_ITEM(a[0], i));
+        if (t.dim() != 2 || !here(&t) || (i > 0 && (t.size(0) != rows || t.size(1) != cols))) return kNotPlain;
+        rows = t.size(0);
+        cols = t.size(1);
+    }
+    if (!n.of(a + 2, rows, cols)) return kNotPlain;
+    return call(lib.equarx_norm_reduced, x.partials(), x.count, block, n.residual.ptr, n.residual.row, n.weight.ptr, rows, cols, n.eps,
+                n.flags, &n.to);
+}
+
 // The Python-callable form of f: kArgs positional arguments; an exception from torch is "not plain" too.
 template <int kArgs, typename F>
 PyObject *enter(PyObject *const *a, Py_ssize_t count, F f)
@@ -540,6 +614,8 @@ ENTRY(5, equarx_mx4_linear, mx4_linear(a))
 ENTRY(4, equarx_cache_write, cache_write(a))
 ENTRY(7, equarx_cache_read, cache_read(a))
 ENTRY(13, equarx_cache_attention, cache_attention(a))
+ENTRY(11, equarx_norm, norm(a))
+ENTRY(12, equarx_norm_reduced, norm_reduced(a))
 #undef ENTRY
 
 // bind({name: address}): where the library's entry points are.
