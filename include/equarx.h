@@ -582,6 +582,85 @@ size_t equarx_cache_attention_workspace_bytes(int32_t heads, int32_t dim, int64_
 size_t equarx_cache_attention_most_workspace_bytes(int32_t heads, int32_t dim, int64_t q_rows, int32_t q_heads,
                                                    int32_t sequences, int64_t max_length);
 
+/*
+ * Pages for the cache's sequences, handed out and taken back on the device, and the
+ * slot of every new token: what equarx_cache_write and equarx_cache_attention read, without
+ * a word from the host, so that a captured step goes on by itself.
+ *
+ *   table      int32 [sequences][width], as the cache's calls take it: a sequence of L
+ *              tokens holds the entries of its first ceil(L / page) pages;
+ *   lengths    int32 [sequences];
+ *   free       int32 [pages]: a stack of the pages that nobody holds, free_count of
+ *              them (int32 [1]), the top one last.
+ *   sequences up to 2^20, width and pages up to 2^31 - 1, page from 1 to 65536, pages * page and
+ *   the table up to 2^40 (EQUARX_BAD_SHAPE).  A page is one sequence's.  Values out of range are taken
+ *   as the nearest in it (lengths, free_count) or for no page (table, when it is given back).
+ *
+ * equarx_pages_trim takes sequence b back to its first keep[b] tokens (int32 [sequences]; 0: it has ended; as many as it has, or
+ * more: as it is): pages behind them go to the stack, in order of the sequences and
+ * of their tokens, and their entries become -1.
+ *
+ * equarx_pages_extend gives sequence b counts[b] more tokens (int32 [sequences]; below 0 as 0): all of them or none.  It gets none
+ * if the table has no room; else if the tokens wanted by it and the sequences before it are
+ * more than `rows`; else if the pages that it and those before it want (as far as they passed these two) are more than the
+ * stack holds, and it wants any.  Pages come from the top of the stack, in the same order.
+ *
+ *   q_starts   int32 [sequences + 1]: rows of the step before each sequence's and, last,
+ *              of all;
+ *   granted    int32 [sequences] or NULL: the tokens that it got;
+ *   slots      int64 [rows]: where row r's token goes; -1 for rows of no sequence;
+ *   positions  int32 [rows] or NULL: its place in its sequence, or -1;
+ *   row_tags   int32 [rows] with tags int32 [sequences], or both NULL: its sequence's
+ *              tag (an adapter, say), or -1.
+ *   rows up to 2^30 (EQUARX_BAD_SHAPE).
+ * Numbers need only their elements' alignment.  No array may overlap another that is written.
+ * Equal contents give equal results.
+ */
+typedef struct equarx_pages {
+    int32_t *table;
+    int32_t *lengths;
+    int32_t *free;
+    int32_t *free_count;
+    int64_t width, pages;
+    int32_t sequences, page;
+} equarx_pages;
+
+int equarx_pages_trim(const equarx_pages *pages, const int32_t *keep, void *stream);
+int equarx_pages_extend(const equarx_pages *pages, const int32_t *counts, int32_t *q_starts, int64_t *slots, int32_t *granted,
+                        int32_t *positions, const int32_t *tags, int32_t *row_tags, int64_t rows, void *stream);
+
+/*
+ * Low-rank adapters of many requests at once, beside a projection that they share:
+ * row m of x has the adapter a = ids[m], and
+ *
+ *   t = A[a] x[m],   out[m][n] = bf16(out[m][n] + factors[a] * sum_j B[a][n][j] t[s(n) * rank + j])
+ * with out the shared projection's outputs (of equarx_mx4_linear, say), added to in place.
+ * The outputs are `slices` runs of columns, run s up to slice_ends[s] - 1, each with `rank` rows of A of its own
+ * (a joint q, k, v projection has three); s(n) is the run that n is in.
+ *
+ *   x_bf16 [M][K]      row m at x_bf16 + m * x_stride;
+ *   a_bf16             [adapters][slices * rank][K],  b_bf16 [adapters][N][rank], contiguous;
+ *   factors            fp32 [adapters];
+ *   ids                int32 [M] on the device; rows whose id is outside [0, adapters) are left as they were;
+ *   slice_ends         HOST int64 [slices], growing, the last one N; read before the call returns;
+ *   out_bf16 [M][N]    row m at out_bf16 + m * out_stride.  Strides need be a multiple of nothing.
+ *   rank a multiple of 8 up to EQUARX_ADAPTERS_MAX_RANK (an adapter of a lower one has zeros in the rest), slices up to
+ *   EQUARX_ADAPTERS_MAX_SLICES, M up to 2^24, N and K up to 2^22, adapters up to EQUARX_ADAPTERS_MAX, every tensor up to 2^40 elements
+ *   (EQUARX_BAD_SHAPE).  K == 0 changes nothing.
+ *   workspace          device, equarx_adapters_workspace_bytes(...) bytes, 256-byte aligned (may be NULL where
+ *                      that is 0); nothing in it needs clearing.  Never less for fewer rows.
+ * Sums are fp32; t meets B as a sum of two bf16, to 2^-16.  The order of a row's sums depends on
+ * the sizes alone: not on its place, its neighbours or their adapters.  Rows of one adapter are brought together
+ * wherever they are.  No output may overlap another buffer of the call (EQUARX_BAD_SHAPE).
+ */
+#define EQUARX_ADAPTERS_MAX 8192
+#define EQUARX_ADAPTERS_MAX_RANK 128
+#define EQUARX_ADAPTERS_MAX_SLICES 4
+int equarx_adapters(const void *x_bf16, int64_t x_stride, const void *a_bf16, const void *b_bf16, const float *factors,
+                    int32_t adapters, int32_t rank, const int32_t *ids, int64_t M, int64_t N, int64_t K, const int64_t *slice_ends,
+                    int32_t slices, void *out_bf16, int64_t out_stride, void *workspace, size_t workspace_bytes, void *stream);
+size_t equarx_adapters_workspace_bytes(int64_t M, int64_t N, int64_t K, int32_t rank, int32_t slices, int32_t adapters);
+
 /* Bytes of workspace equarx_reduce_quantized needs (0 for invalid arguments). */
 size_t equarx_workspace_bytes(int32_t P, int64_t n, int32_t block);
 

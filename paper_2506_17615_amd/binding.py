@@ -83,6 +83,12 @@ class _CNormOutputs(ctypes.Structure):
                 ("mx4_codes", ctypes.c_void_p), ("mx4_scales", ctypes.c_void_p), ("block", ctypes.c_int32)]
 
 
+class _CPages(ctypes.Structure):
+    """equarx_pages of include/equarx.h."""
+    _fields_ = [("table", ctypes.c_void_p), ("lengths", ctypes.c_void_p), ("free", ctypes.c_void_p), ("free_count", ctypes.c_void_p),
+                ("width", ctypes.c_int64), ("pages", ctypes.c_int64), ("sequences", ctypes.c_int32), ("page", ctypes.c_int32)]
+
+
 # name -> (restype, argtypes); SIGNATURES mirrors include/equarx.h, DEVTOOLS_SIGNATURES include/equarx_devtools.h
 _vp, _i64, _i32, _sz = ctypes.c_void_p, ctypes.c_int64, ctypes.c_int32, ctypes.c_size_t
 SIGNATURES = {
@@ -124,6 +130,11 @@ SIGNATURES = {
                                               ctypes.c_float, _i32, _i64, ctypes.c_uint32, _i32, _vp, _vp, _vp, _sz, _vp]),
     "equarx_cache_attention_workspace_bytes": (_sz, [_i32, _i32, _i64, _i32, _i32, _i32, _i64]),
     "equarx_cache_attention_most_workspace_bytes": (_sz, [_i32, _i32, _i64, _i32, _i32, _i64]),
+    "equarx_pages_trim": (ctypes.c_int, [ctypes.POINTER(_CPages), _vp, _vp]),
+    "equarx_pages_extend": (ctypes.c_int, [ctypes.POINTER(_CPages), _vp, _vp, _vp, _vp, _vp, _vp, _vp, _i64, _vp]),
+    "equarx_adapters": (ctypes.c_int, [_vp, _i64, _vp, _vp, _vp, _i32, _i32, _vp, _i64, _i64, _i64, ctypes.POINTER(_i64), _i32, _vp, _i64,
+                                       _vp, _sz, _vp]),
+    "equarx_adapters_workspace_bytes": (_sz, [_i64, _i64, _i64, _i32, _i32, _i32]),
     "equarx_workspace_bytes": (_sz, [_i32, _i64, _i32]),
     "equarx_num_blocks": (_i64, [_i64, _i32]),
     "equarx_wire_row_codes": (_i64, [_i64]),
@@ -835,6 +846,113 @@ def equarx_norm_reduced(partials, block: int, weight=None, eps: float = 1e-6, re
     call = _norm_call(rows, cols, weight, eps, residual, out, codes, scales, codes_block, mx4_codes, mx4_scales, one_plus)
     table = (_vp * max(P, 1))(*[p.data_ptr() for p in partials])
     _check(load().equarx_norm_reduced(table, P, block, *call), "equarx_norm_reduced")
+
+
+class Pages(NamedTuple):
+    """Pages of a cache's sequences: table int32 [sequences, width], lengths int32 [sequences], and the stack of those that nobody holds,
+    free int32 [pages] and free_count int32 [1]."""
+    table: torch.Tensor
+    lengths: torch.Tensor
+    free: torch.Tensor
+    free_count: torch.Tensor
+
+
+def alloc_pages(sequences: int, width: int, pages: int, device="cuda") -> Pages:
+    """Sequences of no tokens, of up to `width` pages each, and `pages` pages that nobody holds, the first on top of the stack."""
+    ints = lambda values: values.to(torch.int32).to(device)
+    return Pages(ints(torch.full((sequences, width), -1)), ints(torch.zeros(sequences)), ints(torch.arange(pages - 1, -1, -1)),
+                 ints(torch.tensor([pages])))
+
+
+def _need_exactly(t, dtype, count: int, what: str) -> None:
+    """A contiguous CUDA tensor of the current device with `count` elements."""
+    if t is None or not t.is_cuda or t.dtype != dtype or not t.is_contiguous() or t.numel() != count:
+        raise ValueError(f"{what}: need a contiguous CUDA {dtype} tensor of {count} elements")
+    _need_here(t)
+
+
+def _need_pages(pages, page):
+    """The C structure of a Pages whose tensors have the shapes they should have."""
+    if not isinstance(pages, (tuple, list)) or len(pages) != 4 or not all(isinstance(t, torch.Tensor) for t in pages):
+        raise ValueError("pages: need the four tensors of a Pages")
+    table, lengths, free, free_count = pages
+    if table.dim() != 2 or free.dim() != 1:
+        raise ValueError("pages: need a table [sequences, width] and a stack [pages]")
+    if not isinstance(page, int) or not 1 <= page <= 65536:
+        raise ValueError("page: need an int from 1 to 65536")
+    sequences, width = table.shape
+    _need_exactly(table, torch.int32, sequences * width, "table")
+    _need_exactly(lengths, torch.int32, sequences, "lengths")
+    _need_exactly(free, torch.int32, free.numel(), "free")
+    _need_exactly(free_count, torch.int32, 1, "free_count")
+    return _CPages(_ptr(table), _ptr(lengths), _ptr(free), _ptr(free_count), width, free.numel(), sequences, page)
+
+
+def equarx_pages_trim(pages: Pages, page: int, keep) -> None:
+    """Takes every sequence back to its first keep[b] tokens (int32 [sequences]); the pages behind them go to the stack."""
+    status = _native.equarx_pages_trim(pages, page, keep)
+    if status >= 0:
+        return _check(status, "equarx_pages_trim")
+    c = _need_pages(pages, page)
+    _need_exactly(keep, torch.int32, c.sequences, "keep")
+    _check(load().equarx_pages_trim(ctypes.byref(c), _ptr(keep), _stream()), "equarx_pages_trim")
+
+
+def equarx_pages_extend(pages: Pages, page: int, counts, q_starts, slots, granted=None, positions=None, tags=None, row_tags=None) -> None:
+    """Gives every sequence counts[b] more tokens, or none where table, rows or stack have no room for them (granted: what it got), and
+    tells the rows of the step: q_starts int32 [sequences + 1], slots int64 [rows], positions int32 [rows], row_tags int32 [rows] its
+    sequence's of tags int32 [sequences]; -1 in rows of no sequence."""
+    status = _native.equarx_pages_extend(pages, page, counts, q_starts, slots, granted, positions, tags, row_tags)
+    if status >= 0:
+        return _check(status, "equarx_pages_extend")
+    c = _need_pages(pages, page)
+    rows = slots.numel() if isinstance(slots, torch.Tensor) else 0
+    _need_exactly(slots, torch.int64, rows, "slots")
+    _need_exactly(counts, torch.int32, c.sequences, "counts")
+    _need_exactly(q_starts, torch.int32, c.sequences + 1, "q_starts")
+    for t, count, what in ((granted, c.sequences, "granted"), (positions, rows, "positions"), (tags, c.sequences, "tags"),
+                           (row_tags, rows, "row_tags")):
+        if t is not None:
+            _need_exactly(t, torch.int32, count, what)
+    _check(load().equarx_pages_extend(ctypes.byref(c), _ptr(counts), _ptr(q_starts), _ptr(slots), _ptr(granted), _ptr(positions), _ptr(tags),
+                                      _ptr(row_tags), rows, _stream()), "equarx_pages_extend")
+
+
+def alloc_adapters_workspace(M: int, N: int, K: int, rank: int, slices: int, adapters: int, device="cuda") -> torch.Tensor:
+    """For calls of up to M rows of these sizes."""
+    nbytes = load().equarx_adapters_workspace_bytes(M, N, K, rank, slices, adapters)
+    return torch.empty(max(int(nbytes), 256), dtype=torch.uint8, device=device)
+
+
+def equarx_adapters(x, a, b, factors, ids, out, slice_ends=None, workspace=None) -> None:
+    """out [M, N] += factors[i] * (x A[i]^T) B[i]^T for every row's adapter i = ids[m] (none outside [0, adapters)): x bf16 [M, K], a bf16
+    [adapters, slices * rank, K], b bf16 [adapters, N, rank]; slice_ends: the columns at which the slices end, the last one N."""
+    status = _native.equarx_adapters(x, a, b, factors, ids, out, slice_ends, workspace)
+    if status >= 0:
+        return _check(status, "equarx_adapters")
+    x_stride, _ = _need_rows(x, 2, "x_bf16")
+    out_stride, _ = _need_rows(out, 2, "out")
+    (M, K), N = x.shape, out.shape[1]
+    if out.shape[0] != M:
+        raise ValueError("x_bf16 and out differ in rows")
+    ends = (N,) if slice_ends is None else tuple(slice_ends)
+    if not all(isinstance(e, int) for e in ends) or not 1 <= len(ends) <= 4:
+        raise ValueError("slice_ends: need one to four ints")
+    for t, what in ((a, "a"), (b, "b")):
+        if not isinstance(t, torch.Tensor) or t.dim() != 3:
+            raise ValueError(f"{what}: need three dimensions")
+    adapters, rank = b.shape[0], b.shape[2]
+    _need_exactly(a, torch.bfloat16, adapters * len(ends) * rank * K, "a")
+    _need_exactly(b, torch.bfloat16, adapters * N * rank, "b")
+    if tuple(a.shape) != (adapters, len(ends) * rank, K) or b.shape[1] != N:
+        raise ValueError(f"a, b: need [{adapters}, {len(ends)} * {rank}, {K}] and [{adapters}, {N}, {rank}]")
+    _need_exactly(factors, torch.float32, adapters, "factors")
+    _need_exactly(ids, torch.int32, M, "ids")
+    _need_here(x, out, workspace)
+    nbytes = _need_workspace(workspace)
+    _check(load().equarx_adapters(_ptr(x), x_stride, _ptr(a), _ptr(b), _ptr(factors), adapters, rank, _ptr(ids), M, N, K,
+                                  (_i64 * len(ends))(*ends), len(ends), _ptr(out), out_stride, _ptr(workspace), nbytes, _stream()),
+           "equarx_adapters")
 
 
 def equarx_calib_copy(src: torch.Tensor, dst: torch.Tensor) -> None:

@@ -11,10 +11,10 @@ CSRC = os.path.join(_PKG, "csrc")
 INCLUDE = os.path.join(_ROOT, "include")
 LIB_PATH = os.path.join(_PKG, "libequarx.so")
 SOURCES = [os.path.join(CSRC, name) for name in ("equarx_api.hip", "equarx_devtools.hip", "equarx_mx4.hip", "equarx_cache.hip",
-                                             "equarx_norm.hip")]
+                                             "equarx_norm.hip", "equarx_adapters.hip", "equarx_pages.hip")]
 HEADERS = [os.path.join(CSRC, name) for name in ("equarx_device.hpp", "equarx_strided.hpp", "equarx_launch.hpp", "equarx_passes.hpp",
                                                   "equarx_devtools_kernels.hpp", "equarx_rows.hpp", "equarx_mx4.hpp", "equarx_cache.hpp",
-                                                  "equarx_norm.hpp")]
+                                                  "equarx_norm.hpp", "equarx_adapters.hpp", "equarx_pages.hpp")]
 HEADERS += [os.path.join(INCLUDE, "equarx.h"), os.path.join(INCLUDE, "equarx_devtools.h")]
 
 HIPCC_FLAGS = [

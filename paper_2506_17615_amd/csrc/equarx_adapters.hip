@@ -1,0 +1,141 @@
+// Host side of the adapters: argument validation, how a call is cut, and launch.
+#include "equarx.h"
+
+#include "equarx_adapters.hpp"
+#include "equarx_launch.hpp"
+
+namespace {
+
+using namespace equarx;
+using namespace equarx::host;
+using namespace equarx::adapters;
+
+constexpr int64_t kMostRows = (int64_t)1 << 24, kMostCols = (int64_t)1 << 22, kMostElements = (int64_t)1 << 40;
+
+struct Sizes {
+    int64_t M, N, K;
+    int32_t rank, slices, adapters;
+};
+
+int check_sizes(const Sizes &z)
+{
+    if (z.M < 0 || z.N < 0 || z.K < 0 || z.M > kMostRows || z.N > kMostCols || z.K > kMostCols) return EQUARX_BAD_SHAPE;
+    if (z.rank < 8 || z.rank % 8 != 0 || z.rank > EQUARX_ADAPTERS_MAX_RANK || z.slices < 1 || z.slices > EQUARX_ADAPTERS_MAX_SLICES ||
+        z.adapters < 1 || z.adapters > EQUARX_ADAPTERS_MAX)
+        return EQUARX_BAD_SHAPE;
+    const int64_t R = (int64_t)z.rank * z.slices;
+    if (z.K > kMostElements / (R * z.adapters) || z.N > kMostElements / ((int64_t)z.rank * z.adapters)) return EQUARX_BAD_SHAPE;
+    return EQUARX_OK;
+}
+
+int check_rows(int64_t rows, int64_t cols, int64_t stride)
+{
+    return stride < cols || stride > kMostElements / rows ? EQUARX_BAD_SHAPE : EQUARX_OK;
+}
+
+inline size_t row_bytes(int64_t rows, int64_t cols, int64_t stride) { return (size_t)((rows - 1) * stride + cols) * 2; }
+
+// How a call is cut, by its sizes alone.
+constexpr int64_t kWorkgroups = 1024;
+
+struct Cut {
+    int tile;               // rows of an item, at most
+    int64_t items;          // at most
+    int32_t rank_tiles, piece, splits;
+    size_t order, list, count, bytes;       // of the workspace: t from 0 on
+};
+
+Cut cut_of(const Sizes &z)
+{
+    Cut c{};
+    const int64_t R = (int64_t)z.rank * z.slices, groups = z.M < z.adapters ? z.M : z.adapters;
+    c.tile = z.M >= 32 * groups ? 64 : 16;
+    c.items = z.M / c.tile + groups;
+    c.rank_tiles = (int32_t)((R + kRankTile - 1) / kRankTile);
+    const int64_t most = (z.K + kWaveSteps - 1) / kWaveSteps;
+    auto limited = [](int64_t v, int64_t hi) { return v < 1 ? 1 : v < hi ? v : hi; };
+    const int64_t splits = limited(kWorkgroups / (c.items * c.rank_tiles), limited(most, 32));
+    c.piece = (int32_t)((most + splits - 1) / splits * kWaveSteps);
+    c.splits = (int32_t)((z.K + c.piece - 1) / c.piece);
+    // room for the partial sums of this many rows or fewer: of m rows in more than one split there are at most 64 kWorkgroups / rank_tiles
+    const int64_t bound = 64 * kWorkgroups / c.rank_tiles, cut_rows = z.M * limited(most, 32);
+    const int64_t rows = z.M > (cut_rows < bound ? cut_rows : bound) ? z.M : (cut_rows < bound ? cut_rows : bound);
+    c.order = round_up((size_t)(rows * R) * sizeof(float), kWorkspaceAlign);
+    c.list = c.order + round_up((size_t)z.M * sizeof(int32_t), kWorkspaceAlign);
+    c.count = c.list + round_up((size_t)(z.M / 16 + groups) * sizeof(Item), kWorkspaceAlign);
+    c.bytes = c.count + kWorkspaceAlign;
+    return c;
+}
+
+template <int RT>
+void launch(const Sizes &z, const Cut &c, const uint16_t *x, int64_t x_stride, const uint16_t *a, const uint16_t *b, const float *factors,
+            const int32_t *ids, const Slices &cut, uint16_t *out, int64_t out_stride, uint8_t *workspace, LaunchCtx &ctx)
+{
+    float *const t = reinterpret_cast<float *>(workspace);
+    int32_t *const order = reinterpret_cast<int32_t *>(workspace + c.order), *const count = reinterpret_cast<int32_t *>(workspace + c.count);
+    Item *const items = reinterpret_cast<Item *>(workspace + c.list);
+    const int32_t R = z.rank * z.slices;
+    ctx.launch(group_kernel, 1, 1024, ids, z.M, z.adapters, c.tile, order, items, count);
+    ctx.launch3d(shrink_kernel<RT>, (unsigned)c.items, (unsigned)c.rank_tiles, (unsigned)c.splits, 256, x, x_stride, a, t, z.M, z.K, R, c.piece,
+                 static_cast<const int32_t *>(order), static_cast<const Item *>(items), static_cast<const int32_t *>(count));
+    ctx.launch2d(expand_kernel<RT>, (unsigned)c.items, (unsigned)cut.first_chunk[z.slices], 256, out, out_stride, b, factors,
+                 static_cast<const float *>(t), z.M, z.N, z.rank, z.slices, c.splits, static_cast<const int32_t *>(order),
+                 static_cast<const Item *>(items), static_cast<const int32_t *>(count), cut);
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t equarx_adapters_workspace_bytes(int64_t M, int64_t N, int64_t K, int32_t rank, int32_t slices, int32_t adapters)
+{
+    const Sizes z{M, N, K, rank, slices, adapters};
+    if (check_sizes(z) != EQUARX_OK || M == 0 || N == 0 || K == 0) return 0;
+    return cut_of(z).bytes;
+}
+
+int equarx_adapters(const void *x_bf16, int64_t x_stride, const void *a_bf16, const void *b_bf16, const float *factors, int32_t adapters,
+                    int32_t rank, const int32_t *ids, int64_t M, int64_t N, int64_t K, const int64_t *slice_ends, int32_t slices,
+                    void *out_bf16, int64_t out_stride, void *workspace, size_t workspace_bytes, void *stream)
+{
+    LaunchCtx ctx(stream);
+    const Sizes z{M, N, K, rank, slices, adapters};
+    if (int st = check_sizes(z)) return st;
+    if (!slice_ends) return EQUARX_NULL_POINTER;
+    Slices cut{};
+    for (int32_t s = 0; s < slices; ++s) {
+        const int64_t from = s == 0 ? 0 : slice_ends[s - 1];
+        if (slice_ends[s] < from || slice_ends[s] > N || (s + 1 == slices && slice_ends[s] != N)) return EQUARX_BAD_SHAPE;
+        cut.first_column[s + 1] = (int32_t)slice_ends[s];
+        cut.first_chunk[s + 1] = cut.first_chunk[s] + (int32_t)((slice_ends[s] - from + kChunk - 1) / kChunk);
+    }
+    if (M == 0 || N == 0) return EQUARX_OK;
+    if (int st = check_rows(M, N, out_stride)) return st;
+    if (int st = check_rows(M, K, x_stride)) return st;
+    if (!out_bf16 || !factors || !ids || !b_bf16 || (K > 0 && (!x_bf16 || !a_bf16))) return EQUARX_NULL_POINTER;
+    if (misaligned(x_bf16, kAlign) || misaligned(a_bf16, kAlign) || misaligned(b_bf16, kAlign) || misaligned(out_bf16, kAlign) ||
+        misaligned(factors, 4) || misaligned(ids, 4) || misaligned(workspace, kWorkspaceAlign))
+        return EQUARX_MISALIGNED;
+    const Cut c = K > 0 ? cut_of(z) : Cut{};
+    if (K > 0) {
+        if (!workspace) return EQUARX_NULL_POINTER;
+        if (workspace_bytes < c.bytes) return EQUARX_WORKSPACE_TOO_SMALL;
+    }
+    Aliasing mem;
+    const size_t many = (size_t)adapters * rank;
+    if (K > 0) mem.reads(x_bf16, row_bytes(M, K, x_stride));
+    mem.reads(a_bf16, many * slices * (size_t)K * 2);
+    mem.reads(b_bf16, many * (size_t)N * 2);
+    mem.reads(factors, (size_t)adapters * sizeof(float));
+    mem.reads(ids, (size_t)M * sizeof(int32_t));
+    mem.writes(out_bf16, row_bytes(M, N, out_stride));
+    if (K > 0) mem.writes(workspace, c.bytes);
+    if (int st = mem.check()) return st;
+    if (K == 0) return EQUARX_OK;
+    (c.tile == 64 ? launch<4> : launch<1>)(z, c, static_cast<const uint16_t *>(x_bf16), x_stride, static_cast<const uint16_t *>(a_bf16),
+                                           static_cast<const uint16_t *>(b_bf16), factors, ids, cut, static_cast<uint16_t *>(out_bf16),
+                                           out_stride, static_cast<uint8_t *>(workspace), ctx);
+    return ctx.status();
+}
+
+}  // extern "C"

@@ -35,7 +35,7 @@ struct Library {
     X(equarx_reduce_fused_strided) X(equarx_reduce_variant_strided) X(equarx_reduce_variant_hops_strided)            \
     X(equarx_mx4_quantize) X(equarx_mx4_dequantize) X(equarx_mx4_product) X(equarx_mx4_linear)                       \
     X(equarx_cache_write) X(equarx_cache_read) X(equarx_cache_attention)                                             \
-    X(equarx_norm) X(equarx_norm_reduced)
+    X(equarx_norm) X(equarx_norm_reduced) X(equarx_pages_trim) X(equarx_pages_extend) X(equarx_adapters)
 #define X(name) decltype(&::name) name;
     EQUARX_CALLS(X)
 #undef X
@@ -565,6 +565,89 @@ int norm_reduced(PyObject *const *a)
                 n.flags, &n.to);
 }
 
+// ---------------------------------------------------------------- pages and adapters
+
+// A contiguous tensor of the current device with exactly `count` elements.
+bool exactly(Buffer &b, PyObject *o, at::ScalarType type, int64_t count) { return b.of(o, type) && b.count == count && here(b.t); }
+
+// A Pages (a tuple of four tensors) and the tokens of a page.
+bool some_pages(PyObject *o, PyObject *page, equarx_pages &p)
+{
+    long long size;
+    Buffer table, lengths, free, count;
+    if (!PyTuple_Check(o) || PyTuple_GET_SIZE(o) != 4 || !integer(page, 1, 65536, size)) return false;
+    if (!table.of(PyTuple_GET_ITEM(o, 0), kInt) || table.t->dim() != 2 || table.count == 0 || table.t->size(0) > INT32_MAX || !here(table.t))
+        return false;
+    p.sequences = (int32_t)table.t->size(0);
+    p.width = table.t->size(1);
+    if (!exactly(lengths, PyTuple_GET_ITEM(o, 1), kInt, p.sequences) || !exactly(count, PyTuple_GET_ITEM(o, 3), kInt, 1)) return false;
+    if (!free.of(PyTuple_GET_ITEM(o, 2), kInt) || free.t->dim() != 1 || !here(free.t)) return false;
+    p.table = static_cast<int32_t *>(table.ptr);
+    p.lengths = static_cast<int32_t *>(lengths.ptr);
+    p.free = static_cast<int32_t *>(free.ptr);
+    p.free_count = static_cast<int32_t *>(count.ptr);
+    p.pages = free.count;
+    p.page = (int32_t)size;
+    return true;
+}
+
+int pages_trim(PyObject *const *a)
+{
+    equarx_pages p;
+    Buffer keep;
+    if (!some_pages(a[0], a[1], p) || !exactly(keep, a[2], kInt, p.sequences)) return kNotPlain;
+    return call(lib.equarx_pages_trim, &p, static_cast<const int32_t *>(keep.ptr));
+}
+
+int pages_extend(PyObject *const *a)
+{
+    equarx_pages p;
+    Buffer counts, starts, slots, granted, positions, tags, row_tags;
+    if (!some_pages(a[0], a[1], p) || !exactly(counts, a[2], kInt, p.sequences) || !exactly(starts, a[3], kInt, (int64_t)p.sequences + 1))
+        return kNotPlain;
+    if (!slots.of(a[4], kLong) || !here(slots.t)) return kNotPlain;
+    if (a[5] != Py_None && !exactly(granted, a[5], kInt, p.sequences)) return kNotPlain;
+    if (a[6] != Py_None && !exactly(positions, a[6], kInt, slots.count)) return kNotPlain;
+    if (a[7] != Py_None && !exactly(tags, a[7], kInt, p.sequences)) return kNotPlain;
+    if (a[8] != Py_None && !exactly(row_tags, a[8], kInt, slots.count)) return kNotPlain;
+    return call(lib.equarx_pages_extend, &p, static_cast<const int32_t *>(counts.ptr), static_cast<int32_t *>(starts.ptr),
+                static_cast<int64_t *>(slots.ptr), static_cast<int32_t *>(granted.ptr), static_cast<int32_t *>(positions.ptr),
+                static_cast<const int32_t *>(tags.ptr), static_cast<int32_t *>(row_tags.ptr), slots.count);
+}
+
+int adapters(PyObject *const *a)
+{
+    Rows x, out;
+    Buffer da, db, factors, ids;
+    Workspace ws;
+    int64_t ends[EQUARX_ADAPTERS_MAX_SLICES];
+    Py_ssize_t slices = 1;
+    if (!x.of(a[0], 2) || !here(x.tensor) || !out.of(a[5], 2) || !here(out.tensor) || out.size[0] != x.size[0]) return kNotPlain;
+    const int64_t M = x.size[0], K = x.size[1], N = out.size[1];
+    if (a[6] == Py_None) {
+        ends[0] = N;
+    } else {
+        if (!PyTuple_CheckExact(a[6])) return kNotPlain;
+        slices = PyTuple_GET_SIZE(a[6]);
+        if (slices < 1 || slices > EQUARX_ADAPTERS_MAX_SLICES) return kNotPlain;
+        for (Py_ssize_t i = 0; i < slices; ++i) {
+            long long end;
+            if (!integer(PyTuple_GET_ITEM(a[6], i), 0, INT32_MAX, end)) return kNotPlain;
+            ends[i] = end;
+        }
+    }
+    if (!da.of(a[1], kBF16) || da.t->dim() != 3 || !here(da.t) || !db.of(a[2], kBF16) || db.t->dim() != 3 || !here(db.t)) return kNotPlain;
+    const int64_t count = db.t->size(0), rank = db.t->size(2);
+    if (count > INT32_MAX || rank > INT32_MAX || db.t->size(1) != N || da.t->size(0) != count || da.t->size(1) != slices * rank ||
+        da.t->size(2) != K)
+        return kNotPlain;
+    if (!exactly(factors, a[3], kFloat, count) || !exactly(ids, a[4], kInt, M) || !ws.of(a[7])) return kNotPlain;
+    if (a[7] != Py_None && !here(plain(a[7]))) return kNotPlain;
+    return call(lib.equarx_adapters, x.ptr, x.row, da.ptr, db.ptr, static_cast<const float *>(factors.ptr), (int32_t)count, (int32_t)rank,
+                static_cast<const int32_t *>(ids.ptr), M, N, K, static_cast<const int64_t *>(ends), (int32_t)slices, out.ptr, out.row, ws.ptr,
+                ws.bytes);
+}
+
 // The Python-callable form of f: kArgs positional arguments; an exception from torch is "not plain" too.
 template <int kArgs, typename F>
 PyObject *enter(PyObject *const *a, Py_ssize_t count, F f)
@@ -616,6 +699,9 @@ ENTRY(7, equarx_cache_read, cache_read(a))
 ENTRY(13, equarx_cache_attention, cache_attention(a))
 ENTRY(11, equarx_norm, norm(a))
 ENTRY(12, equarx_norm_reduced, norm_reduced(a))
+ENTRY(3, equarx_pages_trim, pages_trim(a))
+ENTRY(9, equarx_pages_extend, pages_extend(a))
+ENTRY(8, equarx_adapters, adapters(a))
 #undef ENTRY
 
 // bind({name: address}): where the library's entry points are.
