@@ -592,7 +592,7 @@ size_t equarx_cache_attention_most_workspace_bytes(int32_t heads, int32_t dim, i
  *   lengths    int32 [sequences];
  *   free       int32 [pages]: a stack of the pages that nobody holds, free_count of
  *              them (int32 [1]), the top one last.
- *   sequences up to 2^20, width and pages up to 2^31 - 1, page from 1 to 65536, pages * page and
+ *   sequences and width up to 2^20, pages up to 2^30, page from 1 to 65536, pages * page and
  *   the table up to 2^40 (EQUARX_BAD_SHAPE).  A page is one sequence's.  Values out of range are taken
  *   as the nearest in it (lengths, free_count) or for no page (table, when it is given back).
  *

@@ -10,14 +10,14 @@ using namespace equarx;
 using namespace equarx::host;
 using namespace equarx::pages;
 
-constexpr int64_t kMostElements = (int64_t)1 << 40, kMostRows = (int64_t)1 << 30;
-constexpr int32_t kMostSequences = 1 << 20;
+constexpr int64_t kMostElements = (int64_t)1 << 40, kMostRows = (int64_t)1 << 30, kMostPages = (int64_t)1 << 30;
+constexpr int32_t kMostSequences = 1 << 20, kMostWidth = 1 << 20;
 
 int check_pages(const equarx_pages *p)
 {
     if (!p) return EQUARX_NULL_POINTER;
-    if (p->sequences < 0 || p->sequences > kMostSequences || p->width < 1 || p->width > INT32_MAX || p->pages < 1 ||
-        p->pages > INT32_MAX || p->page < 1 || p->page > 65536)
+    if (p->sequences < 0 || p->sequences > kMostSequences || p->width < 1 || p->width > kMostWidth || p->pages < 1 ||
+        p->pages > kMostPages || p->page < 1 || p->page > 65536)
         return EQUARX_BAD_SHAPE;
     if (p->pages > kMostElements / p->page) return EQUARX_BAD_SHAPE;
     if (p->sequences == 0) return EQUARX_OK;
@@ -27,7 +27,12 @@ int check_pages(const equarx_pages *p)
     return EQUARX_OK;
 }
 
-Pool pool_of(const equarx_pages &p) { return {p.table, p.lengths, p.free, p.free_count, p.width, p.pages, p.sequences, p.page}; }
+Pool pool_of(const equarx_pages &p)
+{
+    const int64_t room = p.width * p.page;
+    return {p.table, p.lengths, p.free, p.free_count, p.width, (int32_t)p.pages, p.sequences, (int32_t)(room < INT32_MAX ? room : INT32_MAX),
+            Divisor((uint32_t)p.page)};
+}
 
 void list_pages(const equarx_pages &p, Aliasing &mem)
 {
@@ -83,7 +88,7 @@ int equarx_pages_extend(const equarx_pages *pages, const int32_t *counts, int32_
     mem.writes(row_tags, (size_t)rows * 4);
     if (int st = mem.check()) return st;
     const Pool p = pool_of(*pages);
-    const Rows to{slots, positions, row_tags, tags, rows};
+    const Rows to{slots, positions, row_tags, tags, (int32_t)rows};
     const bool at_once = rows <= kToldAtOnce;
     ctx.launch(extend_kernel, 1, kTeam, p, counts, q_starts, granted, to, at_once);
     if (!at_once) ctx.launch(tell_kernel, (unsigned)((rows + 255) / 256), 256, p, static_cast<const int32_t *>(q_starts), to);

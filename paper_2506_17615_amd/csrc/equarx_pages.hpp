@@ -1,173 +1,258 @@
 // Device code of page tables: pages handed out to sequences from a stack and taken back, and the slots of new tokens.
 #pragma once
 
-#include "equarx_device.hpp"
+#include "equarx_rows.hpp"
 
 namespace equarx {
 namespace pages {
 
 struct Pool {
     Global<int32_t> table, lengths, free, free_count;
-    int64_t width, pages;
-    int32_t sequences, page;
+    int64_t width;
+    int32_t pages, sequences, most;     // most: tokens that the table has room for, as far as a length can say it
+    Divisor page;
 };
 
-// What a row is told: any may be null.
+// What a row is told: any but the slots may be null.
 struct Rows {
     Global<int64_t> slots;
     Global<int32_t> positions, row_tags;
     Global<const int32_t> tags;
-    int64_t rows;
+    int32_t rows;
 };
 
 constexpr int kTeam = 1024, kWaves = kTeam / 64;
 
-// The sum of v over the threads before this one, and over all: every thread of the workgroup calls it.
+// ---------------------------------------------------------------- sums over a workgroup
+// Up to 2^30 + 1, at which a sum stays: more than rows or pages there can be is as much as one more.
+
+constexpr uint32_t kMany = (1u << 30) + 1;
+
+__device__ __forceinline__ uint32_t add(uint32_t a, uint32_t b) { return a + b < kMany ? a + b : kMany; }
+
+// The other lane's value, zero where the row of sixteen has none.
+template <int kCtrl, int kRows = 0xf>
+__device__ __forceinline__ uint32_t shifted(uint32_t v)
+{
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, kCtrl, kRows, 0xf, false);
+}
+
+__device__ __forceinline__ uint32_t wave_scan(uint32_t v)
+{
+    v = add(v, shifted<0x111>(v));              // row_shr:1, 2, 4, 8
+    v = add(v, shifted<0x112>(v));
+    v = add(v, shifted<0x114>(v));
+    v = add(v, shifted<0x118>(v));
+    v = add(v, shifted<0x142, 0xa>(v));         // row_bcast:15 into rows 1 and 3, row_bcast:31 into rows 2 and 3
+    return add(v, shifted<0x143, 0xc>(v));
+}
+
 struct Scan {
-    int64_t before, all;
+    uint32_t upto, all;         // this thread's and those before it; all threads'
 };
 
-__device__ __forceinline__ Scan scan(int64_t v, int64_t *parts)
+// N sums at once, with two barriers; every thread of the workgroup calls it.
+template <int N>
+__device__ __forceinline__ void scan(const uint32_t (&v)[N], Scan (&s)[N], uint32_t (*parts)[kWaves])
 {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    int64_t sum = v;
 #pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-        const int64_t other = __shfl_up(sum, d);
-        if (lane >= d) sum += other;
+    for (int i = 0; i < N; ++i) s[i].upto = wave_scan(v[i]);
+    __syncthreads();                            // the last scan's parts have been read
+    if (lane == 63) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) parts[i][wave] = s[i].upto;
     }
-    __syncthreads();                    // parts may still be read from the scan before
-    if (lane == 63) parts[wave] = sum;
     __syncthreads();
-    Scan s{sum - v, 0};
 #pragma unroll
-    for (int i = 0; i < kWaves; ++i) {
-        if (i < wave) s.before += parts[i];
-        s.all += parts[i];
+    for (int i = 0; i < N; ++i) {
+        const uint32_t upto = wave_scan(lane < kWaves ? parts[i][lane] : 0);
+        s[i].all = (uint32_t)__builtin_amdgcn_readlane((int)upto, kWaves - 1);
+        if (wave > 0) s[i].upto = add(s[i].upto, (uint32_t)__builtin_amdgcn_readlane((int)upto, wave - 1));
     }
-    return s;
 }
 
-__device__ __forceinline__ int64_t pages_of(int64_t tokens, int32_t page) { return (tokens + page - 1) / page; }
+// ---------------------------------------------------------------- numbers as they are taken
 
-// A sequence's tokens as the table can hold them.
-__device__ __forceinline__ int64_t length_of(const Pool &p, int32_t b)
-{
-    const int64_t n = p.lengths[b], most = p.width * p.page;
-    return n < 0 ? 0 : n < most ? n : most;
-}
+__device__ __forceinline__ int32_t pages_of(const Pool &p, int32_t tokens) { return tokens > 0 ? (int32_t)p.page.of((uint32_t)tokens - 1) + 1 : 0; }
 
-// The free pages that there are: the stack's own count, within its array.
-__device__ __forceinline__ int64_t free_pages(const Pool &p)
+__device__ __forceinline__ int32_t within(int32_t v, int32_t most) { return v < 0 ? 0 : v < most ? v : most; }
+
+// The last i of [0, n) with from[i] <= at, from[0] being 0.
+template <typename T>
+__device__ __forceinline__ int32_t last_from(const T *from, int32_t n, uint32_t at)
 {
-    const int64_t n = p.free_count[0];
-    return n < 0 ? 0 : n < p.pages ? n : p.pages;
+    int32_t lo = 0;
+    for (int32_t step = 1 << 20; step > 0; step /= 2) {
+        if (step < n && lo + step < n && (uint32_t)from[lo + step] <= at) lo += step;
+    }
+    return lo;
 }
 
 // ---------------------------------------------------------------- back to a length
+// Latency is all there is to it: a thread a sequence for what is given back, then a thread an entry, 1024 at a time.
 
 __global__ __launch_bounds__(kTeam) void trim_kernel(const Pool p, Global<const int32_t> keep)
 {
-    __shared__ int64_t parts[kWaves];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    int64_t top = free_pages(p);
-    // a wave a sequence, sixteen sequences at a time; pages to the stack in order of the sequences and of their tokens
-    for (int32_t b0 = 0; b0 < p.sequences; b0 += kWaves) {
-        const int32_t b = b0 + wave;
-        const bool any = b < p.sequences;
-        const int64_t n = any ? length_of(p, b) : 0, wanted = any ? keep[b] : 0, kept = wanted < 0 ? 0 : wanted < n ? wanted : n;
-        const int64_t first = pages_of(kept, p.page), last = pages_of(n, p.page);
-        int32_t *const row = p.table + (any ? b : 0) * p.width;
-        auto is_page = [&](int64_t i) { return i < last && (uint32_t)row[i] < (uint64_t)p.pages; };
-        int64_t count = 0;
-        for (int64_t i0 = first; i0 < last; i0 += 64) count += __popcll(__ballot(is_page(i0 + lane)));
-        const Scan s = scan(lane == 0 ? count : 0, parts);
-        int64_t to = top + __shfl(s.before, 0);
-        top += s.all;
-        for (int64_t i0 = first; i0 < last; i0 += 64) {
-            const int64_t i = i0 + lane;
-            const bool real = is_page(i);
-            const uint64_t mask = __ballot(real);
-            const int64_t place = to + __popcll(mask & (((uint64_t)1 << lane) - 1));
-            if (real && place < p.pages) p.free[place] = row[i];        // a page given back twice has no room at the last
-            if (i < last) row[i] = -1;
-            to += __popcll(mask);
+    __shared__ uint32_t parts[1][kWaves], from[kTeam];
+    __shared__ int32_t first_of[kTeam];
+    const int i = threadIdx.x;
+    int64_t top = within(p.free_count[0], p.pages);
+    for (int32_t b0 = 0; b0 < p.sequences; b0 += kTeam) {
+        const int32_t b = b0 + i, here = p.sequences - b0 < kTeam ? p.sequences - b0 : kTeam;
+        int32_t n = 0, kept = 0;
+        if (b < p.sequences) {
+            n = within(p.lengths[b], p.most);
+            kept = within(keep[b], n);
         }
-        if (any && lane == 0) p.lengths[b] = (int32_t)kept;
+        const int32_t first = pages_of(p, kept), last = pages_of(p, n);
+        const uint32_t gone[1] = {(uint32_t)(last - first)};
+        Scan s[1];
+        scan(gone, s, parts);
+        from[i] = s[0].upto - gone[0];
+        first_of[i] = first;
+        if (b < p.sequences) p.lengths[b] = kept;
+        const uint32_t all = s[0].all;
+        __syncthreads();
+        for (uint32_t e0 = 0; e0 < all; e0 += kTeam) {
+            const uint32_t e = e0 + i;
+            int32_t page = -1;
+            if (e < all) {
+                const int32_t q = last_from(from, here, e);
+                int32_t *const entry = p.table + (int64_t)(b0 + q) * p.width + first_of[q] + (e - from[q]);
+                page = *entry;
+                *entry = -1;
+            }
+            const uint32_t real[1] = {(uint32_t)page < (uint32_t)p.pages ? 1u : 0u};
+            scan(real, s, parts);
+            const int64_t place = top + s[0].upto - 1;
+            if (real[0] && place < p.pages) p.free[place] = page;       // a page given back twice has no room at the last
+            top += s[0].all;
+        }
+        __syncthreads();
     }
-    if (threadIdx.x == 0) p.free_count[0] = (int32_t)(top < p.pages ? top : p.pages);
+    if (i == 0) p.free_count[0] = (int32_t)(top < p.pages ? top : p.pages);
 }
 
 // ---------------------------------------------------------------- new tokens
 
-// What row `row` is told, q_starts and the table being complete; `count` the rows that are a sequence's.
-__device__ __forceinline__ void tell_row(const Pool &p, const Rows &to, const int32_t *q_starts, const int32_t *lengths, int64_t row, int64_t count)
+// What row `row` of sequence b is told: `begin` the sequence's first row, `n` its tokens before the step.
+__device__ __forceinline__ void tell_row(const Pool &p, const Rows &to, int32_t row, int32_t b, int32_t begin, int32_t n)
 {
-    int64_t slot = -1;
-    int32_t position = -1, tag = -1;
-    if (row < count) {
-        int32_t lo = 0, hi = p.sequences;               // the last sequence that begins at or before the row
-        while (hi - lo > 1) {
-            const int32_t mid = lo + (hi - lo) / 2;
-            if (q_starts[mid] <= row) lo = mid; else hi = mid;
-        }
-        const int64_t t = lengths[lo] - (q_starts[lo + 1] - row);
-        const int64_t entry = p.table[lo * p.width + t / p.page];
-        if (entry >= 0 && entry < p.pages) slot = entry * p.page + t % p.page;
-        position = (int32_t)t;
-        if (to.row_tags.address) tag = to.tags[lo];
-    }
-    if (to.slots.address) to.slots[row] = slot;
-    if (to.positions.address) to.positions[row] = position;
-    if (to.row_tags.address) to.row_tags[row] = tag;
+    const int32_t t = n + row - begin, at = (int32_t)p.page.of((uint32_t)t), page = (int32_t)p.page.d;
+    const int32_t entry = p.table[b * p.width + at];
+    to.slots[row] = (uint32_t)entry < (uint32_t)p.pages ? (int64_t)entry * page + (t - at * page) : -1;
+    if (to.positions.address) to.positions[row] = t;
+    if (to.row_tags.address) to.row_tags[row] = to.tags[b];
 }
 
-__global__ __launch_bounds__(kTeam) void extend_kernel(const Pool p, Global<const int32_t> counts, Global<int32_t> q_starts,
-                                                          Global<int32_t> granted, const Rows to, int32_t tell)
+__device__ __forceinline__ void tell_nothing(const Rows &to, int32_t row)
 {
-    __shared__ int64_t parts[kWaves];
-    const int64_t free = free_pages(p);
-    int64_t rows = 0, wanted_pages = 0, taken = 0, granted_rows = 0;      // of the sequences before this thousand
+    to.slots[row] = -1;
+    if (to.positions.address) to.positions[row] = -1;
+    if (to.row_tags.address) to.row_tags[row] = -1;
+}
+
+// One workgroup decides and hands out.  A thread a sequence; one scan says what all of them want, and if rows and stack have it, that is
+// what they get; else two more say who goes without.  Then a thread an entry of the table, and, with `tell`, a thread a row.
+__global__ __launch_bounds__(kTeam) void extend_kernel(const Pool p, Global<const int32_t> counts, Global<int32_t> q_starts,
+                                                       Global<int32_t> granted, const Rows to, int32_t tell)
+{
+    __shared__ uint32_t parts[2][kWaves], from[kTeam];
+    __shared__ int32_t held_of[kTeam], begin_of[kTeam], had[kTeam];
+    const int i = threadIdx.x;
+    const int32_t free = within(p.free_count[0], p.pages);
+    uint32_t rows = 0, pages = 0, got_rows = 0;          // wanted by the sequences before these 1024, and got
+    int32_t taken = 0;
     for (int32_t b0 = 0; b0 < p.sequences; b0 += kTeam) {
-        const int32_t b = b0 + (int32_t)threadIdx.x;
-        const bool any = b < p.sequences;
-        const int64_t n = any ? length_of(p, b) : 0;
-        int64_t want = any ? counts[b] : 0;
-        if (want < 0 || n + want > p.width * p.page || n + want > INT32_MAX) want = 0;
-        Scan s = scan(want, parts);
-        if (rows + s.before + want > to.rows) want = 0;
-        rows += s.all;
-        const int64_t held = pages_of(n, p.page);
-        int64_t need = pages_of(n + want, p.page) - held;
-        s = scan(need, parts);
-        const int64_t at = wanted_pages + s.before;
-        wanted_pages += s.all;
-        if (need > 0 && at + need > free) want = need = 0;
-        s = scan(need, parts);
-        taken += s.all;
-        int32_t *const row = p.table + (any ? b : 0) * p.width;
-        for (int64_t i = 0; i < need; ++i) row[held + i] = p.free[free - 1 - at - i];
-        s = scan(want, parts);
-        if (any) {
-            q_starts[b] = (int32_t)(granted_rows + s.before);
-            p.lengths[b] = (int32_t)(n + want);
+        const int32_t b = b0 + i, here = p.sequences - b0 < kTeam ? p.sequences - b0 : kTeam;
+        int32_t n = 0;
+        uint32_t want = 0;
+        if (b < p.sequences) {
+            n = within(p.lengths[b], p.most);
+            const int32_t count = counts[b];
+            if (count > 0 && count <= p.most - n) want = (uint32_t)count;
+        }
+        const int32_t held = pages_of(p, n);
+        uint32_t need = (uint32_t)(pages_of(p, n + (int32_t)want) - held);
+        Scan s[2];
+        scan<2>({want < kMany ? want : kMany, need}, s, parts);
+        uint32_t begin = got_rows + s[0].upto - want;                  // with all of them served
+        const bool enough = rows == got_rows && pages == (uint32_t)taken && add(rows, s[0].all) <= (uint32_t)to.rows &&
+                            add(pages, s[1].all) <= (uint32_t)free;
+        if (enough) {
+            rows = got_rows = rows + s[0].all;
+            pages += s[1].all;
+            taken = (int32_t)pages;
+        } else {
+            const uint32_t rows_upto = add(rows, s[0].upto);
+            rows = add(rows, s[0].all);
+            if (rows_upto > (uint32_t)to.rows) want = need = 0;
+            Scan some[1];
+            scan<1>({need}, some, parts);
+            const uint32_t pages_upto = add(pages, some[0].upto);
+            pages = add(pages, some[0].all);
+            if (need > 0 && pages_upto > (uint32_t)free) want = need = 0;
+            scan<2>({want, need}, s, parts);
+            begin = got_rows + s[0].upto - want;
+            got_rows += s[0].all;
+            taken += (int32_t)s[1].all;
+        }
+        if (b < p.sequences) {
+            q_starts[b] = (int32_t)begin;
+            p.lengths[b] = n + (int32_t)want;
             if (granted.address) granted[b] = (int32_t)want;
         }
-        granted_rows += s.all;
+        from[i] = s[1].upto - need;                     // of the entries that are handed out here
+        held_of[i] = held;
+        begin_of[i] = (int32_t)begin;
+        had[i] = n;
+        // the first entry's page: those before are the sequences' before these
+        const int32_t top = free - 1 - (taken - (int32_t)s[1].all);
+        const uint32_t all = s[1].all;
+        __syncthreads();
+        for (uint32_t e = i; e < all; e += kTeam) {
+            const int32_t q = last_from(from, here, e);
+            p.table[(int64_t)(b0 + q) * p.width + held_of[q] + (e - from[q])] = p.free[top - (int32_t)e];
+        }
+        __syncthreads();
+        if (tell) {
+            for (uint32_t row = (uint32_t)(got_rows - s[0].all) + i; row < got_rows; row += kTeam) {
+                const int32_t q = last_from(begin_of, here, row);
+                tell_row(p, to, (int32_t)row, b0 + q, begin_of[q], had[q]);
+            }
+            __syncthreads();
+        }
     }
-    if (threadIdx.x == 0) {
-        q_starts[p.sequences] = (int32_t)granted_rows;
-        p.free_count[0] = (int32_t)(free - taken);
+    if (i == 0) {
+        q_starts[p.sequences] = (int32_t)got_rows;
+        p.free_count[0] = free - taken;
     }
-    if (!tell) return;
-    __syncthreads();
-    for (int64_t row = threadIdx.x; row < to.rows; row += kTeam) tell_row(p, to, q_starts, p.lengths, row, granted_rows);
+    if (tell) {
+        for (int32_t row = (int32_t)got_rows + i; row < to.rows; row += kTeam) tell_nothing(to, row);
+    }
 }
 
+// Many rows, by workgroups of their own; the sequences' first rows come to LDS where they fit.
 __global__ __launch_bounds__(256) void tell_kernel(const Pool p, Global<const int32_t> q_starts, const Rows to)
 {
-    const int64_t row = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (row < to.rows) tell_row(p, to, q_starts, p.lengths, row, q_starts[p.sequences]);
+    constexpr int kFit = 1024;
+    __shared__ int32_t starts[kFit];
+    const int32_t row = (int32_t)(blockIdx.x * 256 + threadIdx.x);
+    const int32_t all = q_starts[p.sequences];
+    const bool fits = p.sequences <= kFit;
+    if (fits) {
+        for (int32_t i = threadIdx.x; i < p.sequences; i += 256) starts[i] = q_starts[i];
+        __syncthreads();
+    }
+    if (row >= to.rows) return;
+    if (row >= all) {
+        tell_nothing(to, row);
+        return;
+    }
+    const int32_t b = fits ? last_from(starts, p.sequences, (uint32_t)row) : last_from((const int32_t *)q_starts, p.sequences, (uint32_t)row);
+    const int32_t begin = q_starts[b];
+    tell_row(p, to, row, b, begin, p.lengths[b] - (q_starts[b + 1] - begin));
 }
 
 }  // namespace pages

@@ -24,9 +24,9 @@ def _pages(**changes):
     return ctypes.byref(eq._CPages(**fields))
 
 
-BAD = [(SHAPE, dict(sequences=-1)), (SHAPE, dict(sequences=(1 << 20) + 1)), (SHAPE, dict(width=0)), (SHAPE, dict(width=1 << 31)),
-       (SHAPE, dict(pages=0)), (SHAPE, dict(pages=1 << 31)), (SHAPE, dict(page=0)), (SHAPE, dict(page=-16)), (SHAPE, dict(page=65537)),
-       (SHAPE, dict(pages=1 << 30, page=2048)), (SHAPE, dict(sequences=1 << 20, width=1 << 21)), (NULL, dict(table=None)),
+BAD = [(SHAPE, dict(sequences=-1)), (SHAPE, dict(sequences=(1 << 20) + 1)), (SHAPE, dict(width=0)), (SHAPE, dict(width=(1 << 20) + 1)),
+       (SHAPE, dict(pages=0)), (SHAPE, dict(pages=(1 << 30) + 1)), (SHAPE, dict(page=0)), (SHAPE, dict(page=-16)), (SHAPE, dict(page=65537)),
+       (SHAPE, dict(pages=1 << 30, page=2048)), (NULL, dict(table=None)),
        (NULL, dict(lengths=None)), (NULL, dict(free=None)), (NULL, dict(free_count=None)), (ALIGN, dict(table=P[0] + 2)),
        (ALIGN, dict(lengths=P[1] + 1)), (ALIGN, dict(free=P[2] + 2)), (ALIGN, dict(free_count=P[3] + 2)), (SHAPE, dict(lengths=P[0] + 3196)),
        (SHAPE, dict(free=P[1])), (SHAPE, dict(free_count=P[2] + 3996))]
