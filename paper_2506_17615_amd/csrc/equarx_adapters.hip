@@ -36,51 +36,75 @@ int check_rows(int64_t rows, int64_t cols, int64_t stride)
 inline size_t row_bytes(int64_t rows, int64_t cols, int64_t stride) { return (size_t)((rows - 1) * stride + cols) * 2; }
 
 // How a call is cut, by its sizes alone.
-constexpr int64_t kWorkgroups = 1024;
-
 struct Cut {
+    bool few;               // items are found by those who take them
     int tile;               // rows of an item, at most
     int64_t items;          // at most
-    int32_t rank_tiles, piece, splits;
-    size_t order, list, count, bytes;       // of the workspace: t from 0 on
+    int32_t rank_tiles, piece, splits, chunks;
+    size_t order, list, bytes;              // of the workspace: t from 0 on
 };
+
+// Rows that are taken together, rows of A and waves of a workgroup.
+struct FewRows {
+    static constexpr int RT = 1, QT = 1, W = 8;
+};
+struct ManyRows {
+    static constexpr int RT = 4, QT = 4, W = 8;
+};
+
+constexpr int64_t kTallRows = 2048, kMostSplits = 8, kWorkgroupsOfFew = 512, kWorkgroupsOfMany = 256, kWorkgroupsOfColumns = 512;
 
 Cut cut_of(const Sizes &z)
 {
     Cut c{};
     const int64_t R = (int64_t)z.rank * z.slices, groups = z.M < z.adapters ? z.M : z.adapters;
-    c.tile = z.M >= 32 * groups ? 64 : 16;
-    c.items = z.M / c.tile + groups;
-    c.rank_tiles = (int32_t)((R + kRankTile - 1) / kRankTile);
-    const int64_t most = (z.K + kWaveSteps - 1) / kWaveSteps;
+    const bool tall = z.M >= 32 * groups && z.M >= kTallRows;
+    c.few = z.M <= kFewRows;
+    c.tile = tall ? 64 : 16;
+    c.items = c.few ? z.M : z.M / c.tile + groups;
+    const int rank_tile = 16 * (tall ? ManyRows::QT : FewRows::QT), waves = tall ? ManyRows::W : FewRows::W;
+    c.rank_tiles = (int32_t)((R + rank_tile - 1) / rank_tile);
+    const int64_t steps = (z.K + kStep - 1) / kStep;
     auto limited = [](int64_t v, int64_t hi) { return v < 1 ? 1 : v < hi ? v : hi; };
-    const int64_t splits = limited(kWorkgroups / (c.items * c.rank_tiles), limited(most, 32));
-    c.piece = (int32_t)((most + splits - 1) / splits * kWaveSteps);
+    const int64_t busy = (z.M / c.tile + groups) * c.rank_tiles;
+    const int64_t splits = limited((tall ? kWorkgroupsOfMany : kWorkgroupsOfFew) / busy, limited((steps + waves - 1) / waves, kMostSplits));
+    c.piece = (int32_t)((steps + splits - 1) / splits * kStep);
     c.splits = (int32_t)((z.K + c.piece - 1) / c.piece);
-    // room for the partial sums of this many rows or fewer: of m rows in more than one split there are at most 64 kWorkgroups / rank_tiles
-    const int64_t bound = 64 * kWorkgroups / c.rank_tiles, cut_rows = z.M * limited(most, 32);
+    // columns of a workgroup: as many as leave enough workgroups
+    c.chunks = (int32_t)limited((z.M / c.tile + groups) * ((z.N + kChunk - 1) / kChunk) / kWorkgroupsOfColumns, 8);
+    // Room for the partial sums of this many rows or fewer: of m rows in more than one split, a split has 64 * 512 at most.
+    const int64_t bound = 64 * kWorkgroupsOfFew, cut_rows = z.M * kMostSplits;
     const int64_t rows = z.M > (cut_rows < bound ? cut_rows : bound) ? z.M : (cut_rows < bound ? cut_rows : bound);
     c.order = round_up((size_t)(rows * R) * sizeof(float), kWorkspaceAlign);
-    c.list = c.order + round_up((size_t)z.M * sizeof(int32_t), kWorkspaceAlign);
-    c.count = c.list + round_up((size_t)(z.M / 16 + groups) * sizeof(Item), kWorkspaceAlign);
-    c.bytes = c.count + kWorkspaceAlign;
+    // items of sixteen rows, or of 64 and fewer
+    const int64_t most_items = z.M / 16 + groups + kFewRows;
+    c.list = c.order + round_up((size_t)(z.M + 64 * groups + 16 * kFewRows) * sizeof(int32_t), kWorkspaceAlign);
+    c.bytes = c.list + round_up((size_t)most_items * sizeof(Item), kWorkspaceAlign);
     return c;
 }
 
-template <int RT>
+template <typename S, bool kFew>
 void launch(const Sizes &z, const Cut &c, const uint16_t *x, int64_t x_stride, const uint16_t *a, const uint16_t *b, const float *factors,
             const int32_t *ids, const Slices &cut, uint16_t *out, int64_t out_stride, uint8_t *workspace, LaunchCtx &ctx)
 {
     float *const t = reinterpret_cast<float *>(workspace);
-    int32_t *const order = reinterpret_cast<int32_t *>(workspace + c.order), *const count = reinterpret_cast<int32_t *>(workspace + c.count);
+    int32_t *const order = reinterpret_cast<int32_t *>(workspace + c.order);
     Item *const items = reinterpret_cast<Item *>(workspace + c.list);
     const int32_t R = z.rank * z.slices;
-    ctx.launch(group_kernel, 1, 1024, ids, z.M, z.adapters, c.tile, order, items, count);
-    ctx.launch3d(shrink_kernel<RT>, (unsigned)c.items, (unsigned)c.rank_tiles, (unsigned)c.splits, 256, x, x_stride, a, t, z.M, z.K, R, c.piece,
-                 static_cast<const int32_t *>(order), static_cast<const Item *>(items), static_cast<const int32_t *>(count));
-    ctx.launch2d(expand_kernel<RT>, (unsigned)c.items, (unsigned)cut.first_chunk[z.slices], 256, out, out_stride, b, factors,
-                 static_cast<const float *>(t), z.M, z.N, z.rank, z.slices, c.splits, static_cast<const int32_t *>(order),
-                 static_cast<const Item *>(items), static_cast<const int32_t *>(count), cut);
+    if (!kFew) ctx.launch(group_kernel, 1, 1024, ids, z.M, z.adapters, c.tile, order, items, c.items);
+    ctx.launch3d(shrink_kernel<S::RT, S::QT, S::W, kFew>, (unsigned)c.items, (unsigned)c.rank_tiles, (unsigned)c.splits, 64 * S::W, x, x_stride, a,
+                 t, z.M, z.K, R, c.piece, order, items, ids, z.adapters);
+    auto expand = [&](auto kernel) {
+        ctx.launch2d(kernel, (unsigned)c.items, (unsigned)cut.first_chunk[z.slices], 256, out, out_stride, b, factors, static_cast<const float *>(t),
+                     z.M, z.N, z.rank, z.slices, c.splits, c.chunks, static_cast<const int32_t *>(order), static_cast<const Item *>(items), cut);
+    };
+    if (z.rank <= 32) {
+        expand(expand_kernel<16 * S::RT, 1>);
+    } else if (z.rank <= 64) {
+        expand(expand_kernel<16 * S::RT, 2>);
+    } else {
+        expand(expand_kernel<16 * S::RT, 4>);
+    }
 }
 
 }  // namespace
@@ -102,12 +126,8 @@ int equarx_adapters(const void *x_bf16, int64_t x_stride, const void *a_bf16, co
     const Sizes z{M, N, K, rank, slices, adapters};
     if (int st = check_sizes(z)) return st;
     if (!slice_ends) return EQUARX_NULL_POINTER;
-    Slices cut{};
     for (int32_t s = 0; s < slices; ++s) {
-        const int64_t from = s == 0 ? 0 : slice_ends[s - 1];
-        if (slice_ends[s] < from || slice_ends[s] > N || (s + 1 == slices && slice_ends[s] != N)) return EQUARX_BAD_SHAPE;
-        cut.first_column[s + 1] = (int32_t)slice_ends[s];
-        cut.first_chunk[s + 1] = cut.first_chunk[s] + (int32_t)((slice_ends[s] - from + kChunk - 1) / kChunk);
+        if (slice_ends[s] < (s == 0 ? 0 : slice_ends[s - 1]) || slice_ends[s] > N || (s + 1 == slices && slice_ends[s] != N)) return EQUARX_BAD_SHAPE;
     }
     if (M == 0 || N == 0) return EQUARX_OK;
     if (int st = check_rows(M, N, out_stride)) return st;
@@ -132,7 +152,14 @@ int equarx_adapters(const void *x_bf16, int64_t x_stride, const void *a_bf16, co
     if (K > 0) mem.writes(workspace, c.bytes);
     if (int st = mem.check()) return st;
     if (K == 0) return EQUARX_OK;
-    (c.tile == 64 ? launch<4> : launch<1>)(z, c, static_cast<const uint16_t *>(x_bf16), x_stride, static_cast<const uint16_t *>(a_bf16),
+    Slices cut{};
+    const int64_t width = (int64_t)c.chunks * kChunk;
+    for (int32_t s = 0; s < slices; ++s) {
+        const int64_t columns = slice_ends[s] - (s == 0 ? 0 : slice_ends[s - 1]);
+        cut.first_column[s + 1] = (int32_t)slice_ends[s];
+        cut.first_chunk[s + 1] = cut.first_chunk[s] + (int32_t)((columns + width - 1) / width);
+    }
+    (c.few ? launch<FewRows, true> : c.tile == 64 ? launch<ManyRows, false> : launch<FewRows, false>)(z, c, static_cast<const uint16_t *>(x_bf16), x_stride, static_cast<const uint16_t *>(a_bf16),
                                            static_cast<const uint16_t *>(b_bf16), factors, ids, cut, static_cast<uint16_t *>(out_bf16),
                                            out_stride, static_cast<uint8_t *>(workspace), ctx);
     return ctx.status();
