@@ -67,6 +67,12 @@ Outputs outputs_of(const equarx_norm_outputs &to)
     return {static_cast<uint16_t *>(to.out_bf16), to.out_stride, to.codes, to.scales, to.mx4_codes, to.mx4_scales, to.block};
 }
 
+// Do all rows of the residual stream and of the output begin on sixteen bytes?
+bool in_units(const Inputs &in, const Outputs &to)
+{
+    return (!in.residual.address || in.residual_stride % 8 == 0) && (!to.out.address || to.out_stride % 8 == 0);
+}
+
 // The same from row `at` on.
 void advance(Inputs &in, Outputs &to, int64_t at, int64_t cols)
 {
@@ -83,12 +89,18 @@ void advance(Inputs &in, Outputs &to, int64_t at, int64_t cols)
     }
 }
 
-template <int L_, int K_>
+// From so many elements on bf16 outputs are written past the caches, which would not hold them for the next call as they would a decode
+// step's.  Measured on MI355X, us with ordinary stores -> past the caches: 4096 x 5376 32.1 -> 29.2, 16384 x 1024 23.1 -> 20.4, 1024 x 5376
+// 9.6 -> 9.1, 65536 x 128 8.4 -> 8.1.
+constexpr int64_t kStreamFrom = (int64_t)4 << 20;
+
+template <int L_, int K_, int A_ = 1>
 struct Cut {
-    static constexpr int L = L_, K = K_;
+    static constexpr int L = L_, K = K_, A = A_;
 };
 
-// f(cut) with the lanes that have a row, and their units.
+// f(cut) with the lanes that have a row, and their units: the fewest lanes, four waves at most while they hold a row in registers, since what counts is
+// how many rows are on their way.
 template <typename F>
 void with_cut(int64_t cols, F f)
 {
@@ -113,6 +125,46 @@ void with_cut(int64_t cols, F f)
     }
 }
 
+
+// Few rows of partial sums: sixteen waves a row, and up to sixteen partial sums asked for at once; what is left is the arithmetic of the chain
+// on as many CUs as there are rows, 0.4 us a partial sum of 64 x 5376.  Many: as other rows, the partial sums one after the other, past the
+// caches (8 of 4096 x 5376: 96.6 us with ordinary loads, 81.4 without, 79 with the output's stores past them too: 6.1 TB/s).  Measured on MI355X, us one
+// way and the other, 5376 columns:
+//     rows      P = 4            8               16
+//     128     7.5    5.4          --         19.1   11.2
+//     256     8.6    6.8     12.4    9.4     20.1   14.2
+//     512    11.4   10.9     13.3   14.7     19.8   23.2
+//     1024   17.9   16.8     22.9   28.6     36.7     --
+template <typename F>
+void with_reduced_cut(int64_t rows, int64_t cols, int P, F f)
+{
+    if (rows > (P <= 4 ? 1024 : 256) || cols <= 64 * 16) {
+        with_cut(cols, f);
+    } else if (cols > 1024 * 16) {
+        f(Cut<1024, 4, 4>{});
+    } else if (cols > 1024 * 8) {
+        f(Cut<1024, 2, 8>{});
+    } else if (P <= 4) {
+        f(Cut<1024, 1, 4>{});
+    } else if (P <= 8) {
+        f(Cut<1024, 1, 8>{});
+    } else {
+        f(Cut<1024, 1, 16>{});
+    }
+}
+
+// Up to a row for every CU a row has a workgroup of sixteen waves, a unit a lane: 256 x 8192 5.3 -> 4.8 us, 1 x 8192 4.7 -> 4.4; 512 rows gain nothing,
+// 1024 x 5376 loses (10.2 -> 10.7).
+template <typename F>
+void with_rows_cut(int64_t rows, int64_t cols, F f)
+{
+    if (rows <= 256 && cols > 256 * 8 && cols <= 1024 * 8) {
+        f(Cut<1024, 1>{});
+    } else {
+        with_cut(cols, f);
+    }
+}
+
 // f(first row, rows) for launches of at most 2^20 workgroups.
 template <int L, typename F>
 void in_row_pieces(int64_t rows, F f)
@@ -130,8 +182,9 @@ unsigned workgroups(int64_t rows)
 template <int B>
 void launch_reduced(const PartialTable &partials, int P, int64_t rows, int64_t cols, const Inputs &in, const Outputs &to, LaunchCtx &ctx)
 {
-    with_cut(cols, [&](auto cut) {
-        constexpr int L = decltype(cut)::L, K = decltype(cut)::K;
+    with_reduced_cut(rows, cols, P, [&](auto cut) {
+        constexpr int L = decltype(cut)::L, K = decltype(cut)::K, A = decltype(cut)::A;
+        const bool whole = in_units(in, to), streams = A == 1 && rows * cols >= kStreamFrom;
         if constexpr (L * 8 >= B) {                             // as cols >= B
             in_row_pieces<L>(rows, [&](int64_t at, int64_t count) {
                 Inputs i = in;
@@ -139,7 +192,8 @@ void launch_reduced(const PartialTable &partials, int P, int64_t rows, int64_t c
                 advance(i, o, at, cols);
                 PartialTable tab = partials;
                 for (int j = 0; j < kMaxPartials; ++j) tab.x[j] += at * cols;
-                ctx.launch(reduced_kernel<B, L, K>, workgroups<L>(count), Place<L>::T, P, count, cols, i, o, tab);
+                ctx.launch(!whole ? reduced_kernel<B, L, K, A, false, false> : streams ? reduced_kernel<B, L, K, A, true, A == 1> : reduced_kernel<B, L, K, A, true, false>,
+                           workgroups<L>(count), Place<L>::T, P, count, cols, i, o, tab);
             });
         }
     });
@@ -163,13 +217,15 @@ int equarx_norm(const void *x_bf16, int64_t x_stride, void *residual_bf16, int64
     if (int st = check_norm(residual_bf16, residual_stride, weight_bf16, rows, cols, eps, flags, outputs, mem)) return st;
     const Inputs in = inputs_of(residual_bf16, residual_stride, weight_bf16, eps, flags);
     const Outputs to = outputs_of(*outputs);
-    with_cut(cols, [&](auto cut) {
+    const bool whole = cols % 8 == 0 && x_stride % 8 == 0 && in_units(in, to);
+    with_rows_cut(rows, cols, [&](auto cut) {
         constexpr int L = decltype(cut)::L, K = decltype(cut)::K;
         in_row_pieces<L>(rows, [&](int64_t at, int64_t count) {
             Inputs i = in;
             Outputs o = to;
             advance(i, o, at, cols);
-            ctx.launch(cols % 8 ? rows_kernel<L, K, true> : rows_kernel<L, K, false>, workgroups<L>(count), Place<L>::T,
+            ctx.launch(!whole ? rows_kernel<L, K, false, false> : rows * cols < kStreamFrom ? rows_kernel<L, K, true, false> : rows_kernel<L, K, true, true>,
+                       workgroups<L>(count), Place<L>::T,
                        static_cast<const uint16_t *>(x_bf16) + at * x_stride, x_stride, count, cols, i, o);
         });
     });

@@ -33,10 +33,50 @@ struct Place {
     int lane;
     bool any;
     __device__ __forceinline__ Place(int64_t rows)
-        : row((int64_t)blockIdx.x * kRows + (kRows > 1 ? threadIdx.x / L : 0)), lane(threadIdx.x % L), any(row < rows)
     {
+        const int in = L < 64 ? threadIdx.x / L : __builtin_amdgcn_readfirstlane(threadIdx.x / L);     // a wave's row is a scalar
+        row = (int64_t)blockIdx.x * kRows + (kRows > 1 ? in : 0);
+        lane = threadIdx.x % L;
+        any = kRows == 1 || row < rows;
     }
 };
+
+// ---------------------------------------------------------------- units of a row
+// Where a wave has one row and all rows begin on sixteen bytes and end with a unit (kWhole), through a descriptor that ends with the row:
+// nothing is behind a condition, so that all loads of a thread are asked for together (behind one each the compiler waited for the first
+// two before it asked for the third: 4096 x 5376 to int8 42.5 us, 38.5 this way), and what is past the row's end is not read, zero, and not written.
+
+template <int L, bool kWhole>
+constexpr bool by_descriptor = kWhole && L >= 64;
+
+template <int L, int K, bool kWhole, int kPolicy = 0>
+__device__ __forceinline__ void load_units(const uint16_t *p, const Place<L> &at, int32_t cols, u32x4 (&v)[K])
+{
+    if constexpr (by_descriptor<L, kWhole>) {
+        const auto row = bounded(p, at.any ? cols * 2 : 0);
+#pragma unroll
+        for (int k = 0; k < K; ++k)
+            v[k] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(row, (at.lane + k * L) * 16, 0, kPolicy));
+    } else {
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            const int32_t col = (at.lane + k * L) * 8;
+            v[k] = u32x4{0, 0, 0, 0};
+            if (at.any && col < cols) v[k] = kWhole || cols < 8 ? load_row8(p, col, cols) : load_row8_back(p, col, cols);
+        }
+    }
+}
+
+template <int L, bool kWhole, int kPolicy = 0>
+__device__ __forceinline__ void store_unit(uint16_t *p, const Place<L> &at, int k, int32_t cols, const u32x4 &v)
+{
+    if constexpr (by_descriptor<L, kWhole>) {
+        __builtin_amdgcn_raw_buffer_store_b128(v, bounded(p, at.any ? cols * 2 : 0), (at.lane + k * L) * 16, 0, kPolicy);
+    } else {
+        const int32_t col = (at.lane + k * L) * 8;
+        if (at.any && col < cols) store_row8(p, col, cols, v);
+    }
+}
 
 // ---------------------------------------------------------------- a row's sum
 
@@ -149,7 +189,7 @@ __device__ __forceinline__ uint32_t mx4_of(const float (&y)[8], uint32_t top, ui
 // The sum is taken in 64 bits, where its order does not reach i's last bit (but for one row in 10^8): the codes of the
 // quantized forms, each of which one bit of i can tip over, depend on the row alone, not on how it was cut.  bf16, int8 and 4 bits
 // are each rounded from y itself, once.
-template <int L, int K, bool kTail>
+template <int L, int K, bool kWhole, bool kStreams>
 __device__ __forceinline__ void finish_row(const Place<L> &at, u32x4 (&h)[K], const u32x4 (&r)[K], const u32x4 (&w)[K], int64_t cols,
                                            const Inputs &in, const Outputs &to)
 {
@@ -163,16 +203,8 @@ __device__ __forceinline__ void finish_row(const Place<L> &at, u32x4 (&h)[K], co
             widen_bf16x8(r[k], g);
 #pragma unroll
             for (int i = 0; i < 4; ++i) h[k][i] = narrow_bf16x2(f[2 * i] + g[2 * i], f[2 * i + 1] + g[2 * i + 1]);
+            store_unit<L, kWhole>(in.residual + at.row * in.residual_stride, at, k, (int32_t)cols, h[k]);
             widen_bf16x8(h[k], f);
-            const int64_t col = (int64_t)(at.lane + k * L) * 8;
-            uint16_t *const row = in.residual + at.row * in.residual_stride;
-            if (at.any && col < cols) {
-                if (kTail) {
-                    store_row8(row, col, cols, h[k]);
-                } else {
-                    *reinterpret_cast<u32x4_anywhere *>(row + col) = h[k];
-                }
-            }
         }
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
@@ -193,24 +225,15 @@ __device__ __forceinline__ void finish_row(const Place<L> &at, u32x4 (&h)[K], co
             if (in.one_plus) g[i] += 1.0f;
             y[i] = y[i] * inverse;
             if (in.weight.address) y[i] = y[i] * g[i];
-            if (kTail && col + i >= cols) y[i] = 0.0f;              // 0 * infinity is not a row's
-        }
-        if (!kTail && col >= cols) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) y[i] = 0.0f;
+            if (kWhole ? col >= cols : col + i >= cols) y[i] = 0.0f;        // 0 * infinity is not the row's
         }
         const bool real = at.any && col < cols;
-        if (to.out.address && real) {
-            uint16_t *const row = to.out + at.row * to.out_stride;
+        if (to.out.address) {
             const u32x4 v = {narrow_bf16x2(y[0], y[1]), narrow_bf16x2(y[2], y[3]), narrow_bf16x2(y[4], y[5]), narrow_bf16x2(y[6], y[7])};
-            if (kTail) {
-                store_row8(row, col, cols, v);
-            } else {
-                *reinterpret_cast<u32x4_anywhere *>(row + col) = v;
-            }
+            store_unit<L, kWhole, kStreams ? kNonTemporal : 0>(to.out + at.row * to.out_stride, at, k, (int32_t)cols, v);
         }
         const uint32_t top = top_of(y);
-        if (!kTail && to.codes.address) {                           // whole blocks a row: whole units
+        if (to.codes.address) {                                     // whole blocks a row: whole units
             float scale;
             const u32x2 codes = int8_of(y, top, to.block, scale);
             if (real) {
@@ -235,60 +258,65 @@ __device__ __forceinline__ void finish_row(const Place<L> &at, u32x4 (&h)[K], co
 
 // ---------------------------------------------------------------- rows of a tensor
 
-// A thread's K units of a row; zeros past its end and where there is no row.
-template <int L, int K, bool kTail>
-__device__ __forceinline__ void load_units(const uint16_t *p, int lane, bool any, int64_t cols, u32x4 (&v)[K])
-{
-#pragma unroll
-    for (int k = 0; k < K; ++k) {
-        const int64_t col = (int64_t)(lane + k * L) * 8;
-        v[k] = u32x4{0, 0, 0, 0};
-        if (any && col < cols) v[k] = kTail ? load_row8(p, col, cols) : *reinterpret_cast<const u32x4_anywhere *>(p + col);
-    }
-}
-
-// kTail: rows whose last unit is not whole.
-template <int L, int K, bool kTail>
+// kStreams: a bf16 output that is written past the caches.
+template <int L, int K, bool kWhole, bool kStreams>
 __global__ __launch_bounds__(Place<L>::T) void rows_kernel(Global<const uint16_t> x, int64_t x_stride, int64_t rows, int64_t cols,
                                                            const Inputs in, const Outputs to)
 {
     const Place<L> at(rows);
     u32x4 h[K], r[K], w[K];
-    load_units<L, K, kTail>(x + at.row * x_stride, at.lane, at.any, cols, h);
-    if (in.residual.address) load_units<L, K, kTail>(in.residual + at.row * in.residual_stride, at.lane, at.any, cols, r);
-    if (in.weight.address) load_units<L, K, kTail>(in.weight, at.lane, true, cols, w);
+    load_units<L, K, kWhole>(x + at.row * x_stride, at, (int32_t)cols, h);
+    if (in.residual.address) load_units<L, K, kWhole>(in.residual + at.row * in.residual_stride, at, (int32_t)cols, r);
+    if (in.weight.address) load_units<L, K, kWhole>(in.weight, at, (int32_t)cols, w);
     loads_first();
-    finish_row<L, K, kTail>(at, h, r, w, cols, in, to);
+    finish_row<L, K, kWhole, kStreams>(at, h, r, w, cols, in, to);
 }
 
 // ---------------------------------------------------------------- rows that a reduction leaves
 // The chain of chain_kernel over a row's blocks, B / 8 lanes each, whole blocks a row; its last dequantization is rounded to
 // bf16, as equarx_reduce_fused writes it, and is the row that is normed.
 
-template <int B, int L, int K>
+// A: partials that are asked for together; of one at a time they are many, and read past the caches.  kWhole: of residual and output; the
+// partials and the weight always are.
+template <int B, int L, int K, int A, bool kWhole, bool kStreams>
 __global__ __launch_bounds__(Place<L>::T) void reduced_kernel(int P, int64_t rows, int64_t cols, const Inputs in, const Outputs to,
                                                               const PartialTable tab)
 {
     constexpr int G = B / kLaneElems;
     const Place<L> at(rows);
-    u32x4 h[K], r[K], w[K];
-    float t[K][8];
-    load_units<L, K, false>(tab.x[0] + at.row * cols, at.lane, at.any, cols, h);
-    if (in.residual.address) load_units<L, K, false>(in.residual + at.row * in.residual_stride, at.lane, at.any, cols, r);
-    if (in.weight.address) load_units<L, K, false>(in.weight, at.lane, true, cols, w);
+    u32x4 x[A][K], r[K] = {}, w[K] = {};
+    float t[K][8] = {};
+    // a wave behind the row's end has nothing to add up
+    const int wave_lane = __builtin_amdgcn_readfirstlane(at.lane & ~63);
+    const int batches = L > 64 && (int64_t)wave_lane * 8 >= cols ? 0 : P;
+    for (int j = 0; j < batches; j += A) {
 #pragma unroll
-    for (int k = 0; k < K; ++k) widen_bf16x8(h[k], t[k]);
-    for (int j = 1; j < P; ++j) {
-        load_units<L, K, false>(tab.x[j] + at.row * cols, at.lane, at.any, cols, h);
+        for (int a = 0; a < A; ++a) load_units<L, K, true, A == 1 ? kNonTemporal : 0>(tab.x[j + a] + at.row * cols, at, (int32_t)cols, x[a]);
+        if (j == 0) {
+            if (in.residual.address) load_units<L, K, kWhole>(in.residual + at.row * in.residual_stride, at, (int32_t)cols, r);
+            if (in.weight.address) load_units<L, K, true>(in.weight, at, (int32_t)cols, w);
+        }
+        if (A > 1) loads_first();
 #pragma unroll
-        for (int k = 0; k < K; ++k) {
-            float c[8], s, x[8];
-            quantize_lane_f<G>(t[k], c, s);
-            widen_bf16x8(h[k], x);
+        for (int a = 0; a < A; ++a) {
+            if (A > 1 && j + a >= P) break;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) t[k][i] = __builtin_fmaf(c[i], s, x[i]);
+            for (int k = 0; k < K; ++k) {
+                float f[8];
+                widen_bf16x8(x[a][k], f);
+                if (j + a == 0) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) t[k][i] = f[i];
+                    continue;
+                }
+                float c[8], s;
+                quantize_lane_f<G>(t[k], c, s);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) t[k][i] = __builtin_fmaf(c[i], s, f[i]);
+            }
         }
     }
+    u32x4 h[K];
 #pragma unroll
     for (int k = 0; k < K; ++k) {
         float c[8], s;
@@ -296,7 +324,7 @@ __global__ __launch_bounds__(Place<L>::T) void reduced_kernel(int P, int64_t row
 #pragma unroll
         for (int i = 0; i < 4; ++i) h[k][i] = narrow_bf16x2(c[2 * i] * s, c[2 * i + 1] * s);
     }
-    finish_row<L, K, false>(at, h, r, w, cols, in, to);
+    finish_row<L, K, kWhole, kStreams>(at, h, r, w, cols, in, to);
 }
 
 }  // namespace norm
