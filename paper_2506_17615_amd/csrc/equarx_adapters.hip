@@ -10,6 +10,21 @@ using namespace equarx;
 using namespace equarx::host;
 using namespace equarx::adapters;
 
+#ifndef EQX_RT
+#define EQX_RT 4
+#endif
+#ifndef EQX_W
+#define EQX_W 8
+#endif
+#ifndef EQX_WM
+#define EQX_WM 256
+#endif
+#ifndef EQX_WC
+#define EQX_WC 1024
+#endif
+#ifndef EQX_WF
+#define EQX_WF 512
+#endif
 constexpr int64_t kMostRows = (int64_t)1 << 24, kMostCols = (int64_t)1 << 22, kMostElements = (int64_t)1 << 40;
 
 struct Sizes {
@@ -40,28 +55,28 @@ struct Cut {
     bool few;               // items are found by those who take them
     int tile;               // rows of an item, at most
     int64_t items;          // at most
-    int32_t rank_tiles, piece, splits, chunks;
+    int32_t rank_tiles, piece, splits, columns, chunks;
     size_t order, list, bytes;              // of the workspace: t from 0 on
 };
 
 // Rows that are taken together, rows of A and waves of a workgroup.
 struct FewRows {
-    static constexpr int RT = 1, QT = 1, W = 8;
+    static constexpr int RT = 1, QT = 1, W = 8, D = 2;
 };
 struct ManyRows {
-    static constexpr int RT = 4, QT = 4, W = 8;
+    static constexpr int RT = EQX_RT, QT = 4, W = EQX_W, D = 1;
 };
 
-constexpr int64_t kTallRows = 2048, kMostSplits = 8, kWorkgroupsOfFew = 512, kWorkgroupsOfMany = 256, kWorkgroupsOfColumns = 512;
+constexpr int64_t kTallRows = 2048, kMostSplits = 8, kWorkgroupsOfFew = EQX_WF, kWorkgroupsOfMany = EQX_WM, kWorkgroupsOfColumns = EQX_WC;
 
 Cut cut_of(const Sizes &z)
 {
     Cut c{};
     const int64_t R = (int64_t)z.rank * z.slices, groups = z.M < z.adapters ? z.M : z.adapters;
-    const bool tall = z.M >= 32 * groups && z.M >= kTallRows;
+    const bool tall = z.M >= 32 * groups && z.M >= kTallRows && z.N >= 8;
     c.few = z.M <= kFewRows;
-    c.tile = tall ? 64 : 16;
-    c.items = c.few ? z.M : z.M / c.tile + groups;
+    c.tile = 16 * (tall ? ManyRows::RT : FewRows::RT);
+    c.items = c.few ? z.M : (z.M / c.tile + groups + 7) / 8 * 8;
     const int rank_tile = 16 * (tall ? ManyRows::QT : FewRows::QT), waves = tall ? ManyRows::W : FewRows::W;
     c.rank_tiles = (int32_t)((R + rank_tile - 1) / rank_tile);
     const int64_t steps = (z.K + kStep - 1) / kStep;
@@ -71,14 +86,15 @@ Cut cut_of(const Sizes &z)
     c.piece = (int32_t)((steps + splits - 1) / splits * kStep);
     c.splits = (int32_t)((z.K + c.piece - 1) / c.piece);
     // columns of a workgroup: as many as leave enough workgroups
-    c.chunks = (int32_t)limited((z.M / c.tile + groups) * ((z.N + kChunk - 1) / kChunk) / kWorkgroupsOfColumns, 8);
+    c.columns = tall ? 64 : 64 * kFewWaves;
+    c.chunks = (int32_t)limited((c.items * ((z.N + c.columns - 1) / c.columns) + kWorkgroupsOfColumns - 1) / kWorkgroupsOfColumns, 16);
     // Room for the partial sums of this many rows or fewer: of m rows in more than one split, a split has 64 * 512 at most.
     const int64_t bound = 64 * kWorkgroupsOfFew, cut_rows = z.M * kMostSplits;
     const int64_t rows = z.M > (cut_rows < bound ? cut_rows : bound) ? z.M : (cut_rows < bound ? cut_rows : bound);
     c.order = round_up((size_t)(rows * R) * sizeof(float), kWorkspaceAlign);
     // items of sixteen rows, or of 64 and fewer
-    const int64_t most_items = z.M / 16 + groups + kFewRows;
-    c.list = c.order + round_up((size_t)(z.M + 64 * groups + 16 * kFewRows) * sizeof(int32_t), kWorkspaceAlign);
+    const int64_t most_items = z.M / 16 + groups + kFewRows + 8;
+    c.list = c.order + round_up((size_t)(z.M + 64 * (groups + 8) + 16 * kFewRows) * sizeof(int32_t), kWorkspaceAlign);
     c.bytes = c.list + round_up((size_t)most_items * sizeof(Item), kWorkspaceAlign);
     return c;
 }
@@ -92,18 +108,17 @@ void launch(const Sizes &z, const Cut &c, const uint16_t *x, int64_t x_stride, c
     Item *const items = reinterpret_cast<Item *>(workspace + c.list);
     const int32_t R = z.rank * z.slices;
     if (!kFew) ctx.launch(group_kernel, 1, 1024, ids, z.M, z.adapters, c.tile, order, items, c.items);
-    ctx.launch3d(shrink_kernel<S::RT, S::QT, S::W, kFew>, (unsigned)c.items, (unsigned)c.rank_tiles, (unsigned)c.splits, 64 * S::W, x, x_stride, a,
+    ctx.launch3d(shrink_kernel<S::RT, S::QT, S::W, S::D, kFew>, (unsigned)c.items, (unsigned)c.rank_tiles, (unsigned)c.splits, 64 * S::W, x, x_stride, a,
                  t, z.M, z.K, R, c.piece, order, items, ids, z.adapters);
-    auto expand = [&](auto kernel) {
-        ctx.launch2d(kernel, (unsigned)c.items, (unsigned)cut.first_chunk[z.slices], 256, out, out_stride, b, factors, static_cast<const float *>(t),
-                     z.M, z.N, z.rank, z.slices, c.splits, c.chunks, static_cast<const int32_t *>(order), static_cast<const Item *>(items), cut);
-    };
-    if (z.rank <= 32) {
-        expand(expand_kernel<16 * S::RT, 1>);
-    } else if (z.rank <= 64) {
-        expand(expand_kernel<16 * S::RT, 2>);
+    const Expansion p{out, out_stride, b, factors, t, (int32_t)z.M, (int32_t)z.N, z.rank, z.slices, c.splits, c.chunks, c.tile, order, items, cut};
+    auto expand = [&](auto kernel) { ctx.launch2d(kernel, (unsigned)c.items, (unsigned)cut.first_chunk[z.slices], 256, p); };
+    if constexpr (S::RT > 1) {
+        expand(z.rank <= 32 ? expand_many_kernel<1> : z.rank <= 64 ? expand_many_kernel<2> : expand_many_kernel<4>);
     } else {
-        expand(expand_kernel<16 * S::RT, 4>);
+        expand(z.N < 8        ? expand_few_kernel<4, kFew, true>
+               : z.rank <= 32 ? expand_few_kernel<1, kFew, false>
+               : z.rank <= 64 ? expand_few_kernel<2, kFew, false>
+                              : expand_few_kernel<4, kFew, false>);
     }
 }
 
@@ -153,13 +168,13 @@ int equarx_adapters(const void *x_bf16, int64_t x_stride, const void *a_bf16, co
     if (int st = mem.check()) return st;
     if (K == 0) return EQUARX_OK;
     Slices cut{};
-    const int64_t width = (int64_t)c.chunks * kChunk;
+    const int64_t width = (int64_t)c.chunks * c.columns;
     for (int32_t s = 0; s < slices; ++s) {
         const int64_t columns = slice_ends[s] - (s == 0 ? 0 : slice_ends[s - 1]);
         cut.first_column[s + 1] = (int32_t)slice_ends[s];
         cut.first_chunk[s + 1] = cut.first_chunk[s] + (int32_t)((columns + width - 1) / width);
     }
-    (c.few ? launch<FewRows, true> : c.tile == 64 ? launch<ManyRows, false> : launch<FewRows, false>)(z, c, static_cast<const uint16_t *>(x_bf16), x_stride, static_cast<const uint16_t *>(a_bf16),
+    (c.few ? launch<FewRows, true> : c.tile != 16 ? launch<ManyRows, false> : launch<FewRows, false>)(z, c, static_cast<const uint16_t *>(x_bf16), x_stride, static_cast<const uint16_t *>(a_bf16),
                                            static_cast<const uint16_t *>(b_bf16), factors, ids, cut, static_cast<uint16_t *>(out_bf16),
                                            out_stride, static_cast<uint8_t *>(workspace), ctx);
     return ctx.status();

@@ -104,6 +104,13 @@ __global__ __launch_bounds__(1024) void group_kernel(Global<const int32_t> ids, 
     }
 }
 
+// What lanes of a wave hand each other through LDS needs no barrier, but the compiler has to leave it in order.
+__device__ __forceinline__ void in_wave_order()
+{
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
 // Few rows are brought together without a launch: item i is row i's, if every sixteenth of its adapter's rows, from the first on, is row i,
 // and has that row and the next fifteen.  Each wave finds that for itself, with lane l's rows l, 64 + l, ...
 constexpr int kFewRows = 256, kIdsPerLane = kFewRows / 64;
@@ -132,7 +139,8 @@ __device__ __forceinline__ int32_t find_item(const int32_t *ids, int32_t M, int3
     for (int q = 0; q < kIdsPerLane; ++q) {
         if (id[q] == mine && rank[q] >= before && rank[q] < before + 16) places[rank[q] - before] = q * 64 + lane;
     }
-    return places[lane % 16 < item.count ? lane % 16 : 0];      // its own wave's writes, in order
+    in_wave_order();
+    return places[lane % 16 < item.count ? lane % 16 : 0];
 }
 
 // ---------------------------------------------------------------- products of sixteen by sixteen
@@ -146,215 +154,384 @@ __device__ __forceinline__ v4f multiply(const u32x4 &a, const u32x4 &b, const v4
 
 __device__ __forceinline__ u32x4 load8(const uint16_t *p) { return *reinterpret_cast<const u32x4_anywhere *>(p); }
 
+// A lane's operand is sixteen bytes of a row, its neighbour's of the next row: loaded so, every lane is an access of the cache by itself (four a
+// cycle at 64 bytes a lane's quad would be one), and those bounded both kernels (4096 rows, rank 64: 18 and 32 us).  So rows come in whole
+// 128 bytes, eight lanes a row, and through LDS to the lanes that multiply; each wave has a place of its own there, and no barrier is needed.
+
+// Items of one adapter, which follow each other, go to one XCD: workgroups go round the eight, `x` of `count` (a multiple of eight) is
+// item x / 8 of the x % 8th eighth.
+__device__ __forceinline__ int32_t item_of(uint32_t x, uint32_t count) { return (int32_t)((x & 7) * (count / 8) + x / 8); }
+
 // ---------------------------------------------------------------- t = A x
 // A workgroup has an item's rows, 16 RT of them, 16 QT rows of A and a piece of k, of which its W waves take 64 in turn; their sums are
-// added in order through LDS.  Sums of the pieces go to t [split][M][R].
+// added in order through LDS.  Sums of the pieces go to t [split][M][R].  D: steps of a wave that are on their way.
 // kFew: items are found here, and the first workgroup of each writes it down for the launch that follows.
 
 constexpr int kStep = 64;
 
-template <int RT, int QT, int W, bool kFew>
+template <int RT, int QT, int W, int D, bool kFew>
 __global__ __launch_bounds__(64 * W) void shrink_kernel(Global<const uint16_t> x, int64_t x_stride, Global<const uint16_t> a, Global<float> t,
                                                         int32_t M, int32_t K, int32_t R, int32_t piece, Global<int32_t> order, Global<Item> items,
                                                         Global<const int32_t> ids, int32_t adapters)
 {
-    constexpr int T = 16 * RT, kPitch = QT * 16 + 4;
-    constexpr int U = RT == 1 ? 2 : 1;                          // steps whose loads are asked for together
-    __shared__ __align__(16) float sums[W][16][kPitch];
+    constexpr int T = 16 * RT, Q = 16 * QT, kPitch = Q + 4, kTile = (T + Q) * 2 * kStep;
+    constexpr int kSums = W * 16 * kPitch * 4, kAll = W * kTile > kSums ? W * kTile : kSums;
+    __shared__ __align__(16) uint8_t lds[kAll];
     __shared__ int32_t places[kFew ? W : 1][16];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l = lane & 15, g = lane >> 4;
+    const int32_t at = kFew ? (int32_t)blockIdx.x : item_of(blockIdx.x, gridDim.x);
     Item item;
-    int32_t row[RT];
     if constexpr (kFew) {
-        row[0] = find_item(ids, M, adapters, (int32_t)blockIdx.x, places[wave], item);
+        const int32_t row = find_item(ids, M, adapters, at, places[wave], item);
         if (blockIdx.y == 0 && blockIdx.z == 0 && wave == 0) {
-            if (lane == 0) items[blockIdx.x] = item;
-            if (lane < item.count) order[blockIdx.x * 16 + lane] = row[0];
+            if (lane == 0) items[at] = item;
+            if (lane < item.count) order[at * 16 + lane] = row;
         }
     } else {
-        item = items[blockIdx.x];
-#pragma unroll
-        for (int i = 0; i < RT; ++i) row[i] = order[blockIdx.x * T + (i * 16 + l < item.count ? i * 16 + l : 0)];
+        item = items[at];
     }
     if (item.count == 0) return;
-    const int32_t r0 = blockIdx.y * (16 * QT), k_from = blockIdx.z * piece, k_to = k_from + piece < K ? k_from + piece : K;
-    const uint16_t *xr[RT], *ar[QT];
+    const int32_t *const rows = kFew ? places[wave] : (const int32_t *)order + (int64_t)at * T;
+    const int32_t r0 = blockIdx.y * Q, k_from = blockIdx.z * piece, k_to = k_from + piece < K ? k_from + piece : K;
+    const int in = lane / 8, eighth = lane % 8;                 // of the rows that are loaded
+    const uint16_t *from[2 * (RT + QT)];
 #pragma unroll
-    for (int i = 0; i < RT; ++i) xr[i] = x + row[i] * x_stride;
+    for (int i = 0; i < 2 * RT; ++i) from[i] = x + rows[i * 8 + in < item.count ? i * 8 + in : 0] * x_stride;
 #pragma unroll
-    for (int q = 0; q < QT; ++q) {
-        const int32_t r = r0 + q * 16 + l < R ? r0 + q * 16 + l : R - 1;
-        ar[q] = a + ((int64_t)item.adapter * R + r) * K;
+    for (int i = 0; i < 2 * QT; ++i) {
+        const int32_t r = r0 + i * 8 + in < R ? r0 + i * 8 + in : R - 1;
+        from[2 * RT + i] = a + ((int64_t)item.adapter * R + r) * K;
     }
     struct Step {
-        u32x4 x[RT][2], a[QT][2];
+        u32x4 v[2 * (RT + QT)];
     };
-    auto load = [&](Step &to, int32_t k0) {
-        const int32_t k = k0 + g * 16;
-        auto each = [&](auto get) {
+    uint8_t *const mine = lds + wave * kTile;
+    auto put = [&](const Step &s) {                             // block b of row r in place b xor r / 2 % 8: sixteen rows' block is in all banks
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
-#pragma unroll
-                for (int i = 0; i < RT; ++i) to.x[i][j] = get(xr[i], k + 8 * j);
-#pragma unroll
-                for (int q = 0; q < QT; ++q) to.a[q][j] = get(ar[q], k + 8 * j);
-            }
-        };
-        if (k0 + kStep <= k_to) {
-            each([](const uint16_t *p, int32_t at) { return load8(p + at); });
-        } else if (k0 >= k_to) {
-            each([](const uint16_t *, int32_t) { return u32x4{0, 0, 0, 0}; });
-        } else if (K >= 8) {                                    // past the end zeros, in both
-            each([&](const uint16_t *p, int32_t at) { return load_row8_back(p, at, K); });
-        } else {
-            each([&](const uint16_t *p, int32_t at) { return load_row8(p, at, K); });
+        for (int i = 0; i < 2 * (RT + QT); ++i) {
+            const int row = i * 8 + in;
+            *reinterpret_cast<u32x4 *>(mine + row * (2 * kStep) + (eighth ^ (row >> 1 & 7)) * 16) = s.v[i];
         }
+        in_wave_order();
     };
     v4f sum[RT][QT] = {};
-    auto add = [&](const Step &s) {
+    auto add = [&]() {
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
+            u32x4 av[QT];
+            auto get = [&](int row) { return *reinterpret_cast<const u32x4 *>(mine + row * (2 * kStep) + ((j * 4 + g) ^ (row >> 1 & 7)) * 16); };
+#pragma unroll
+            for (int q = 0; q < QT; ++q) av[q] = get(T + q * 16 + l);
 #pragma unroll
             for (int i = 0; i < RT; ++i) {
+                const u32x4 xv = get(i * 16 + l);
 #pragma unroll
-                for (int q = 0; q < QT; ++q) sum[i][q] = multiply(s.a[q][j], s.x[i][j], sum[i][q]);
+                for (int q = 0; q < QT; ++q) sum[i][q] = multiply(av[q], xv, sum[i][q]);
             }
         }
+        in_wave_order();
     };
-    constexpr int kNext = W * kStep;
-    Step now[U];
-    for (int32_t k0 = k_from + wave * kStep; k0 < k_to; k0 += U * kNext) {
+    // Whole steps; no load is behind a condition (behind one the compiler waits for it there): past the last it is the last once more, not added.
+    const int32_t steps = (k_to - k_from) / kStep;
+    auto whole = [&](Step &to, int32_t step) {
+        const int32_t k = k_from + (step < steps ? step : steps - 1) * kStep + eighth * 8;
 #pragma unroll
-        for (int u = 0; u < U; ++u) load(now[u], k0 + u * kNext);
+        for (int i = 0; i < 2 * (RT + QT); ++i) to.v[i] = load8(from[i] + k);
+    };
+    if (wave < steps) {
+        Step s[D];
 #pragma unroll
-        for (int u = 0; u < U; ++u) add(now[u]);
+        for (int d = 0; d < D; ++d) whole(s[d], wave + d * W);
+        for (int32_t step = wave; step < steps; step += D * W) {
+#pragma unroll
+            for (int d = 0; d < D; ++d) {
+                if (d > 0 && step + d * W >= steps) break;
+                put(s[d]);
+                whole(s[d], step + (d + D) * W);
+                add();
+            }
+        }
     }
+    if (k_from + steps * kStep < k_to && steps % W == wave) {      // past K zeros, in both
+        Step last;
+        const int32_t k = k_from + steps * kStep + eighth * 8;
+#pragma unroll
+        for (int i = 0; i < 2 * (RT + QT); ++i) last.v[i] = K >= 8 ? load_row8_back(from[i], k, K) : load_row8(from[i], k, K);
+        put(last);
+        add();
+    }
+    float(*const sums)[16][kPitch] = reinterpret_cast<float(*)[16][kPitch]>(lds);
 #pragma unroll
     for (int i = 0; i < RT; ++i) {
-        if (i > 0) __syncthreads();
+        __syncthreads();
 #pragma unroll
         for (int q = 0; q < QT; ++q) *reinterpret_cast<v4f *>(&sums[wave][l][q * 16 + g * 4]) = sum[i][q];
         __syncthreads();
         for (int e = threadIdx.x; e < 16 * QT * 4; e += 64 * W) {
-            const int in = e / (QT * 4), r = e % (QT * 4) * 4;
-            if (i * 16 + in >= item.count || r0 + r >= R) continue;             // R is a multiple of 8
-            v4f s = *reinterpret_cast<const v4f *>(&sums[0][in][r]);
+            const int row = e / (QT * 4), r = e % (QT * 4) * 4;
+            if (i * 16 + row >= item.count || r0 + r >= R) continue;            // R is a multiple of 8
+            v4f v = *reinterpret_cast<const v4f *>(&sums[0][row][r]);
 #pragma unroll
-            for (int w = 1; w < W; ++w) s += *reinterpret_cast<const v4f *>(&sums[w][in][r]);
-            const int32_t m = kFew ? places[0][in] : (int32_t)order[blockIdx.x * T + i * 16 + in];
-            *reinterpret_cast<v4f *>(t + ((int64_t)blockIdx.z * M + m) * R + r0 + r) = s;
+            for (int w = 1; w < W; ++w) v += *reinterpret_cast<const v4f *>(&sums[w][row][r]);
+            *reinterpret_cast<v4f *>(t + ((int64_t)blockIdx.z * M + rows[i * 16 + row]) * R + r0 + r) = v;
         }
     }
 }
 
 // ---------------------------------------------------------------- out += f B t
-// A workgroup has an item's rows and chunks of 256 columns of a slice, a wave 64 of each.  t, joined from its partial sums, is taken as
-// two bf16; one read of B's columns meets both halves of all rows, sixteen at a time.  Tile i of a wave's four has columns 32 (i / 2) + 8 g +
-// 4 (i % 2) + 0 .. 3 for the four lane groups g, so that a lane ends with eight consecutive outputs, and the four groups with 64 bytes of a row.
+// t, joined from its partial sums, is taken as two bf16 and stays in registers; B's columns come to LDS and meet both halves; what comes of sixteen
+// rows and 64 columns goes through LDS to the lanes that have eight columns of a row.  S: steps of 32 of the rank, at most.  kNarrow: rows of fewer
+// than eight columns.
 
 struct Slices {
     int32_t first_column[kMostSlices + 1], first_chunk[kMostSlices + 1];     // of the slices there are; the end after them
 };
 
-constexpr int kChunk = 256;                 // columns that a workgroup takes at a time
+// What a launch hands to its workgroups.
+struct Expansion {
+    Global<uint16_t> out;
+    int64_t out_stride;
+    Global<const uint16_t> b;
+    Global<const float> factors, t;
+    int32_t M, N, rank, slices, splits, chunks, tile;
+    Global<const int32_t> order;
+    Global<const Item> items;
+    Slices cut;
+};
 
-// S: steps of 32 of the rank, at most.
-template <int T, int S>
-__global__ __launch_bounds__(256) void expand_kernel(Global<uint16_t> out, int64_t out_stride, Global<const uint16_t> b,
-                                                     Global<const float> factors, Global<const float> t, int32_t M, int32_t N, int32_t rank,
-                                                     int32_t slices, int32_t splits, int32_t chunks, Global<const int32_t> order,
-                                                     Global<const Item> items, const Slices cut)
-{
-    constexpr int kPitch = S * 128 + 16;                        // bytes of a row of t: the first halves, the second, and a shift of banks
-    __shared__ __align__(16) uint8_t lds[T * kPitch];
-    const Item item = items[blockIdx.x];
-    if (item.count == 0) return;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l = lane & 15, g = lane >> 4;
-    const int32_t R = slices * rank, chunk = blockIdx.y;
-    int s = 0;
-    while (s + 1 < slices && chunk >= cut.first_chunk[s + 1]) ++s;
-    const int32_t n_end = cut.first_column[s + 1];
-    const int32_t n_from = cut.first_column[s] + (chunk - cut.first_chunk[s]) * chunks * kChunk + wave * 64;
-    const int32_t n_to = n_from + chunks * kChunk < n_end ? n_from + chunks * kChunk : n_end;
-    const int32_t *const rows = order + (int64_t)blockIdx.x * T;
-    const uint16_t *const mine = b + (int64_t)item.adapter * N * rank;
-    struct Outputs {
-        uint16_t *row;
-        u32x4 v[2];
-    };
-    auto load_outputs = [&](Outputs &to, int32_t r, int32_t n0) {       // what is added to
-        const bool real = r + l < item.count;
-        to.row = real ? out + rows[r + l] * out_stride : nullptr;
+// bytes of a column of B in LDS, with a shift of banks, and of a row of 64 results
+template <int S>
+constexpr int kColumn = S * 64 + 16;
+constexpr int kResult = 64 * 4 + 16;
+
+// A wave's sixteen rows of an item.
+template <int S, bool kNarrow>
+struct SixteenRows {
+    const int lane = threadIdx.x & 63, l = lane & 15, g = lane >> 4, in = lane / 8, eighth = lane % 8;
+    int32_t count, N;
+    uint16_t *row[2];
+    u32x4 before[2], t[2 * S];
+
+    __device__ __forceinline__ SixteenRows(const Expansion &p, const int32_t *rows, int32_t count_) : count(count_), N(p.N)
+    {
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            const int32_t n = n0 + half * 32 + g * 8;
-            if (real && n < n_end) to.v[half] = load_row8(to.row, n, n_end);
-        }
-    };
-    u32x4 entries[S][4];
-    auto load_entries = [&](int32_t n0) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int32_t c = n0 + (i / 2) * 32 + (l / 4) * 8 + (i % 2) * 4 + l % 4;
-            const uint16_t *const p = mine + (int64_t)(c < n_end ? c : n_end - 1) * rank;
-#pragma unroll
-            for (int q = 0; q < S; ++q) entries[q][i] = q * 32 + g * 8 < rank ? load8(p + q * 32 + g * 8) : u32x4{0, 0, 0, 0};
-        }
-    };
-    Outputs now, next;
-    if (n_from < n_to) {
-        load_outputs(now, 0, n_from);
-        load_entries(n_from);
+        for (int half = 0; half < 2; ++half) row[half] = p.out + rows[half * 8 + in < count ? half * 8 + in : 0] * p.out_stride;
     }
-    const float factor = factors[item.adapter];
-    // four entries of a row's rank at a time; zeros behind them
-    for (int32_t e = threadIdx.x; e < T * S * 8; e += 256) {
-        const int32_t row = e / (S * 8), k = e % (S * 8) * 4;
-        v4f v = {0, 0, 0, 0};
-        if (row < item.count && k < rank) {
-            const float *const p = t + (int64_t)rows[row] * R + s * rank + k;
-            for (int32_t q = 0; q < splits; ++q) v += *reinterpret_cast<const v4f *>(p + (int64_t)q * M * R);
-            v *= factor;
-        }
-        const u32x2 high = {narrow_bf16x2(v[0], v[1]), narrow_bf16x2(v[2], v[3])};
-        float h[4];
-        widen_bf16x4(high, h);
-        *reinterpret_cast<u32x2 *>(lds + row * kPitch + k * 2) = high;
-        *reinterpret_cast<u32x2 *>(lds + row * kPitch + S * 64 + k * 2) =
-            u32x2{narrow_bf16x2(v[0] - h[0], v[1] - h[1]), narrow_bf16x2(v[2] - h[2], v[3] - h[3])};
+
+    // What is added to.  No load is behind a condition (the compiler waits for what it loads there): rows that are not there are the first once more, and
+    // units that reach past a row's end begin before it (drop_elements puts their elements in place).
+    __device__ __forceinline__ void load(int32_t n0)
+    {
+        const int32_t n = n0 + eighth * 8;
+#pragma unroll
+        for (int half = 0; half < 2; ++half) before[half] = kNarrow ? load_row8(row[half], n, N) : load8(row[half] + (n + 8 <= N ? n : N - 8));
     }
-    __syncthreads();
-    for (int32_t n0 = n_from; n0 < n_to; n0 += kChunk) {
-        if (n0 > n_from) load_entries(n0);
-        for (int32_t r = 0; r < item.count; r += 16) {
-            const bool last = r + 16 >= item.count;
-            if (!last || n0 + kChunk < n_to) load_outputs(next, last ? 0 : r + 16, last ? n0 + kChunk : n0);
-            v4f sum[4] = {};
-            const uint8_t *const at = lds + (r + l) * kPitch + g * 16;
+
+    // The rows' t of slice s times the factor: lane l has row l % 16, eight entries of each step.
+    __device__ __forceinline__ void join(const Expansion &p, const int32_t *rows, int s, float factor)
+    {
+        const int32_t R = p.slices * p.rank;
+        const float *const from = p.t + (int64_t)rows[l < count ? l : 0] * R + s * p.rank;
+        v4f v[S][2];
+#pragma unroll
+        for (int q = 0; q < S; ++q) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int32_t k = q * 32 + g * 8 + h * 4;
+                v[q][h] = *reinterpret_cast<const v4f *>(from + (k < p.rank ? k : 0));
+            }
+        }
+        for (int32_t i = 1; i < p.splits; ++i) {
 #pragma unroll
             for (int q = 0; q < S; ++q) {
-                const u32x4 first = *reinterpret_cast<const u32x4 *>(at + q * 64), second = *reinterpret_cast<const u32x4 *>(at + S * 64 + q * 64);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) sum[i] = multiply(entries[q][i], second, multiply(entries[q][i], first, sum[i]));
-            }
-            if (now.row) {
-#pragma unroll
-                for (int half = 0; half < 2; ++half) {
-                    const int32_t n = n0 + half * 32 + g * 8;
-                    if (n >= n_end) continue;
-                    float f[8];
-                    widen_bf16x8(now.v[half], f);
-                    u32x4 v;
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const v4f d = sum[half * 2 + i / 2];
-                        v[i] = narrow_bf16x2(f[2 * i] + d[i % 2 * 2], f[2 * i + 1] + d[i % 2 * 2 + 1]);
-                    }
-                    store_row8(now.row, n, n_end, v);
+                for (int h = 0; h < 2; ++h) {
+                    const int32_t k = q * 32 + g * 8 + h * 4;
+                    v[q][h] += *reinterpret_cast<const v4f *>(from + (int64_t)i * p.M * R + (k < p.rank ? k : 0));
                 }
             }
-            now = next;
         }
+#pragma unroll
+        for (int q = 0; q < S; ++q) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const v4f f = q * 32 + g * 8 < p.rank ? v[q][h] * factor : v4f{0, 0, 0, 0};
+                const u32x2 high = {narrow_bf16x2(f[0], f[1]), narrow_bf16x2(f[2], f[3])};
+                float w[4];
+                widen_bf16x4(high, w);
+                const u32x2 low = {narrow_bf16x2(f[0] - w[0], f[1] - w[1]), narrow_bf16x2(f[2] - w[2], f[3] - w[3])};
+                t[q][2 * h] = high.x;
+                t[q][2 * h + 1] = high.y;
+                t[S + q][2 * h] = low.x;
+                t[S + q][2 * h + 1] = low.y;
+            }
+        }
+    }
+
+    __device__ __forceinline__ void multiply_columns(const uint8_t *columns, v4f (&sum)[4]) const
+    {
+#pragma unroll
+        for (int q = 0; q < S; ++q) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                sum[i] = multiply(*reinterpret_cast<const u32x4 *>(columns + (i * 16 + l) * kColumn<S> + q * 64 + g * 16), t[q], sum[i]);
+        }
+#pragma unroll
+        for (int q = 0; q < S; ++q) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                sum[i] = multiply(*reinterpret_cast<const u32x4 *>(columns + (i * 16 + l) * kColumn<S> + q * 64 + g * 16), t[S + q], sum[i]);
+        }
+    }
+
+    // Sums of the columns from n0 on, through `results`, to the rows, as far as n_end.
+    __device__ __forceinline__ void store(const v4f (&sum)[4], uint8_t *results, int32_t n0, int32_t n_end)
+    {
+        const int32_t n = n0 + eighth * 8;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) *reinterpret_cast<v4f *>(results + l * kResult + (i * 16 + g * 4) * 4) = sum[i];
+        in_wave_order();
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            const uint8_t *const p = results + (half * 8 + in) * kResult + eighth * 32;
+            const v4f d[2] = {*reinterpret_cast<const v4f *>(p), *reinterpret_cast<const v4f *>(p + 16)};
+            float f[8];
+            widen_bf16x8(kNarrow || n + 8 <= N ? before[half] : drop_elements(before[half], n + 8 - N), f);
+            u32x4 v;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = narrow_bf16x2(f[2 * i] + d[i / 2][i % 2 * 2], f[2 * i + 1] + d[i / 2][i % 2 * 2 + 1]);
+            if (n0 + 64 <= n_end) {                             // all of the wave's columns
+                if (half * 8 + in < count) *reinterpret_cast<u32x4_anywhere *>(row[half] + n) = v;
+            } else if (half * 8 + in < count && n < n_end) {
+                store_row8(row[half], n, n_end, v);
+            }
+        }
+        in_wave_order();
+    }
+};
+
+// 64 columns of B on their way to LDS by Threads lanes: pieces of eight of the rank, one after the other as they lie in memory.
+template <int S, int Threads>
+struct Columns {
+    static constexpr int kPieces = 64 * 4 * S / Threads;
+    u32x4 v[kPieces];
+
+    __device__ __forceinline__ void load(const uint8_t *adapter, uint32_t per, int32_t n0, int32_t n_end)      // 2^30 bytes at most
+    {
+        const uint32_t last = (uint32_t)n_end * per - 1;        // past the slice's end it is the last piece once more
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) {
+            const uint32_t e = (uint32_t)n0 * per + i * Threads + threadIdx.x % Threads;
+            v[i] = *reinterpret_cast<const u32x4 *>(adapter + (e < last ? e : last) * 16);
+        }
+    }
+
+    __device__ __forceinline__ void put(uint8_t *columns, uint32_t per) const
+    {
+        const uint32_t thread = threadIdx.x % Threads;
+        if (per == 4 * S) {
+#pragma unroll
+            for (int i = 0; i < kPieces; ++i) {
+                const uint32_t e = i * Threads + thread;
+                *reinterpret_cast<u32x4 *>(columns + e / (4 * S) * kColumn<S> + e % (4 * S) * 16) = v[i];
+            }
+            return;
+        }
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) {
+            const uint32_t e = i * Threads + thread, c = e / per;
+            if (c < 64) *reinterpret_cast<u32x4 *>(columns + c * kColumn<S> + (e - c * per) * 16) = v[i];
+        }
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) {                     // zeros behind the rank
+            const uint32_t e = i * Threads + thread;
+            if (e % (4 * S) >= per) *reinterpret_cast<u32x4 *>(columns + e / (4 * S) * kColumn<S> + e % (4 * S) * 16) = u32x4{0, 0, 0, 0};
+        }
+    }
+};
+
+// The columns [from, to) that row y of the grid has, of a slice that ends at `end`; `width` at a time.
+struct Range {
+    int slice = 0;
+    int32_t from, to, end;
+    __device__ __forceinline__ Range(const Expansion &p, int32_t width)
+    {
+        const int32_t chunk = blockIdx.y;
+        while (slice + 1 < p.slices && chunk >= p.cut.first_chunk[slice + 1]) ++slice;
+        end = p.cut.first_column[slice + 1];
+        from = p.cut.first_column[slice] + (chunk - p.cut.first_chunk[slice]) * p.chunks * width;
+        to = from + p.chunks * width < end ? from + p.chunks * width : end;
+    }
+};
+
+// Items of sixteen rows: every wave has columns of its own, 64 at a time, and waits for no other.
+constexpr int kFewWaves = 4;
+
+template <int S, bool kFew, bool kNarrow>
+__global__ __launch_bounds__(64 * kFewWaves) void expand_few_kernel(const Expansion p)
+{
+    static_assert(16 * kResult <= 64 * kColumn<S>, "results have the columns' place");
+    __shared__ __align__(16) uint8_t lds[kFewWaves][64 * kColumn<S>];
+    const int32_t at = kFew ? (int32_t)blockIdx.x : item_of(blockIdx.x, gridDim.x);
+    const Item item = p.items[at];
+    if (item.count == 0) return;
+    const int wave = threadIdx.x >> 6;
+    const Range range(p, 64 * kFewWaves);
+    const int32_t from = range.from + wave * 64;
+    if (from >= range.to) return;
+    const int32_t *const rows = p.order + (int64_t)at * 16;
+    const uint8_t *const adapter = reinterpret_cast<const uint8_t *>(p.b + (int64_t)item.adapter * p.N * p.rank);
+    const uint32_t per = (uint32_t)p.rank / 8;
+    Columns<S, 64> columns;
+    columns.load(adapter, per, from, range.end);
+    SixteenRows<S, kNarrow> sixteen(p, rows, item.count);
+    sixteen.load(from);
+    sixteen.join(p, rows, range.slice, p.factors[item.adapter]);
+    for (int32_t n0 = from; n0 < range.to; n0 += 64 * kFewWaves) {
+        const int32_t n1 = n0 + 64 * kFewWaves < range.to ? n0 + 64 * kFewWaves : n0;
+        columns.put(lds[wave], per);
+        in_wave_order();
+        columns.load(adapter, per, n1, range.end);
+        v4f sum[4] = {};
+        sixteen.multiply_columns(lds[wave], sum);
+        in_wave_order();
+        sixteen.store(sum, lds[wave], n0, range.end);
+        sixteen.load(n1);
+    }
+}
+
+// Items of 64 rows: four waves of sixteen share 64 columns at a time, in two places in turn, so that B is read once for all of them (every sixteen rows
+// reading it for themselves were bound by that: 4096 rows, rank 64, 5376 columns 28 us).
+template <int S>
+__global__ __launch_bounds__(256) void expand_many_kernel(const Expansion p)
+{
+    __shared__ __align__(16) uint8_t lds[2][64 * kColumn<S>], results[4][16 * kResult];
+    const int32_t at = item_of(blockIdx.x, gridDim.x);
+    const Item item = p.items[at];
+    if (item.count == 0) return;
+    const int wave = threadIdx.x >> 6;
+    const Range range(p, 64);
+    const int32_t count = item.count - wave * 16;
+    const int32_t *const rows = p.order + (int64_t)at * 64 + (count > 0 ? wave * 16 : 0);
+    const uint8_t *const adapter = reinterpret_cast<const uint8_t *>(p.b + (int64_t)item.adapter * p.N * p.rank);
+    const uint32_t per = (uint32_t)p.rank / 8;
+    Columns<S, 256> columns;
+    columns.load(adapter, per, range.from, range.end);
+    SixteenRows<S, false> sixteen(p, rows, count);
+    sixteen.load(range.from);
+    sixteen.join(p, rows, range.slice, p.factors[item.adapter]);
+    int turn = 0;
+    for (int32_t n0 = range.from; n0 < range.to; n0 += 64, turn ^= 1) {
+        const int32_t n1 = n0 + 64 < range.to ? n0 + 64 : n0;
+        columns.put(lds[turn], per);
+        __syncthreads();                        // and the other place is written again only after the next
+        columns.load(adapter, per, n1, range.end);
+        if (count > 0) {
+            v4f sum[4] = {};
+            sixteen.multiply_columns(lds[turn], sum);
+            sixteen.store(sum, results[wave], n0, range.end);
+        }
+        sixteen.load(n1);
     }
 }
 

@@ -32,11 +32,9 @@ __device__ __forceinline__ u32x4 load_row8(const uint16_t *row, int64_t col, int
     return u32x4{e[0] | e[1] << 16, e[2] | e[3] << 16, e[4] | e[5] << 16, e[6] | e[7] << 16};
 }
 
-// The same without a branch, for rows of eight elements and more: what would reach past the end is read from its last eight.
-__device__ __forceinline__ u32x4 load_row8_back(const uint16_t *row, int32_t col, int32_t cols)
+// Eight elements without the first `by`, zeros after them.
+__device__ __forceinline__ u32x4 drop_elements(const u32x4 &v, int32_t by)
 {
-    const int32_t from = col + 8 <= cols ? col : cols - 8, by = col - from;         // elements that are not this unit's
-    const u32x4 v = *reinterpret_cast<const u32x4_anywhere *>(row + from);
     const uint64_t low = (uint64_t)v.y << 32 | v.x, high = (uint64_t)v.w << 32 | v.z;
     const int bits = (by & 3) * 16;
     uint64_t l = low >> bits | (high << 1) << (63 - bits), h = high >> bits;
@@ -46,6 +44,14 @@ __device__ __forceinline__ u32x4 load_row8_back(const uint16_t *row, int32_t col
     }
     if (by >= 8) l = 0;
     return u32x4{(uint32_t)l, (uint32_t)(l >> 32), (uint32_t)h, (uint32_t)(h >> 32)};
+}
+
+// load_row8 without a branch, for rows of eight elements and more: what would reach past the end is read from its last eight.
+__device__ __forceinline__ u32x4 load_row8_back(const uint16_t *row, int32_t col, int32_t cols)
+{
+    const int32_t from = col + 8 <= cols ? col : cols - 8;
+    const u32x4 v = *reinterpret_cast<const u32x4_anywhere *>(row + from);
+    return drop_elements(v, col - from);
 }
 
 __device__ __forceinline__ void store_row8(uint16_t *row, int64_t col, int64_t cols, const u32x4 &v)
