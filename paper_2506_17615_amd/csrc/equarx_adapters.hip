@@ -13,6 +13,18 @@ using namespace equarx::adapters;
 #ifndef EQX_RT
 #define EQX_RT 4
 #endif
+#ifndef EQX_STREAM
+#define EQX_STREAM ((int64_t)20 << 20)
+#endif
+#ifndef EQX_FW
+#define EQX_FW 8
+#endif
+#ifndef EQX_FD
+#define EQX_FD 1
+#endif
+#ifndef EQX_TALL
+#define EQX_TALL 2048
+#endif
 #ifndef EQX_W
 #define EQX_W 8
 #endif
@@ -23,7 +35,7 @@ using namespace equarx::adapters;
 #define EQX_WC 1024
 #endif
 #ifndef EQX_WF
-#define EQX_WF 512
+#define EQX_WF 256
 #endif
 constexpr int64_t kMostRows = (int64_t)1 << 24, kMostCols = (int64_t)1 << 22, kMostElements = (int64_t)1 << 40;
 
@@ -61,20 +73,20 @@ struct Cut {
 
 // Rows that are taken together, rows of A and waves of a workgroup.
 struct FewRows {
-    static constexpr int RT = 1, QT = 1, W = 8, D = 2;
+    static constexpr int RT = 1, QT = 1, W = EQX_FW, D = EQX_FD;
 };
 struct ManyRows {
     static constexpr int RT = EQX_RT, QT = 4, W = EQX_W, D = 1;
 };
 
-constexpr int64_t kTallRows = 2048, kMostSplits = 8, kWorkgroupsOfFew = EQX_WF, kWorkgroupsOfMany = EQX_WM, kWorkgroupsOfColumns = EQX_WC;
+constexpr int64_t kStreamFrom = EQX_STREAM, kTallRows = EQX_TALL, kMostSplits = 8, kWorkgroupsOfFew = EQX_WF, kWorkgroupsOfMany = EQX_WM, kWorkgroupsOfColumns = EQX_WC;
 
 Cut cut_of(const Sizes &z)
 {
     Cut c{};
     const int64_t R = (int64_t)z.rank * z.slices, groups = z.M < z.adapters ? z.M : z.adapters;
     const bool tall = z.M >= 32 * groups && z.M >= kTallRows && z.N >= 8;
-    c.few = z.M <= kFewRows;
+    c.few = z.M <= kFewRows && (z.M <= 64 || 2 * groups >= z.M);
     c.tile = 16 * (tall ? ManyRows::RT : FewRows::RT);
     c.items = c.few ? z.M : (z.M / c.tile + groups + 7) / 8 * 8;
     const int rank_tile = 16 * (tall ? ManyRows::QT : FewRows::QT), waves = tall ? ManyRows::W : FewRows::W;
@@ -82,14 +94,15 @@ Cut cut_of(const Sizes &z)
     const int64_t steps = (z.K + kStep - 1) / kStep;
     auto limited = [](int64_t v, int64_t hi) { return v < 1 ? 1 : v < hi ? v : hi; };
     const int64_t busy = (z.M / c.tile + groups) * c.rank_tiles;
-    const int64_t splits = limited((tall ? kWorkgroupsOfMany : kWorkgroupsOfFew) / busy, limited((steps + waves - 1) / waves, kMostSplits));
+    const int64_t splits = limited(tall ? kWorkgroupsOfMany / busy : (kWorkgroupsOfFew + busy / 2) / busy, limited((steps + waves - 1) / waves, kMostSplits));
     c.piece = (int32_t)((steps + splits - 1) / splits * kStep);
     c.splits = (int32_t)((z.K + c.piece - 1) / c.piece);
     // columns of a workgroup: as many as leave enough workgroups
+    const int64_t wide = tall ? 512 : kWorkgroupsOfColumns;
     c.columns = tall ? 64 : 64 * kFewWaves;
-    c.chunks = (int32_t)limited((c.items * ((z.N + c.columns - 1) / c.columns) + kWorkgroupsOfColumns - 1) / kWorkgroupsOfColumns, 16);
-    // Room for the partial sums of this many rows or fewer: of m rows in more than one split, a split has 64 * 512 at most.
-    const int64_t bound = 64 * kWorkgroupsOfFew, cut_rows = z.M * kMostSplits;
+    c.chunks = (int32_t)limited((c.items * ((z.N + c.columns - 1) / c.columns) + wide - 1) / wide, 16);
+    // Room for the partial sums of this many rows or fewer: m rows in s > 1 splits have s <= 4 / 3 * kWorkgroups / (m / 64).
+    const int64_t bound = 64 * 2 * (kWorkgroupsOfFew > kWorkgroupsOfMany ? kWorkgroupsOfFew : kWorkgroupsOfMany), cut_rows = z.M * kMostSplits;
     const int64_t rows = z.M > (cut_rows < bound ? cut_rows : bound) ? z.M : (cut_rows < bound ? cut_rows : bound);
     c.order = round_up((size_t)(rows * R) * sizeof(float), kWorkspaceAlign);
     // items of sixteen rows, or of 64 and fewer
@@ -113,7 +126,11 @@ void launch(const Sizes &z, const Cut &c, const uint16_t *x, int64_t x_stride, c
     const Expansion p{out, out_stride, b, factors, t, (int32_t)z.M, (int32_t)z.N, z.rank, z.slices, c.splits, c.chunks, c.tile, order, items, cut};
     auto expand = [&](auto kernel) { ctx.launch2d(kernel, (unsigned)c.items, (unsigned)cut.first_chunk[z.slices], 256, p); };
     if constexpr (S::RT > 1) {
-        expand(z.rank <= 32 ? expand_many_kernel<1> : z.rank <= 64 ? expand_many_kernel<2> : expand_many_kernel<4>);
+        if (z.M * z.N >= kStreamFrom) {
+            expand(z.rank <= 32 ? expand_many_kernel<1, true> : z.rank <= 64 ? expand_many_kernel<2, true> : expand_many_kernel<4, true>);
+        } else {
+            expand(z.rank <= 32 ? expand_many_kernel<1, false> : z.rank <= 64 ? expand_many_kernel<2, false> : expand_many_kernel<4, false>);
+        }
     } else {
         expand(z.N < 8        ? expand_few_kernel<4, kFew, true>
                : z.rank <= 32 ? expand_few_kernel<1, kFew, false>

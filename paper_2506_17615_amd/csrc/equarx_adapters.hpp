@@ -32,13 +32,12 @@ __device__ __forceinline__ int32_t count_up(int32_t *at, int32_t a, int32_t adap
         const uint64_t mask = __ballot(left);
         if (mask == 0) return found;
         const int first = __builtin_ctzll(mask);
-        const uint64_t same = __ballot(left && a == __shfl(a, first));
-        if (left && (same >> lane & 1)) {
-            int32_t base = 0;
-            if (lane == first) base = atomicAdd(&at[a], (int32_t)__popcll(same));
-            found = __shfl(base, first) + (int32_t)__popcll(same & (((uint64_t)1 << lane) - 1));
-            left = false;
-        }
+        const uint64_t same = __ballot(left && a == __builtin_amdgcn_readlane(a, first));
+        if (same >> lane & 1) left = false;
+        int32_t base = 0;
+        if (lane == first) base = atomicAdd(&at[a], (int32_t)__popcll(same));
+        base = __builtin_amdgcn_readlane(base, first);
+        if (same >> lane & 1) found = base + (int32_t)__popcll(same & (((uint64_t)1 << lane) - 1));
     }
     if (left) found = atomicAdd(&at[a], 1);
     return found;
@@ -113,7 +112,10 @@ __device__ __forceinline__ void in_wave_order()
 
 // Few rows are brought together without a launch: item i is row i's, if every sixteenth of its adapter's rows, from the first on, is row i,
 // and has that row and the next fifteen.  Each wave finds that for itself, with lane l's rows l, 64 + l, ...
-constexpr int kFewRows = 256, kIdsPerLane = kFewRows / 64;
+#ifndef EQX_FEWROWS
+#define EQX_FEWROWS 256
+#endif
+constexpr int kFewRows = EQX_FEWROWS, kIdsPerLane = kFewRows / 64;
 
 // Row l % 16 of item i in lane l; `count` rows, 0 where there is no such item.
 __device__ __forceinline__ int32_t find_item(const int32_t *ids, int32_t M, int32_t adapters, int32_t i, int32_t *places, Item &item)
@@ -281,7 +283,7 @@ __global__ __launch_bounds__(64 * W) void shrink_kernel(Global<const uint16_t> x
 // ---------------------------------------------------------------- out += f B t
 // t, joined from its partial sums, is taken as two bf16 and stays in registers; B's columns come to LDS and meet both halves; what comes of sixteen
 // rows and 64 columns goes through LDS to the lanes that have eight columns of a row.  S: steps of 32 of the rank, at most.  kNarrow: rows of fewer
-// than eight columns.
+// than eight columns.  kStreams: out is more than the caches keep for the next call, and is read and written past them.
 
 struct Slices {
     int32_t first_column[kMostSlices + 1], first_chunk[kMostSlices + 1];     // of the slices there are; the end after them
@@ -305,49 +307,78 @@ constexpr int kColumn = S * 64 + 16;
 constexpr int kResult = 64 * 4 + 16;
 
 // A wave's sixteen rows of an item.
-template <int S, bool kNarrow>
+template <int S, bool kNarrow, bool kStreams>
 struct SixteenRows {
-    const int lane = threadIdx.x & 63, l = lane & 15, g = lane >> 4, in = lane / 8, eighth = lane % 8;
+    int lane = threadIdx.x & 63, l = lane & 15, g = lane >> 4, in = lane / 8, eighth = lane % 8;
     int32_t count, N;
     uint16_t *row[2];
-    u32x4 before[2], t[2 * S];
+    u32x4 t[2 * S];
+    struct Before {
+        u32x4 v[2];
+    };
 
-    __device__ __forceinline__ SixteenRows(const Expansion &p, const int32_t *rows, int32_t count_) : count(count_), N(p.N)
+    int32_t place[2], mine;
+
+    // The rows' numbers are asked for beside the item: behind its last they are whatever the place holds, and not used.
+    __device__ __forceinline__ SixteenRows(const Expansion &p, const int32_t *rows) : N(p.N)
     {
 #pragma unroll
-        for (int half = 0; half < 2; ++half) row[half] = p.out + rows[half * 8 + in < count ? half * 8 + in : 0] * p.out_stride;
+        for (int half = 0; half < 2; ++half) place[half] = rows[half * 8 + in];
+        mine = rows[l];
+    }
+
+    __device__ __forceinline__ void take(const Expansion &p, int32_t count_)
+    {
+        count = count_;
+        const int32_t first = __builtin_amdgcn_readfirstlane(mine);
+#pragma unroll
+        for (int half = 0; half < 2; ++half) row[half] = p.out + (half * 8 + in < count ? place[half] : first) * p.out_stride;
+        mine = l < count ? mine : first;
     }
 
     // What is added to.  No load is behind a condition (the compiler waits for what it loads there): rows that are not there are the first once more, and
     // units that reach past a row's end begin before it (drop_elements puts their elements in place).
-    __device__ __forceinline__ void load(int32_t n0)
+    __device__ __forceinline__ void load(Before &to, int32_t n0) const
     {
         const int32_t n = n0 + eighth * 8;
 #pragma unroll
-        for (int half = 0; half < 2; ++half) before[half] = kNarrow ? load_row8(row[half], n, N) : load8(row[half] + (n + 8 <= N ? n : N - 8));
+        for (int half = 0; half < 2; ++half) if constexpr (kNarrow) {
+                to.v[half] = load_row8(row[half], n, N);
+            } else {
+                const auto *const from = reinterpret_cast<const u32x4_anywhere *>(row[half] + (n + 8 <= N ? n : N - 8));
+                to.v[half] = kStreams ? __builtin_nontemporal_load(from) : *from;
+            }
     }
 
     // The rows' t of slice s times the factor: lane l has row l % 16, eight entries of each step.
-    __device__ __forceinline__ void join(const Expansion &p, const int32_t *rows, int s, float factor)
+    __device__ __forceinline__ void join(const Expansion &p, int s, float factor)
     {
         const int32_t R = p.slices * p.rank;
-        const float *const from = p.t + (int64_t)rows[l < count ? l : 0] * R + s * p.rank;
-        v4f v[S][2];
+        const float *const from = p.t + (int64_t)mine * R + s * p.rank;
+        // in order, and asked for J at a time: one after the other is a latency each
+        constexpr int J = S == 1 ? 8 : S == 2 ? 4 : 2;
+        v4f v[S][2] = {};
+        for (int32_t i = 0; i < p.splits; i += J) {
+            v4f part[J][S][2];
 #pragma unroll
-        for (int q = 0; q < S; ++q) {
+            for (int j = 0; j < J; ++j) {
+                const float *const at = from + (int64_t)(i + j < p.splits ? i + j : i) * p.M * R;
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int32_t k = q * 32 + g * 8 + h * 4;
-                v[q][h] = *reinterpret_cast<const v4f *>(from + (k < p.rank ? k : 0));
+                for (int q = 0; q < S; ++q) {
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const int32_t k = q * 32 + g * 8 + h * 4;
+                        part[j][q][h] = *reinterpret_cast<const v4f *>(at + (k < p.rank ? k : 0));
+                    }
+                }
             }
-        }
-        for (int32_t i = 1; i < p.splits; ++i) {
 #pragma unroll
-            for (int q = 0; q < S; ++q) {
+            for (int j = 0; j < J; ++j) {
+                if (j > 0 && i + j >= p.splits) break;
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const int32_t k = q * 32 + g * 8 + h * 4;
-                    v[q][h] += *reinterpret_cast<const v4f *>(from + (int64_t)i * p.M * R + (k < p.rank ? k : 0));
+                for (int q = 0; q < S; ++q) {
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) v[q][h] = i + j == 0 ? part[j][q][h] : v[q][h] + part[j][q][h];
                 }
             }
         }
@@ -385,7 +416,7 @@ struct SixteenRows {
     }
 
     // Sums of the columns from n0 on, through `results`, to the rows, as far as n_end.
-    __device__ __forceinline__ void store(const v4f (&sum)[4], uint8_t *results, int32_t n0, int32_t n_end)
+    __device__ __forceinline__ void store(const v4f (&sum)[4], const Before &before, uint8_t *results, int32_t n0, int32_t n_end) const
     {
         const int32_t n = n0 + eighth * 8;
 #pragma unroll
@@ -396,12 +427,19 @@ struct SixteenRows {
             const uint8_t *const p = results + (half * 8 + in) * kResult + eighth * 32;
             const v4f d[2] = {*reinterpret_cast<const v4f *>(p), *reinterpret_cast<const v4f *>(p + 16)};
             float f[8];
-            widen_bf16x8(kNarrow || n + 8 <= N ? before[half] : drop_elements(before[half], n + 8 - N), f);
+            widen_bf16x8(kNarrow || n + 8 <= N ? before.v[half] : drop_elements(before.v[half], n + 8 - N), f);
             u32x4 v;
 #pragma unroll
             for (int i = 0; i < 4; ++i) v[i] = narrow_bf16x2(f[2 * i] + d[i / 2][i % 2 * 2], f[2 * i + 1] + d[i / 2][i % 2 * 2 + 1]);
             if (n0 + 64 <= n_end) {                             // all of the wave's columns
-                if (half * 8 + in < count) *reinterpret_cast<u32x4_anywhere *>(row[half] + n) = v;
+                auto *const to = reinterpret_cast<u32x4_anywhere *>(row[half] + n);
+                if (half * 8 + in < count) {
+                    if constexpr (kStreams) {
+                        __builtin_nontemporal_store(v, to);
+                    } else {
+                        *to = v;
+                    }
+                }
             } else if (half * 8 + in < count && n < n_end) {
                 store_row8(row[half], n, n_end, v);
             }
@@ -473,65 +511,77 @@ __global__ __launch_bounds__(64 * kFewWaves) void expand_few_kernel(const Expans
     static_assert(16 * kResult <= 64 * kColumn<S>, "results have the columns' place");
     __shared__ __align__(16) uint8_t lds[kFewWaves][64 * kColumn<S>];
     const int32_t at = kFew ? (int32_t)blockIdx.x : item_of(blockIdx.x, gridDim.x);
+    SixteenRows<S, kNarrow, false> sixteen(p, p.order + (int64_t)at * 16);
     const Item item = p.items[at];
     if (item.count == 0) return;
     const int wave = threadIdx.x >> 6;
     const Range range(p, 64 * kFewWaves);
     const int32_t from = range.from + wave * 64;
     if (from >= range.to) return;
-    const int32_t *const rows = p.order + (int64_t)at * 16;
     const uint8_t *const adapter = reinterpret_cast<const uint8_t *>(p.b + (int64_t)item.adapter * p.N * p.rank);
     const uint32_t per = (uint32_t)p.rank / 8;
     Columns<S, 64> columns;
     columns.load(adapter, per, from, range.end);
-    SixteenRows<S, kNarrow> sixteen(p, rows, item.count);
-    sixteen.load(from);
-    sixteen.join(p, rows, range.slice, p.factors[item.adapter]);
-    for (int32_t n0 = from; n0 < range.to; n0 += 64 * kFewWaves) {
+    sixteen.take(p, item.count);
+    typename SixteenRows<S, kNarrow, false>::Before before[2];
+    sixteen.load(before[0], from);
+    sixteen.join(p, range.slice, p.factors[item.adapter]);
+    // Two turns a round, so that what a turn asks for has registers of its own; it is asked for before the turn's own stores, which a wait for it would
+    // have to wait for too.
+    auto turn = [&](int32_t n0, int which) {
         const int32_t n1 = n0 + 64 * kFewWaves < range.to ? n0 + 64 * kFewWaves : n0;
         columns.put(lds[wave], per);
         in_wave_order();
         columns.load(adapter, per, n1, range.end);
+        sixteen.load(before[which ^ 1], n1);
         v4f sum[4] = {};
         sixteen.multiply_columns(lds[wave], sum);
         in_wave_order();
-        sixteen.store(sum, lds[wave], n0, range.end);
-        sixteen.load(n1);
+        sixteen.store(sum, before[which], lds[wave], n0, range.end);
+    };
+    for (int32_t n0 = from; n0 < range.to; n0 += 2 * 64 * kFewWaves) {
+        turn(n0, 0);
+        if (n0 + 64 * kFewWaves < range.to) turn(n0 + 64 * kFewWaves, 1);
     }
 }
 
 // Items of 64 rows: four waves of sixteen share 64 columns at a time, in two places in turn, so that B is read once for all of them (every sixteen rows
 // reading it for themselves were bound by that: 4096 rows, rank 64, 5376 columns 28 us).
-template <int S>
+template <int S, bool kStreams>
 __global__ __launch_bounds__(256) void expand_many_kernel(const Expansion p)
 {
     __shared__ __align__(16) uint8_t lds[2][64 * kColumn<S>], results[4][16 * kResult];
     const int32_t at = item_of(blockIdx.x, gridDim.x);
+    const int wave = threadIdx.x >> 6;
+    SixteenRows<S, false, kStreams> sixteen(p, p.order + (int64_t)at * 64 + wave * 16);
     const Item item = p.items[at];
     if (item.count == 0) return;
-    const int wave = threadIdx.x >> 6;
     const Range range(p, 64);
     const int32_t count = item.count - wave * 16;
-    const int32_t *const rows = p.order + (int64_t)at * 64 + (count > 0 ? wave * 16 : 0);
+    if (count <= 0) sixteen = SixteenRows<S, false, kStreams>(p, p.order + (int64_t)at * 64);
     const uint8_t *const adapter = reinterpret_cast<const uint8_t *>(p.b + (int64_t)item.adapter * p.N * p.rank);
     const uint32_t per = (uint32_t)p.rank / 8;
     Columns<S, 256> columns;
     columns.load(adapter, per, range.from, range.end);
-    SixteenRows<S, false> sixteen(p, rows, count);
-    sixteen.load(range.from);
-    sixteen.join(p, rows, range.slice, p.factors[item.adapter]);
-    int turn = 0;
-    for (int32_t n0 = range.from; n0 < range.to; n0 += 64, turn ^= 1) {
+    sixteen.take(p, count);
+    typename SixteenRows<S, false, kStreams>::Before before[2];
+    sixteen.load(before[0], range.from);
+    sixteen.join(p, range.slice, p.factors[item.adapter]);
+    auto turn = [&](int32_t n0, int which) {
         const int32_t n1 = n0 + 64 < range.to ? n0 + 64 : n0;
-        columns.put(lds[turn], per);
-        __syncthreads();                        // and the other place is written again only after the next
+        columns.put(lds[which], per);
+        __syncthreads();                        // the other place is written again only after the next
         columns.load(adapter, per, n1, range.end);
+        sixteen.load(before[which ^ 1], n1);
         if (count > 0) {
             v4f sum[4] = {};
-            sixteen.multiply_columns(lds[turn], sum);
-            sixteen.store(sum, results[wave], n0, range.end);
+            sixteen.multiply_columns(lds[which], sum);
+            sixteen.store(sum, before[which], results[wave], n0, range.end);
         }
-        sixteen.load(n1);
+    };
+    for (int32_t n0 = range.from; n0 < range.to; n0 += 128) {
+        turn(n0, 0);
+        if (n0 + 64 < range.to) turn(n0 + 64, 1);
     }
 }
 
