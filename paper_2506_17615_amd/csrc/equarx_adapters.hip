@@ -10,33 +10,6 @@ using namespace equarx;
 using namespace equarx::host;
 using namespace equarx::adapters;
 
-#ifndef EQX_RT
-#define EQX_RT 4
-#endif
-#ifndef EQX_STREAM
-#define EQX_STREAM ((int64_t)20 << 20)
-#endif
-#ifndef EQX_FW
-#define EQX_FW 8
-#endif
-#ifndef EQX_FD
-#define EQX_FD 1
-#endif
-#ifndef EQX_TALL
-#define EQX_TALL 2048
-#endif
-#ifndef EQX_W
-#define EQX_W 8
-#endif
-#ifndef EQX_WM
-#define EQX_WM 256
-#endif
-#ifndef EQX_WC
-#define EQX_WC 1024
-#endif
-#ifndef EQX_WF
-#define EQX_WF 256
-#endif
 constexpr int64_t kMostRows = (int64_t)1 << 24, kMostCols = (int64_t)1 << 22, kMostElements = (int64_t)1 << 40;
 
 struct Sizes {
@@ -73,13 +46,21 @@ struct Cut {
 
 // Rows that are taken together, rows of A and waves of a workgroup.
 struct FewRows {
-    static constexpr int RT = 1, QT = 1, W = EQX_FW, D = EQX_FD;
+    static constexpr int RT = 1, QT = 1, W = 8;
 };
 struct ManyRows {
-    static constexpr int RT = EQX_RT, QT = 4, W = EQX_W, D = 1;
+    static constexpr int RT = 4, QT = 4, W = 8;
 };
 
-constexpr int64_t kStreamFrom = EQX_STREAM, kTallRows = EQX_TALL, kMostSplits = 8, kWorkgroupsOfFew = EQX_WF, kWorkgroupsOfMany = EQX_WM, kWorkgroupsOfColumns = EQX_WC;
+// Rows of one adapter are taken sixteen together, or 64: from 2048 rows on, 32 to an adapter or more.  Measured on MI355X, us by sixteen -> by 64, 5376 to
+// 8192 columns in three slices: 1024 rows of 4 adapters of rank 16 22.2 -> 27.0, of 8 of rank 64 35.1 -> 32.5.
+// k is cut where that gives more workgroups, as far as one for every CU: a workgroup of many rows has its CU's LDS for itself (one more than 256
+// is a round more: 4096 rows of 4 adapters 15.6 -> 22.6); of few a second one gains nothing (64 rows 12.8, with twice as many 13.6), and what is cut
+// has to be joined again (more than four pieces: 64 rows of 4 adapters 12.9 -> 14.6).
+// Columns: two workgroups of the second launch for every CU (64 rows 13.2 us, with four 14.3; 4096 42.3 and 44.2).  From 20 Mi outputs on these go past the
+// caches (4096 x 5376 44.2 -> 42.3, 4096 x 8192 58.0 -> 55.0; 2048 x 8192 34.7 -> 37.5).
+constexpr int64_t kTallRows = 2048, kWorkgroupsOfFew = 256, kWorkgroupsOfMany = 256, kMostSplits = 4, kWorkgroupsOfColumns = 512,
+                  kStreamFrom = (int64_t)20 << 20;
 
 Cut cut_of(const Sizes &z)
 {
@@ -98,9 +79,8 @@ Cut cut_of(const Sizes &z)
     c.piece = (int32_t)((steps + splits - 1) / splits * kStep);
     c.splits = (int32_t)((z.K + c.piece - 1) / c.piece);
     // columns of a workgroup: as many as leave enough workgroups
-    const int64_t wide = tall ? 512 : kWorkgroupsOfColumns;
     c.columns = tall ? 64 : 64 * kFewWaves;
-    c.chunks = (int32_t)limited((c.items * ((z.N + c.columns - 1) / c.columns) + wide - 1) / wide, 16);
+    c.chunks = (int32_t)limited((c.items * ((z.N + c.columns - 1) / c.columns) + kWorkgroupsOfColumns - 1) / kWorkgroupsOfColumns, 16);
     // Room for the partial sums of this many rows or fewer: m rows in s > 1 splits have s <= 4 / 3 * kWorkgroups / (m / 64).
     const int64_t bound = 64 * 2 * (kWorkgroupsOfFew > kWorkgroupsOfMany ? kWorkgroupsOfFew : kWorkgroupsOfMany), cut_rows = z.M * kMostSplits;
     const int64_t rows = z.M > (cut_rows < bound ? cut_rows : bound) ? z.M : (cut_rows < bound ? cut_rows : bound);
@@ -121,7 +101,7 @@ void launch(const Sizes &z, const Cut &c, const uint16_t *x, int64_t x_stride, c
     Item *const items = reinterpret_cast<Item *>(workspace + c.list);
     const int32_t R = z.rank * z.slices;
     if (!kFew) ctx.launch(group_kernel, 1, 1024, ids, z.M, z.adapters, c.tile, order, items, c.items);
-    ctx.launch3d(shrink_kernel<S::RT, S::QT, S::W, S::D, kFew>, (unsigned)c.items, (unsigned)c.rank_tiles, (unsigned)c.splits, 64 * S::W, x, x_stride, a,
+    ctx.launch3d(shrink_kernel<S::RT, S::QT, S::W, kFew>, (unsigned)c.items, (unsigned)c.rank_tiles, (unsigned)c.splits, 64 * S::W, x, x_stride, a,
                  t, z.M, z.K, R, c.piece, order, items, ids, z.adapters);
     const Expansion p{out, out_stride, b, factors, t, (int32_t)z.M, (int32_t)z.N, z.rank, z.slices, c.splits, c.chunks, c.tile, order, items, cut};
     auto expand = [&](auto kernel) { ctx.launch2d(kernel, (unsigned)c.items, (unsigned)cut.first_chunk[z.slices], 256, p); };

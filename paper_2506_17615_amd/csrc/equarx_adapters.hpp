@@ -1,6 +1,8 @@
 // Device code of low-rank adapters of many requests: rows brought together by adapter, t = A x, and out += f B t.
 #pragma once
 
+#include <type_traits>
+
 #include "equarx.h"
 #include "equarx_rows.hpp"
 
@@ -112,10 +114,7 @@ __device__ __forceinline__ void in_wave_order()
 
 // Few rows are brought together without a launch: item i is row i's, if every sixteenth of its adapter's rows, from the first on, is row i,
 // and has that row and the next fifteen.  Each wave finds that for itself, with lane l's rows l, 64 + l, ...
-#ifndef EQX_FEWROWS
-#define EQX_FEWROWS 256
-#endif
-constexpr int kFewRows = EQX_FEWROWS, kIdsPerLane = kFewRows / 64;
+constexpr int kFewRows = 256, kIdsPerLane = kFewRows / 64;
 
 // Row l % 16 of item i in lane l; `count` rows, 0 where there is no such item.
 __device__ __forceinline__ int32_t find_item(const int32_t *ids, int32_t M, int32_t adapters, int32_t i, int32_t *places, Item &item)
@@ -166,12 +165,14 @@ __device__ __forceinline__ int32_t item_of(uint32_t x, uint32_t count) { return 
 
 // ---------------------------------------------------------------- t = A x
 // A workgroup has an item's rows, 16 RT of them, 16 QT rows of A and a piece of k, of which its W waves take 64 in turn; their sums are
-// added in order through LDS.  Sums of the pieces go to t [split][M][R].  D: steps of a wave that are on their way.
+// added in order through LDS.  Sums of the pieces go to t [split][M][R].  A wave's next step is on its way
+// while it multiplies one; a second gained nothing.  64 rows of 32 adapters, 48 x 5376: 6.5 us, 2.5 TB/s of A; 4096 rows of 4, 64 x 5376: 15.6, the
+// 44 MB of x at 2.8 TB/s, of which a workgroup has a CU's LDS and 128 KB on their way.
 // kFew: items are found here, and the first workgroup of each writes it down for the launch that follows.
 
 constexpr int kStep = 64;
 
-template <int RT, int QT, int W, int D, bool kFew>
+template <int RT, int QT, int W, bool kFew>
 __global__ __launch_bounds__(64 * W) void shrink_kernel(Global<const uint16_t> x, int64_t x_stride, Global<const uint16_t> a, Global<float> t,
                                                         int32_t M, int32_t K, int32_t R, int32_t piece, Global<int32_t> order, Global<Item> items,
                                                         Global<const int32_t> ids, int32_t adapters)
@@ -241,17 +242,12 @@ __global__ __launch_bounds__(64 * W) void shrink_kernel(Global<const uint16_t> x
         for (int i = 0; i < 2 * (RT + QT); ++i) to.v[i] = load8(from[i] + k);
     };
     if (wave < steps) {
-        Step s[D];
-#pragma unroll
-        for (int d = 0; d < D; ++d) whole(s[d], wave + d * W);
-        for (int32_t step = wave; step < steps; step += D * W) {
-#pragma unroll
-            for (int d = 0; d < D; ++d) {
-                if (d > 0 && step + d * W >= steps) break;
-                put(s[d]);
-                whole(s[d], step + (d + D) * W);
-                add();
-            }
+        Step now;
+        whole(now, wave);
+        for (int32_t step = wave; step < steps; step += W) {
+            put(now);
+            whole(now, step + W);
+            add();
         }
     }
     if (k_from + steps * kStep < k_to && steps % W == wave) {      // past K zeros, in both
@@ -355,10 +351,10 @@ struct SixteenRows {
     {
         const int32_t R = p.slices * p.rank;
         const float *const from = p.t + (int64_t)mine * R + s * p.rank;
-        // in order, and asked for J at a time: one after the other is a latency each
-        constexpr int J = S == 1 ? 8 : S == 2 ? 4 : 2;
+        // in order, and several asked for together: one after the other is a latency each
         v4f v[S][2] = {};
-        for (int32_t i = 0; i < p.splits; i += J) {
+        auto several = [&](auto most, int32_t i) {
+            constexpr int J = decltype(most)::value;
             v4f part[J][S][2];
 #pragma unroll
             for (int j = 0; j < J; ++j) {
@@ -372,6 +368,7 @@ struct SixteenRows {
                     }
                 }
             }
+            asm volatile("" ::: "memory");                      // or they move to the additions, each behind its condition
 #pragma unroll
             for (int j = 0; j < J; ++j) {
                 if (j > 0 && i + j >= p.splits) break;
@@ -381,6 +378,12 @@ struct SixteenRows {
                     for (int h = 0; h < 2; ++h) v[q][h] = i + j == 0 ? part[j][q][h] : v[q][h] + part[j][q][h];
                 }
             }
+        };
+        if (p.splits <= 2) {
+            several(std::integral_constant<int, 2>{}, 0);
+        } else {
+            constexpr int kMany = S <= 2 ? 4 : 2;
+            for (int32_t i = 0; i < p.splits; i += kMany) several(std::integral_constant<int, kMany>{}, i);
         }
 #pragma unroll
         for (int q = 0; q < S; ++q) {
@@ -502,7 +505,8 @@ struct Range {
     }
 };
 
-// Items of sixteen rows: every wave has columns of its own, 64 at a time, and waits for no other.
+// Items of sixteen rows: every wave has columns of its own, 64 at a time, and waits for no other.  64 rows of 32 adapters, rank 16, 8192 columns: 6.5
+// us, two thirds of it the launch and three latencies, one after the other: the item, what it names, the result.
 constexpr int kFewWaves = 4;
 
 template <int S, bool kFew, bool kNarrow>
@@ -546,7 +550,8 @@ __global__ __launch_bounds__(64 * kFewWaves) void expand_few_kernel(const Expans
 }
 
 // Items of 64 rows: four waves of sixteen share 64 columns at a time, in two places in turn, so that B is read once for all of them (every sixteen rows
-// reading it for themselves were bound by that: 4096 rows, rank 64, 5376 columns 28 us).
+// reading it for themselves were bound by that: 4096 rows, rank 64, 5376 columns 28 us).  What bounds it now is latency between its barriers, four
+// workgroups a CU: 21 us for the 88 MB of out, 4.2 TB/s.
 template <int S, bool kStreams>
 __global__ __launch_bounds__(256) void expand_many_kernel(const Expansion p)
 {

@@ -81,7 +81,8 @@ SIZES = [(1, 8, (8,), 8, 1), (1, 4096, (4096, 2048, 2048), 16, 32), (3, 1, (1,),
          (17, 65, (65, 63), 24, 5), (33, 255, (257,), 32, 40), (64, 5376, (512, 256, 256), 16, 32), (65, 1511, (1001, 1500), 24, 7),
          (100, 300, (31, 1, 900, 70), 64, 9), (31, 1024, (129,), 128, 6), (128, 333, (400, 1), 128, 2), (200, 2049, (333,), 40, 64),
          (333, 130, (1000,), 8, 5), (700, 96, (90,), 16, 300), (1000, 777, (300, 200), 56, 3), (4096, 256, (128,), 64, 4),
-         (2111, 515, (77, 300, 5), 72, 8000)]
+         (2111, 515, (77, 300, 5), 72, 8000), (200, 700, (300, 20), 16, 130), (256, 264, (70,), 48, 300), (64, 3, (7,), 128, 64), (2048, 90, (6,), 16, 2),
+         (5000, 8, (9, 8), 8, 20)]
 
 
 @pytest.mark.parametrize("kind", ("mixed", "grouped", "one", "distinct", "none"))
@@ -96,6 +97,16 @@ def test_rows_of_every_kind(M, K, widths, rank, adapters, kind):
     _call(dev, wide[:, :sum(widths)])
     assert (wide[:, sum(widths):] == 9.0).all()
     _check(case, wide[:, :sum(widths)].cpu())
+
+
+@pytest.mark.parametrize("rank", (8, 24, 32, 40, 64, 72, 128))
+def test_many_rows_and_columns(rank):
+    """Rows by 64, the last ones of an adapter fewer; outputs that go past the caches."""
+    case = _on(_case(rank, 2300, 200, (5003, 4200, 1), rank, 3))
+    start = case["out"].clone()
+    got = _call(case).clone()
+    case["out"] = start
+    _check(case, got, "cuda")
 
 
 def test_the_largest_products():
