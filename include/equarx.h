@@ -640,7 +640,7 @@ int equarx_pages_extend(const equarx_pages *pages, const int32_t *counts, int32_
  *
  *   x_bf16 [M][K]      row m at x_bf16 + m * x_stride;
  *   a_bf16             [adapters][slices * rank][K],  b_bf16 [adapters][N][rank], contiguous;
- *   factors            fp32 [adapters];
+ *   factors            fp32 [adapters] (factors and ids need only their elements' alignment);
  *   ids                int32 [M] on the device; rows whose id is outside [0, adapters) are left as they were;
  *   slice_ends         HOST int64 [slices], growing, the last one N; read before the call returns;
  *   out_bf16 [M][N]    row m at out_bf16 + m * out_stride.  Strides need be a multiple of nothing.

@@ -213,6 +213,7 @@ __device__ __forceinline__ void finish_row(const Place<L> &at, u32x4 (&h)[K], co
         }
     }
     sum = row_sum<L>(sum);
+    const int shift = 31 - __builtin_clz((uint32_t)to.block | 1u);       // a block is a power of two
     const float inverse = (float)(1.0 / __builtin_sqrt(sum / (double)cols + in.eps));
 #pragma unroll
     for (int k = 0; k < K; ++k) {
@@ -238,7 +239,7 @@ __device__ __forceinline__ void finish_row(const Place<L> &at, u32x4 (&h)[K], co
             const u32x2 codes = int8_of(y, top, to.block, scale);
             if (real) {
                 *reinterpret_cast<u32x2 *>((int8_t *)to.codes + at.row * cols + col) = codes;
-                if ((uint32_t)col % (uint32_t)to.block == 0) to.scales[(at.row * cols + col) / to.block] = scale;
+                if ((col & (to.block - 1)) == 0) to.scales[at.row * (cols >> shift) + (col >> shift)] = scale;
             }
         }
         if (to.mx_codes.address) {                                  // rows are padded to whole sixteens of units

@@ -178,15 +178,34 @@ def test_in_place(cols):
 
 
 def test_more_rows_than_workgroups_of_one_launch():
-    """2^20 workgroups of sixteen rows, and some."""
-    rows = (16 << 20) + 37
-    x = torch.randn(rows, 8, device="cuda", generator=torch.Generator("cuda").manual_seed(1)).to(torch.bfloat16)
-    out = torch.full_like(x, 9.0)
-    eq.equarx_norm(x, None, out=out)
-    for part in (slice(0, 64), slice((16 << 20) - 32, rows)):
-        _, ys = _two(x[part].cpu(), None, 1e-6)
-        _rows_match(out[part].cpu(), [y.to(torch.bfloat16) for y in ys])
-    assert not (out == 9.0).all(dim=1).any()
+    """2^20 workgroups of sixteen rows, and some: every input and output goes on where the first launch ends."""
+    rows, cols = (16 << 20) + 37, 32
+    g = torch.Generator("cuda").manual_seed(1)
+    partials = [torch.randn(rows, cols, device="cuda", generator=g).to(torch.bfloat16) for _ in range(2)]
+    x = torch.empty_like(partials[0])
+    eq.equarx_reduce_fused([p.view(-1) for p in partials], 32, x.view(-1))
+
+    def outputs(n):
+        codes, scales = eq.alloc_mx4(n, cols)
+        return dict(out=torch.full((n, cols), 9.0, dtype=torch.bfloat16, device="cuda"), codes=torch.full((n, cols), 99, dtype=torch.int8, device="cuda"),
+                    scales=torch.full((n, 1), 9.0, device="cuda"), codes_block=32, mx4_codes=codes, mx4_scales=scales)
+
+    for reduced in (False, True):
+        stream = torch.ones_like(x)
+        all_rows = outputs(rows)
+        if reduced:
+            eq.equarx_norm_reduced(partials, 32, None, residual=stream, **all_rows)
+        else:
+            eq.equarx_norm(x, None, residual=stream, **all_rows)
+        for part in (slice(0, 64), slice((16 << 20) - 32, rows)):
+            small, few = torch.ones_like(x[part]), outputs(x[part].shape[0])
+            eq.equarx_norm(x[part], None, residual=small, **few)
+            assert torch.equal(stream[part], small)
+            for k, t in few.items():
+                assert not torch.is_tensor(t) or torch.equal(all_rows[k][part], t), k
+        assert not (all_rows["out"] == 9.0).all(dim=1).any() and not (all_rows["codes"] == 99).all(dim=1).any()
+    _, ys = _two(x[-50:].cpu(), None, 1e-6, residual=torch.ones(50, cols, dtype=torch.bfloat16))
+    _rows_match(all_rows["out"][-50:].cpu(), [y.to(torch.bfloat16) for y in ys])
 
 
 def test_offsets_past_32_bits():
