@@ -182,19 +182,32 @@ unsigned workgroups(int64_t rows)
 template <int B>
 void launch_reduced(const PartialTable &partials, int P, int64_t rows, int64_t cols, const Inputs &in, const Outputs &to, LaunchCtx &ctx)
 {
+    auto launch = [&](auto cut, auto kernel) {
+        constexpr int L = decltype(cut)::L;
+        in_row_pieces<L>(rows, [&](int64_t at, int64_t count) {
+            Inputs i = in;
+            Outputs o = to;
+            advance(i, o, at, cols);
+            PartialTable tab = partials;
+            for (int j = 0; j < kMaxPartials; ++j) tab.x[j] += at * cols;
+            ctx.launch(kernel, workgroups<L>(count), Place<L>::T, P, count, cols, i, o, tab);
+        });
+    };
+    if (!in_units(in, to)) {                                    // seldom: three cuts are enough
+        if (cols <= 64 * 16) {
+            launch(Cut<64, 2>{}, reduced_kernel<B, 64, 2, 1, false, false>);
+        } else if (cols <= 256 * 32) {
+            launch(Cut<256, 4>{}, reduced_kernel<B, 256, 4, 1, false, false>);
+        } else {
+            launch(Cut<1024, 4>{}, reduced_kernel<B, 1024, 4, 1, false, false>);
+        }
+        return;
+    }
     with_reduced_cut(rows, cols, P, [&](auto cut) {
         constexpr int L = decltype(cut)::L, K = decltype(cut)::K, A = decltype(cut)::A;
-        const bool whole = in_units(in, to), streams = A == 1 && rows * cols >= kStreamFrom;
         if constexpr (L * 8 >= B) {                             // as cols >= B
-            in_row_pieces<L>(rows, [&](int64_t at, int64_t count) {
-                Inputs i = in;
-                Outputs o = to;
-                advance(i, o, at, cols);
-                PartialTable tab = partials;
-                for (int j = 0; j < kMaxPartials; ++j) tab.x[j] += at * cols;
-                ctx.launch(!whole ? reduced_kernel<B, L, K, A, false, false> : streams ? reduced_kernel<B, L, K, A, true, A == 1> : reduced_kernel<B, L, K, A, true, false>,
-                           workgroups<L>(count), Place<L>::T, P, count, cols, i, o, tab);
-            });
+            constexpr bool kMayStream = A == 1 && L > 64;
+            launch(cut, rows * cols >= kStreamFrom ? reduced_kernel<B, L, K, A, true, kMayStream> : reduced_kernel<B, L, K, A, true, false>);
         }
     });
 }

@@ -253,6 +253,20 @@ def test_reduced_rows_are_the_two_calls(block, P, rows, blocks):
         assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))
 
 
+@pytest.mark.parametrize("block,cols", ((32, 96), (64, 1024), (256, 5376), (512, 8192), (128, 16384)))
+def test_reduced_rows_beside_strides_of_any_length(block, cols):
+    """Residual and output in rows that begin on two bytes only: the bits of those that begin on sixteen."""
+    rows, P = 37, 5
+    partials, w = [_rows(p, rows, cols).cuda() for p in range(P)], _rows(9, 1, cols)[0].cuda()
+    stream, out = _rows(8, rows, cols).cuda(), torch.empty(rows, cols, dtype=torch.bfloat16, device="cuda")
+    wide_stream, wide_out = (torch.full((rows, cols + 3), 9.0, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    wide_stream[:, :cols] = stream
+    eq.equarx_norm_reduced(partials, block, w, 1e-5, stream, out)
+    eq.equarx_norm_reduced(partials, block, w, 1e-5, wide_stream[:, :cols], wide_out[:, :cols])
+    assert torch.equal(wide_stream[:, :cols], stream) and torch.equal(wide_out[:, :cols], out)
+    assert (wide_stream[:, cols:] == 9.0).all() and (wide_out[:, cols:] == 9.0).all()
+
+
 def test_reduced_rows_in_place_of_a_partial():
     partials = [_rows(p, 40, 768).cuda() for p in range(5)]
     want = torch.empty_like(partials[0])
