@@ -10,6 +10,7 @@
 #include <Python.h>
 
 #include <ATen/core/Tensor.h>
+#include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -496,8 +497,10 @@ int cache_attention(PyObject *const *a)
 
 // ---------------------------------------------------------------- norms
 
-// On the device whose stream the call is made on?
-bool here(const at::Tensor *t) { return !t || t->device().index() == c10::hip::getCurrentHIPStream().device_index(); }
+// On the device whose stream the call is made on?  A call that asks sets it first.
+thread_local c10::DeviceIndex current_device = -1;
+
+bool here(const at::Tensor *t) { return !t || t->device().index() == current_device; }
 
 // The arguments of a norm of [rows][cols] from `weight` on: weight, eps, residual, out, codes, scales, their block, packed codes and
 // scales, whether 1 is added to the weight.
@@ -540,6 +543,7 @@ struct Norm {
 
 int norm(PyObject *const *a)
 {
+    current_device = c10::hip::current_device();
     Rows x;
     Norm n;
     if (!x.of(a[0], 2) || !here(x.tensor) || !n.of(a + 1, x.size[0], x.size[1])) return kNotPlain;
@@ -548,6 +552,7 @@ int norm(PyObject *const *a)
 
 int norm_reduced(PyObject *const *a)
 {
+    current_device = c10::hip::current_device();
     Buffers x;
     Norm n;
     int64_t count = -1;
@@ -593,6 +598,7 @@ bool some_pages(PyObject *o, PyObject *page, equarx_pages &p)
 
 int pages_trim(PyObject *const *a)
 {
+    current_device = c10::hip::current_device();
     equarx_pages p;
     Buffer keep;
     if (!some_pages(a[0], a[1], p) || !exactly(keep, a[2], kInt, p.sequences)) return kNotPlain;
@@ -601,6 +607,7 @@ int pages_trim(PyObject *const *a)
 
 int pages_extend(PyObject *const *a)
 {
+    current_device = c10::hip::current_device();
     equarx_pages p;
     Buffer counts, starts, slots, granted, positions, tags, row_tags;
     if (!some_pages(a[0], a[1], p) || !exactly(counts, a[2], kInt, p.sequences) || !exactly(starts, a[3], kInt, (int64_t)p.sequences + 1))
@@ -617,6 +624,7 @@ int pages_extend(PyObject *const *a)
 
 int adapters(PyObject *const *a)
 {
+    current_device = c10::hip::current_device();
     Rows x, out;
     Buffer da, db, factors, ids;
     Workspace ws;
