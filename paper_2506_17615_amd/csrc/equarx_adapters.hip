@@ -38,6 +38,7 @@ inline size_t row_bytes(int64_t rows, int64_t cols, int64_t stride) { return (si
 // How a call is cut, by its sizes alone.
 struct Cut {
     bool few;               // items are found by those who take them
+    bool few_of_each;       // many items of few rows: what counts is reading A
     int tile;               // rows of an item, at most
     int64_t items;          // at most
     int32_t rank_tiles, piece, splits, columns, chunks;
@@ -47,6 +48,12 @@ struct Cut {
 // Rows that are taken together, rows of A and waves of a workgroup.
 struct FewRows {
     static constexpr int RT = 1, QT = 1, W = 8;
+};
+// Where there are workgroups enough, of items of few rows that share none of A, more rows of A to one of x: 256 rows of 200 adapters of rank 16 39.4 ->
+// 35.2 us, 64 of 32 of rank 64 28.8 -> 25.9, 4096 of 200 112 -> 102; with fewer workgroups it loses (1 row 7.6 -> 8.3, 128 of 32 16.4 -> 17.1), and with many rows
+// of an adapter (512 of 4 of rank 64 23.3 -> 24.3).
+struct FewOfEach {
+    static constexpr int RT = 1, QT = 3, W = 8;
 };
 struct ManyRows {
     static constexpr int RT = 4, QT = 4, W = 8;
@@ -70,7 +77,8 @@ Cut cut_of(const Sizes &z)
     c.few = z.M <= kFewRows && (z.M <= 64 || 2 * groups >= z.M);
     c.tile = 16 * (tall ? ManyRows::RT : FewRows::RT);
     c.items = c.few ? z.M : (z.M / c.tile + groups + 7) / 8 * 8;
-    const int rank_tile = 16 * (tall ? ManyRows::QT : FewRows::QT), waves = tall ? ManyRows::W : FewRows::W;
+    c.few_of_each = z.M < 32 * groups && (z.M / 16 + groups) * ((R + 15) / 16) >= kWorkgroupsOfFew;
+    const int rank_tile = 16 * (tall ? ManyRows::QT : c.few_of_each ? FewOfEach::QT : FewRows::QT), waves = 8;
     c.rank_tiles = (int32_t)((R + rank_tile - 1) / rank_tile);
     const int64_t steps = (z.K + kStep - 1) / kStep;
     auto limited = [](int64_t v, int64_t hi) { return v < 1 ? 1 : v < hi ? v : hi; };
@@ -171,7 +179,10 @@ int equarx_adapters(const void *x_bf16, int64_t x_stride, const void *a_bf16, co
         cut.first_column[s + 1] = (int32_t)slice_ends[s];
         cut.first_chunk[s + 1] = cut.first_chunk[s] + (int32_t)((columns + width - 1) / width);
     }
-    (c.few ? launch<FewRows, true> : c.tile != 16 ? launch<ManyRows, false> : launch<FewRows, false>)(z, c, static_cast<const uint16_t *>(x_bf16), x_stride, static_cast<const uint16_t *>(a_bf16),
+    auto *const go = c.tile != 16    ? launch<ManyRows, false>
+                     : c.few_of_each ? (c.few ? launch<FewOfEach, true> : launch<FewOfEach, false>)
+                                     : (c.few ? launch<FewRows, true> : launch<FewRows, false>);
+    go(z, c, static_cast<const uint16_t *>(x_bf16), x_stride, static_cast<const uint16_t *>(a_bf16),
                                            static_cast<const uint16_t *>(b_bf16), factors, ids, cut, static_cast<uint16_t *>(out_bf16),
                                            out_stride, static_cast<uint8_t *>(workspace), ctx);
     return ctx.status();
