@@ -65,7 +65,7 @@ struct ManyRows {
 // is a round more: 4096 rows of 4 adapters 15.6 -> 22.6); of few a second one gains nothing (64 rows 12.8, with twice as many 13.6), and what is cut
 // has to be joined again (more than four pieces: 64 rows of 4 adapters 12.9 -> 14.6).
 // Columns: two workgroups of the second launch for every CU (64 rows 13.2 us, with four 14.3; 4096 42.3 and 44.2).  From 20 Mi outputs on these go past the
-// caches (4096 x 5376 44.2 -> 42.3, 4096 x 8192 58.0 -> 55.0; 2048 x 8192 34.7 -> 37.5).
+// caches (4096 x 5376 44.2 -> 42.3, 4096 x 8192 58.0 -> 55.0; 2048 x 8192 34.7 -> 37.5; of 200 adapters 4096 x 8192 102 -> 98).
 constexpr int64_t kTallRows = 2048, kWorkgroupsOfFew = 256, kWorkgroupsOfMany = 256, kMostSplits = 4, kWorkgroupsOfColumns = 512,
                   kStreamFrom = (int64_t)20 << 20;
 
@@ -113,17 +113,22 @@ void launch(const Sizes &z, const Cut &c, const uint16_t *x, int64_t x_stride, c
                  t, z.M, z.K, R, c.piece, order, items, ids, z.adapters);
     const Expansion p{out, out_stride, b, factors, t, (int32_t)z.M, (int32_t)z.N, z.rank, z.slices, c.splits, c.chunks, c.tile, order, items, cut};
     auto expand = [&](auto kernel) { ctx.launch2d(kernel, (unsigned)c.items, (unsigned)cut.first_chunk[z.slices], 256, p); };
+    const bool streams = z.M * z.N >= kStreamFrom;
     if constexpr (S::RT > 1) {
-        if (z.M * z.N >= kStreamFrom) {
+        if (streams) {
             expand(z.rank <= 32 ? expand_many_kernel<1, true> : z.rank <= 64 ? expand_many_kernel<2, true> : expand_many_kernel<4, true>);
         } else {
             expand(z.rank <= 32 ? expand_many_kernel<1, false> : z.rank <= 64 ? expand_many_kernel<2, false> : expand_many_kernel<4, false>);
         }
+    } else if (!kFew && streams && z.N >= 8) {
+        expand(z.rank <= 32   ? expand_few_kernel<1, false, false, true>
+               : z.rank <= 64 ? expand_few_kernel<2, false, false, true>
+                              : expand_few_kernel<4, false, false, true>);
     } else {
-        expand(z.N < 8        ? expand_few_kernel<4, kFew, true>
-               : z.rank <= 32 ? expand_few_kernel<1, kFew, false>
-               : z.rank <= 64 ? expand_few_kernel<2, kFew, false>
-                              : expand_few_kernel<4, kFew, false>);
+        expand(z.N < 8        ? expand_few_kernel<4, kFew, true, false>
+               : z.rank <= 32 ? expand_few_kernel<1, kFew, false, false>
+               : z.rank <= 64 ? expand_few_kernel<2, kFew, false, false>
+                              : expand_few_kernel<4, kFew, false, false>);
     }
 }
 

@@ -509,13 +509,13 @@ struct Range {
 // us, two thirds of it the launch and three latencies, one after the other: the item, what it names, the result.
 constexpr int kFewWaves = 4;
 
-template <int S, bool kFew, bool kNarrow>
+template <int S, bool kFew, bool kNarrow, bool kStreams>
 __global__ __launch_bounds__(64 * kFewWaves) void expand_few_kernel(const Expansion p)
 {
     static_assert(16 * kResult <= 64 * kColumn<S>, "results have the columns' place");
     __shared__ __align__(16) uint8_t lds[kFewWaves][64 * kColumn<S>];
     const int32_t at = kFew ? (int32_t)blockIdx.x : item_of(blockIdx.x, gridDim.x);
-    SixteenRows<S, kNarrow, false> sixteen(p, p.order + (int64_t)at * 16);
+    SixteenRows<S, kNarrow, kStreams> sixteen(p, p.order + (int64_t)at * 16);
     const Item item = p.items[at];
     if (item.count == 0) return;
     const int wave = threadIdx.x >> 6;
@@ -527,7 +527,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void expand_few_kernel(const Expans
     Columns<S, 64> columns;
     columns.load(adapter, per, from, range.end);
     sixteen.take(p, item.count);
-    typename SixteenRows<S, kNarrow, false>::Before before[2];
+    typename SixteenRows<S, kNarrow, kStreams>::Before before[2];
     sixteen.load(before[0], from);
     sixteen.join(p, range.slice, p.factors[item.adapter]);
     // Two turns a round, so that what a turn asks for has registers of its own; it is asked for before the turn's own stores, which a wait for it would

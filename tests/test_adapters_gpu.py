@@ -109,6 +109,17 @@ def test_many_rows_and_columns(rank):
     _check(case, got, "cuda")
 
 
+@pytest.mark.parametrize("M,widths,rank,adapters", ((2600, (8001, 100), 16, 300), (2600, (8001, 100), 64, 300), (2600, (8001, 100), 128, 300),
+                                                   ((20 << 20) // 5, (5,), 8, 3)))
+def test_many_rows_of_many_adapters(M, widths, rank, adapters):
+    """Rows by sixteen with outputs that go past the caches; and so many rows of fewer than eight columns."""
+    case = _on(_case(rank, M, 72, widths, rank, adapters))
+    start = case["out"].clone()
+    got = _call(case).clone()
+    case["out"] = start
+    _check(case, got, "cuda")
+
+
 def test_the_largest_products():
     case = _on(_case(1, 4096, 5376, (5376,), 64, 4, "grouped"))
     start = case["out"].clone()
