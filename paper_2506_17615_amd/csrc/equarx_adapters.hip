@@ -187,9 +187,8 @@ int equarx_adapters(const void *x_bf16, int64_t x_stride, const void *a_bf16, co
     auto *const go = c.tile != 16    ? launch<ManyRows, false>
                      : c.few_of_each ? (c.few ? launch<FewOfEach, true> : launch<FewOfEach, false>)
                                      : (c.few ? launch<FewRows, true> : launch<FewRows, false>);
-    go(z, c, static_cast<const uint16_t *>(x_bf16), x_stride, static_cast<const uint16_t *>(a_bf16),
-                                           static_cast<const uint16_t *>(b_bf16), factors, ids, cut, static_cast<uint16_t *>(out_bf16),
-                                           out_stride, static_cast<uint8_t *>(workspace), ctx);
+    go(z, c, static_cast<const uint16_t *>(x_bf16), x_stride, static_cast<const uint16_t *>(a_bf16), static_cast<const uint16_t *>(b_bf16), factors, ids,
+       cut, static_cast<uint16_t *>(out_bf16), out_stride, static_cast<uint8_t *>(workspace), ctx);
     return ctx.status();
 }
 

@@ -161,7 +161,7 @@ __global__ __launch_bounds__(kTeam) void extend_kernel(const Pool p, Global<cons
     __shared__ uint32_t parts[2][kWaves], from[kTeam];
     __shared__ int32_t held_of[kTeam], begin_of[kTeam], had[kTeam];
     const int i = threadIdx.x;
-    const int32_t free = within(p.free_count[0], p.pages);
+    const int32_t free = p.sequences > 0 ? within(p.free_count[0], p.pages) : 0;       // without sequences there need be no pages
     uint32_t rows = 0, pages = 0, got_rows = 0;          // wanted by the sequences before these 1024, and got
     int32_t taken = 0;
     for (int32_t b0 = 0; b0 < p.sequences; b0 += kTeam) {
@@ -226,7 +226,7 @@ __global__ __launch_bounds__(kTeam) void extend_kernel(const Pool p, Global<cons
     }
     if (i == 0) {
         q_starts[p.sequences] = (int32_t)got_rows;
-        p.free_count[0] = free - taken;
+        if (p.sequences > 0) p.free_count[0] = free - taken;
     }
     if (tell) {
         for (int32_t row = (int32_t)got_rows + i; row < to.rows; row += kTeam) tell_nothing(to, row);

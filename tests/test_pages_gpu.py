@@ -1,4 +1,6 @@
 """Page tables on the GPU against a plain statement of what they hold: whole numbers, which have one right answer."""
+import ctypes
+
 import pytest
 import torch
 
@@ -148,6 +150,23 @@ def test_no_rows_and_no_counts():
     starts = on([9, 9, 9, 9])
     eq.equarx_pages_extend(pages, 16, on([1, 0, 2]), starts, torch.empty(0, dtype=torch.int64, device="cuda"))
     assert starts.tolist() == [0, 0, 0, 0] and pages.lengths.tolist() == [0, 0, 0]
+
+
+@pytest.mark.parametrize("rows", (1, 300, 5000))
+def test_no_sequences(rows):
+    """Every row is told that it is nobody's; there need be no pages, and what there is stays."""
+    pages, ints = eq.alloc_pages(0, 4, 8), lambda n, dtype=torch.int32: torch.full((n,), 12345, dtype=dtype, device="cuda")
+    pages.free_count.fill_(77)
+    starts, slots, positions = ints(1), ints(rows, torch.int64), ints(rows)
+    for own in (eq._CPages(None, None, pages.free.data_ptr(), pages.free_count.data_ptr(), 4, 8, 0, 16), eq._CPages(None, None, None, None, 4, 8, 0, 16)):
+        for t in (starts, slots, positions):
+            t.fill_(12345)
+        assert eq.load().equarx_pages_extend(ctypes.byref(own), None, starts.data_ptr(), slots.data_ptr(), None, positions.data_ptr(), None, None, rows,
+                                             torch.cuda.current_stream().cuda_stream) == 0
+        assert starts.tolist() == [0] and (slots == -1).all() and (positions == -1).all() and int(pages.free_count) == 77
+    slots.fill_(5)
+    eq.equarx_pages_extend(pages, 16, ints(0), starts, slots)
+    assert starts.tolist() == [0] and (slots == -1).all() and int(pages.free_count) == 77
 
 
 def test_values_out_of_range():
