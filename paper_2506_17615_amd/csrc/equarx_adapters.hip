@@ -37,7 +37,7 @@ inline size_t row_bytes(int64_t rows, int64_t cols, int64_t stride) { return (si
 
 // How a call is cut, by its sizes alone.
 struct Cut {
-    bool few;               // items are found by those who take them
+    Find find;              // how those who take the items have them
     bool few_of_each;       // many items of few rows: what counts is reading A
     int tile;               // rows of an item, at most
     int64_t items;          // at most
@@ -64,6 +64,10 @@ struct ManyRows {
 // k is cut where that gives more workgroups, as far as one for every CU: a workgroup of many rows has its CU's LDS for itself (one more than 256
 // is a round more: 4096 rows of 4 adapters 15.6 -> 22.6); of few a second one gains nothing (64 rows 12.8, with twice as many 13.6), and what is cut
 // has to be joined again (more than four pieces: 64 rows of 4 adapters 12.9 -> 14.6).
+// Items are found by those who take them, which saves the launch that lists them (333 rows 15.4 -> 13.3 us, 4096 of 4 adapters 42.6 -> 40.2, of 200
+// 97.4 -> 94.4); more than 4096 rows only where no workgroup waits for another (6000 rows 32.9 -> 28.7; 8192 of 64 adapters, three such rounds, 68 -> 72).
+// Few rows, without barriers, an item a row: 64 rows of 64 adapters of rank 64 49.9 -> 30.1, 128 of 200 of rank 16 32.5 -> 21.8; of few adapters the many
+// workgroups of no item cost more (64 rows of 4 of rank 64 14.7 -> 21.7, 128 of 32 31.7 -> 38.9; 48 of 8 still 16.5 -> 14.6).
 // Columns: two workgroups of the second launch for every CU (64 rows 13.2 us, with four 14.3; 4096 42.3 and 44.2).  From 20 Mi outputs on these go past the
 // caches (4096 x 5376 44.2 -> 42.3, 4096 x 8192 58.0 -> 55.0; 2048 x 8192 34.7 -> 37.5; of 200 adapters 4096 x 8192 102 -> 98).
 constexpr int64_t kTallRows = 2048, kWorkgroupsOfFew = 256, kWorkgroupsOfMany = 256, kMostSplits = 4, kWorkgroupsOfColumns = 512,
@@ -74,9 +78,9 @@ Cut cut_of(const Sizes &z)
     Cut c{};
     const int64_t R = (int64_t)z.rank * z.slices, groups = z.M < z.adapters ? z.M : z.adapters;
     const bool tall = z.M >= 32 * groups && z.M >= kTallRows && z.N >= 8;
-    c.few = z.M <= kFewRows && (z.M <= 64 || 2 * groups >= z.M);
+    const bool few = z.M <= kFewRows && (z.M <= 24 || (z.M <= 64 ? 6 : 2) * groups >= z.M);
     c.tile = 16 * (tall ? ManyRows::RT : FewRows::RT);
-    c.items = c.few ? z.M : (z.M / c.tile + groups + 7) / 8 * 8;
+    c.items = few ? z.M : (z.M / c.tile + groups + 7) / 8 * 8;
     c.few_of_each = z.M < 32 * groups && (z.M / 16 + groups) * ((R + 15) / 16) >= kWorkgroupsOfFew;
     const int rank_tile = 16 * (tall ? ManyRows::QT : c.few_of_each ? FewOfEach::QT : FewRows::QT), waves = 8;
     c.rank_tiles = (int32_t)((R + rank_tile - 1) / rank_tile);
@@ -86,6 +90,8 @@ Cut cut_of(const Sizes &z)
     const int64_t splits = limited(tall ? kWorkgroupsOfMany / busy : (kWorkgroupsOfFew + busy / 2) / busy, limited((steps + waves - 1) / waves, kMostSplits));
     c.piece = (int32_t)((steps + splits - 1) / splits * kStep);
     c.splits = (int32_t)((z.K + c.piece - 1) / c.piece);
+    const bool long_found = tall && c.items * c.rank_tiles * c.splits <= kWorkgroupsOfMany;
+    c.find = few ? kFew : z.adapters > kFoundAdapters ? kListed : z.M <= kFound * 64 * waves ? kFound : long_found && z.M <= kFoundLong * 64 * waves ? kFoundLong : kListed;
     // columns of a workgroup: as many as leave enough workgroups
     c.columns = tall ? 64 : 64 * kFewWaves;
     c.chunks = (int32_t)limited((c.items * ((z.N + c.columns - 1) / c.columns) + kWorkgroupsOfColumns - 1) / kWorkgroupsOfColumns, 16);
@@ -100,7 +106,7 @@ Cut cut_of(const Sizes &z)
     return c;
 }
 
-template <typename S, bool kFew>
+template <typename S, Find kFind>
 void launch(const Sizes &z, const Cut &c, const uint16_t *x, int64_t x_stride, const uint16_t *a, const uint16_t *b, const float *factors,
             const int32_t *ids, const Slices &cut, uint16_t *out, int64_t out_stride, uint8_t *workspace, LaunchCtx &ctx)
 {
@@ -108,8 +114,8 @@ void launch(const Sizes &z, const Cut &c, const uint16_t *x, int64_t x_stride, c
     int32_t *const order = reinterpret_cast<int32_t *>(workspace + c.order);
     Item *const items = reinterpret_cast<Item *>(workspace + c.list);
     const int32_t R = z.rank * z.slices;
-    if (!kFew) ctx.launch(group_kernel, 1, 1024, ids, z.M, z.adapters, c.tile, order, items, c.items);
-    ctx.launch3d(shrink_kernel<S::RT, S::QT, S::W, kFew>, (unsigned)c.items, (unsigned)c.rank_tiles, (unsigned)c.splits, 64 * S::W, x, x_stride, a,
+    if (kFind == kListed) ctx.launch(group_kernel, 1, 1024, ids, z.M, z.adapters, c.tile, order, items, c.items);
+    ctx.launch3d(shrink_kernel<S::RT, S::QT, S::W, kFind>, (unsigned)c.items, (unsigned)c.rank_tiles, (unsigned)c.splits, 64 * S::W, x, x_stride, a,
                  t, z.M, z.K, R, c.piece, order, items, ids, z.adapters);
     const Expansion p{out, out_stride, b, factors, t, (int32_t)z.M, (int32_t)z.N, z.rank, z.slices, c.splits, c.chunks, c.tile, order, items, cut};
     auto expand = [&](auto kernel) { ctx.launch2d(kernel, (unsigned)c.items, (unsigned)cut.first_chunk[z.slices], 256, p); };
@@ -120,15 +126,15 @@ void launch(const Sizes &z, const Cut &c, const uint16_t *x, int64_t x_stride, c
         } else {
             expand(z.rank <= 32 ? expand_many_kernel<1, false> : z.rank <= 64 ? expand_many_kernel<2, false> : expand_many_kernel<4, false>);
         }
-    } else if (!kFew && streams && z.N >= 8) {
+    } else if (kFind != kFew && streams && z.N >= 8) {
         expand(z.rank <= 32   ? expand_few_kernel<1, false, false, true>
                : z.rank <= 64 ? expand_few_kernel<2, false, false, true>
                               : expand_few_kernel<4, false, false, true>);
     } else {
-        expand(z.N < 8        ? expand_few_kernel<4, kFew, true, false>
-               : z.rank <= 32 ? expand_few_kernel<1, kFew, false, false>
-               : z.rank <= 64 ? expand_few_kernel<2, kFew, false, false>
-                              : expand_few_kernel<4, kFew, false, false>);
+        expand(z.N < 8        ? expand_few_kernel<4, kFind == kFew, true, false>
+               : z.rank <= 32 ? expand_few_kernel<1, kFind == kFew, false, false>
+               : z.rank <= 64 ? expand_few_kernel<2, kFind == kFew, false, false>
+                              : expand_few_kernel<4, kFind == kFew, false, false>);
     }
 }
 
@@ -184,9 +190,16 @@ int equarx_adapters(const void *x_bf16, int64_t x_stride, const void *a_bf16, co
         cut.first_column[s + 1] = (int32_t)slice_ends[s];
         cut.first_chunk[s + 1] = cut.first_chunk[s] + (int32_t)((columns + width - 1) / width);
     }
-    auto *const go = c.tile != 16    ? launch<ManyRows, false>
-                     : c.few_of_each ? (c.few ? launch<FewOfEach, true> : launch<FewOfEach, false>)
-                                     : (c.few ? launch<FewRows, true> : launch<FewRows, false>);
+    auto pick = [&](auto shape) {
+        using S = decltype(shape);
+        if constexpr (S::RT == 1) {
+            if (c.find == kFew) return launch<S, kFew>;
+        } else {
+            if (c.find == kFoundLong) return launch<S, kFoundLong>;
+        }
+        return c.find == kFound ? launch<S, kFound> : launch<S, kListed>;
+    };
+    auto *const go = c.tile != 16 ? pick(ManyRows{}) : c.few_of_each ? pick(FewOfEach{}) : pick(FewRows{});
     go(z, c, static_cast<const uint16_t *>(x_bf16), x_stride, static_cast<const uint16_t *>(a_bf16), static_cast<const uint16_t *>(b_bf16), factors, ids,
        cut, static_cast<uint16_t *>(out_bf16), out_stride, static_cast<uint8_t *>(workspace), ctx);
     return ctx.status();

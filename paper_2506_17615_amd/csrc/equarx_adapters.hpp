@@ -144,6 +144,77 @@ __device__ __forceinline__ int32_t find_item(const int32_t *ids, int32_t M, int3
     return places[lane % 16 < item.count ? lane % 16 : 0];
 }
 
+// More rows, without a launch too: every workgroup counts all of them, finds what its item is, and which rows that has, in their order: every
+// workgroup has to find the same.  T rows of an item at most; W waves, of which each has rows that follow each other, I a lane at most.
+constexpr int kFoundAdapters = 1024;
+
+template <int T, int W, int I>
+__device__ __forceinline__ void find_rows(const int32_t *ids, int32_t M, int32_t adapters, int32_t i, int32_t *at, int32_t *places, Item &item)
+{
+    __shared__ int32_t parts[2][W], found[3];
+    constexpr int kEach = kFoundAdapters / (64 * W);
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int32_t per = (M + 64 * W - 1) / (64 * W), m0 = wave * per * 64 + lane;
+    int32_t id[I];
+#pragma unroll
+    for (int q = 0; q < I; ++q) id[q] = q < per && m0 + q * 64 < M ? ids[m0 + q * 64] : -1;
+    for (int a = threadIdx.x; a < kFoundAdapters; a += 64 * W) at[a] = 0;
+    if (threadIdx.x == 0) found[2] = 0;
+    __syncthreads();
+#pragma unroll
+    for (int q = 0; q < I; ++q) {
+        if (q < per) count_up(at, id[q], adapters);
+    }
+    __syncthreads();
+    int32_t n[kEach], pieces = 0;
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) {
+        n[e] = at[threadIdx.x * kEach + e];
+        pieces += (n[e] + T - 1) / T;
+    }
+    int32_t upto = pieces;
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+        const int32_t other = __shfl_up(upto, d);
+        if (lane >= d) upto += other;
+    }
+    if (lane == 63) parts[0][wave] = upto;
+    __syncthreads();
+    int32_t first = upto - pieces;
+    for (int w = 0; w < wave; ++w) first += parts[0][w];
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) {
+        const int32_t next = first + (n[e] + T - 1) / T;
+        if (first <= i && i < next) {
+            found[0] = threadIdx.x * kEach + e;
+            found[1] = (i - first) * T;
+            found[2] = n[e] - (i - first) * T < T ? n[e] - (i - first) * T : T;
+        }
+        first = next;
+    }
+    __syncthreads();
+    item = Item{__builtin_amdgcn_readfirstlane(found[0]), __builtin_amdgcn_readfirstlane(found[2])};
+    if (item.count == 0) return;
+    uint64_t same[I];
+    int32_t all = 0;
+#pragma unroll
+    for (int q = 0; q < I; ++q) {
+        same[q] = __ballot(id[q] == item.adapter);
+        all += __popcll(same[q]);
+    }
+    if (lane == 0) parts[1][wave] = all;
+    __syncthreads();
+    int32_t place = -found[1];
+    for (int w = 0; w < wave; ++w) place += parts[1][w];
+#pragma unroll
+    for (int q = 0; q < I; ++q) {
+        const int32_t mine = place + (int32_t)__popcll(same[q] & (((uint64_t)1 << lane) - 1));
+        if (id[q] == item.adapter && mine >= 0 && mine < T) places[mine] = m0 + q * 64;
+        place += __popcll(same[q]);
+    }
+    __syncthreads();
+}
+
 // ---------------------------------------------------------------- products of sixteen by sixteen
 // v_mfma_f32_16x16x32_bf16: lane l has row l % 16 of the first operand and column l % 16 of the second, k = 8 (l / 16) + 0 .. 7 of both,
 // and of the result column l % 16, rows 4 (l / 16) + 0 .. 3.  Rows of x are always the columns: a NaN or an infinity stays in its row.
@@ -168,11 +239,14 @@ __device__ __forceinline__ int32_t item_of(uint32_t x, uint32_t count) { return 
 // added in order through LDS.  Sums of the pieces go to t [split][M][R].  A wave's next step is on its way
 // while it multiplies one; a second gained nothing.  64 rows of 32 adapters, 48 x 5376: 6.5 us, 2.5 TB/s of A; 4096 rows of 4, 64 x 5376: 15.6, the
 // 44 MB of x at 2.8 TB/s, of which a workgroup has a CU's LDS and 128 KB on their way.
-// kFew: items are found here, and the first workgroup of each writes it down for the launch that follows.
+// kFind: items are found here, and the first workgroup of each writes it down for the launch that follows.
 
 constexpr int kStep = 64;
 
-template <int RT, int QT, int W, bool kFew>
+// How an item is found: few rows, by a list, or, with so many rows a lane, among all.
+enum Find { kFew = -1, kListed = 0, kFound = 8, kFoundLong = 16 };
+
+template <int RT, int QT, int W, Find kFind>
 __global__ __launch_bounds__(64 * W) void shrink_kernel(Global<const uint16_t> x, int64_t x_stride, Global<const uint16_t> a, Global<float> t,
                                                         int32_t M, int32_t K, int32_t R, int32_t piece, Global<int32_t> order, Global<Item> items,
                                                         Global<const int32_t> ids, int32_t adapters)
@@ -180,21 +254,28 @@ __global__ __launch_bounds__(64 * W) void shrink_kernel(Global<const uint16_t> x
     constexpr int T = 16 * RT, Q = 16 * QT, kPitch = Q + 4, kTile = (T + Q) * 2 * kStep;
     constexpr int kSums = W * 16 * kPitch * 4, kAll = W * kTile > kSums ? W * kTile : kSums;
     __shared__ __align__(16) uint8_t lds[kAll];
-    __shared__ int32_t places[kFew ? W : 1][16];
+    __shared__ int32_t places[kFind == kFew ? W : 1][kFind == kListed ? 1 : T];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l = lane & 15, g = lane >> 4;
-    const int32_t at = kFew ? (int32_t)blockIdx.x : item_of(blockIdx.x, gridDim.x);
+    const int32_t at = kFind == kFew ? (int32_t)blockIdx.x : item_of(blockIdx.x, gridDim.x);
     Item item;
-    if constexpr (kFew) {
+    if constexpr (kFind == kFew) {
         const int32_t row = find_item(ids, M, adapters, at, places[wave], item);
         if (blockIdx.y == 0 && blockIdx.z == 0 && wave == 0) {
             if (lane == 0) items[at] = item;
             if (lane < item.count) order[at * 16 + lane] = row;
         }
+    } else if constexpr (kFind != kListed) {
+        static_assert(kFoundAdapters * 4 <= kAll, "counts have the operands' place");
+        find_rows<T, W, kFind>(ids, M, adapters, at, reinterpret_cast<int32_t *>(lds), places[0], item);
+        if (blockIdx.y == 0 && blockIdx.z == 0 && wave == 0) {
+            if (lane == 0) items[at] = item;
+            if (lane < item.count) order[at * T + lane] = places[0][lane];
+        }
     } else {
         item = items[at];
     }
     if (item.count == 0) return;
-    const int32_t *const rows = kFew ? places[wave] : (const int32_t *)order + (int64_t)at * T;
+    const int32_t *const rows = kFind == kFew ? places[wave] : kFind != kListed ? places[0] : (const int32_t *)order + (int64_t)at * T;
     const int32_t r0 = blockIdx.y * Q, k_from = blockIdx.z * piece, k_to = k_from + piece < K ? k_from + piece : K;
     const int in = lane / 8, eighth = lane % 8;                 // of the rows that are loaded
     const uint16_t *from[2 * (RT + QT)];
@@ -506,15 +587,15 @@ struct Range {
 };
 
 // Items of sixteen rows: every wave has columns of its own, 64 at a time, and waits for no other.  64 rows of 32 adapters, rank 16, 8192 columns: 6.5
-// us, two thirds of it the launch and three latencies, one after the other: the item, what it names, the result.
+// us, two thirds of it the launch and three latencies, one after the other: the item, what it names, the result.  kRows: an item for every row, some of none.
 constexpr int kFewWaves = 4;
 
-template <int S, bool kFew, bool kNarrow, bool kStreams>
+template <int S, bool kRows, bool kNarrow, bool kStreams>
 __global__ __launch_bounds__(64 * kFewWaves) void expand_few_kernel(const Expansion p)
 {
     static_assert(16 * kResult <= 64 * kColumn<S>, "results have the columns' place");
     __shared__ __align__(16) uint8_t lds[kFewWaves][64 * kColumn<S>];
-    const int32_t at = kFew ? (int32_t)blockIdx.x : item_of(blockIdx.x, gridDim.x);
+    const int32_t at = kRows ? (int32_t)blockIdx.x : item_of(blockIdx.x, gridDim.x);
     SixteenRows<S, kNarrow, kStreams> sixteen(p, p.order + (int64_t)at * 16);
     const Item item = p.items[at];
     if (item.count == 0) return;
