@@ -63,12 +63,12 @@ struct ManyRows {
 // 8192 columns in three slices: 1024 rows of 4 adapters of rank 16 22.2 -> 27.0, of 8 of rank 64 35.1 -> 32.5.
 // k is cut where that gives more workgroups, as far as one for every CU: a workgroup of many rows has its CU's LDS for itself (one more than 256
 // is a round more: 4096 rows of 4 adapters 15.6 -> 22.6); of few a second one gains nothing (64 rows 12.8, with twice as many 13.6), and what is cut
-// has to be joined again (more than four pieces: 64 rows of 4 adapters 12.9 -> 14.6).
-// Items are found by those who take them, which saves the launch that lists them (333 rows 15.4 -> 13.3 us, 4096 of 4 adapters 42.6 -> 40.2, of 200
+// has to be joined again (more than four pieces: 64 rows of 4 adapters of rank 16 12.9 -> 14.6).
+// Items are found by those who take them, which saves the launch that lists them (333 rows 15.4 -> 13.0 us, 4096 of 4 adapters 42.6 -> 39.9, of 200
 // 97.4 -> 94.4); more than 4096 rows only where no workgroup waits for another (6000 rows 32.9 -> 28.7; 8192 of 64 adapters, three such rounds, 68 -> 72).
 // Few rows, without barriers, an item a row: 64 rows of 64 adapters of rank 64 49.9 -> 30.1, 128 of 200 of rank 16 32.5 -> 21.8; of few adapters the many
 // workgroups of no item cost more (64 rows of 4 of rank 64 14.7 -> 21.7, 128 of 32 31.7 -> 38.9; 48 of 8 still 16.5 -> 14.6).
-// Columns: two workgroups of the second launch for every CU (64 rows 13.2 us, with four 14.3; 4096 42.3 and 44.2).  From 20 Mi outputs on these go past the
+// Columns: two workgroups of the second launch for every CU (64 rows 13.2 us, with four 14.3; 4096 42.3 -> 44.2 before rows were found in the first).  From 20 Mi outputs on these go past the
 // caches (4096 x 5376 44.2 -> 42.3, 4096 x 8192 58.0 -> 55.0; 2048 x 8192 34.7 -> 37.5; of 200 adapters 4096 x 8192 102 -> 98).
 constexpr int64_t kTallRows = 2048, kWorkgroupsOfFew = 256, kWorkgroupsOfMany = 256, kMostSplits = 4, kWorkgroupsOfColumns = 512,
                   kStreamFrom = (int64_t)20 << 20;

@@ -45,6 +45,11 @@ __device__ __forceinline__ int32_t count_up(int32_t *at, int32_t a, int32_t adap
     return found;
 }
 
+__device__ __forceinline__ int32_t wave_sums(int32_t v)
+{
+    return (int32_t)wave_scan((uint32_t)v, [](uint32_t a, uint32_t b) { return a + b; });
+}
+
 __global__ __launch_bounds__(1024) void group_kernel(Global<const int32_t> ids, int32_t M, int32_t adapters, int32_t tile, Global<int32_t> order,
                                                      Global<Item> items, int32_t most_items)
 {
@@ -75,12 +80,7 @@ __global__ __launch_bounds__(1024) void group_kernel(Global<const int32_t> ids, 
     for (int a0 = 0; a0 < adapters; a0 += 1024) {
         const int a = a0 + (int)threadIdx.x;
         const int32_t n = a < adapters ? at[a] : 0, pieces = (n + tile - 1) / tile;
-        int32_t p = pieces;
-#pragma unroll
-        for (int d = 1; d < 64; d *= 2) {
-            const int32_t other = __shfl_up(p, d);
-            if (lane >= d) p += other;
-        }
+        const int32_t p = wave_sums(pieces);
         __syncthreads();
         if (lane == 63) parts[wave] = p;
         __syncthreads();
@@ -172,12 +172,7 @@ __device__ __forceinline__ void find_rows(const int32_t *ids, int32_t M, int32_t
         n[e] = at[threadIdx.x * kEach + e];
         pieces += (n[e] + T - 1) / T;
     }
-    int32_t upto = pieces;
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-        const int32_t other = __shfl_up(upto, d);
-        if (lane >= d) upto += other;
-    }
+    const int32_t upto = wave_sums(pieces);
     if (lane == 63) parts[0][wave] = upto;
     __syncthreads();
     int32_t first = upto - pieces;
@@ -237,8 +232,8 @@ __device__ __forceinline__ int32_t item_of(uint32_t x, uint32_t count) { return 
 // ---------------------------------------------------------------- t = A x
 // A workgroup has an item's rows, 16 RT of them, 16 QT rows of A and a piece of k, of which its W waves take 64 in turn; their sums are
 // added in order through LDS.  Sums of the pieces go to t [split][M][R].  A wave's next step is on its way
-// while it multiplies one; a second gained nothing.  64 rows of 32 adapters, 48 x 5376: 6.5 us, 2.5 TB/s of A; 4096 rows of 4, 64 x 5376: 15.6, the
-// 44 MB of x at 2.8 TB/s, of which a workgroup has a CU's LDS and 128 KB on their way.
+// while it multiplies one; a second gained nothing.  64 rows of 32 adapters, 48 x 5376: 6.2 us, 2.7 TB/s of A; 4096 rows of 4, 64 x 5376: 14.3 without
+// what finds the rows (3 more), the 44 MB of x at 3.1 TB/s, of which a workgroup has a CU's LDS and 128 KB on their way.
 // kFind: items are found here, and the first workgroup of each writes it down for the launch that follows.
 
 constexpr int kStep = 64;
@@ -586,7 +581,7 @@ struct Range {
     }
 };
 
-// Items of sixteen rows: every wave has columns of its own, 64 at a time, and waits for no other.  64 rows of 32 adapters, rank 16, 8192 columns: 6.5
+// Items of sixteen rows: every wave has columns of its own, 64 at a time, and waits for no other.  64 rows of 32 adapters, rank 16, 8192 columns: 7.4
 // us, two thirds of it the launch and three latencies, one after the other: the item, what it names, the result.  kRows: an item for every row, some of none.
 constexpr int kFewWaves = 4;
 
@@ -631,8 +626,8 @@ __global__ __launch_bounds__(64 * kFewWaves) void expand_few_kernel(const Expans
 }
 
 // Items of 64 rows: four waves of sixteen share 64 columns at a time, in two places in turn, so that B is read once for all of them (every sixteen rows
-// reading it for themselves were bound by that: 4096 rows, rank 64, 5376 columns 28 us).  What bounds it now is latency between its barriers, four
-// workgroups a CU: 21 us for the 88 MB of out, 4.2 TB/s.
+// reading it for themselves were bound by that: 4096 rows, rank 64, 5376 columns 28 us).  What bounds it now is latency between its barriers, two
+// workgroups a CU: 22 us for the 88 MB of out, 4.0 TB/s.
 template <int S, bool kStreams>
 __global__ __launch_bounds__(256) void expand_many_kernel(const Expansion p)
 {

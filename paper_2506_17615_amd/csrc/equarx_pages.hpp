@@ -30,21 +30,9 @@ constexpr uint32_t kMany = (1u << 30) + 1;
 
 __device__ __forceinline__ uint32_t add(uint32_t a, uint32_t b) { return a + b < kMany ? a + b : kMany; }
 
-// The other lane's value, zero where the row of sixteen has none.
-template <int kCtrl, int kRows = 0xf>
-__device__ __forceinline__ uint32_t shifted(uint32_t v)
-{
-    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, kCtrl, kRows, 0xf, false);
-}
-
 __device__ __forceinline__ uint32_t wave_scan(uint32_t v)
 {
-    v = add(v, shifted<0x111>(v));              // row_shr:1, 2, 4, 8
-    v = add(v, shifted<0x112>(v));
-    v = add(v, shifted<0x114>(v));
-    v = add(v, shifted<0x118>(v));
-    v = add(v, shifted<0x142, 0xa>(v));         // row_bcast:15 into rows 1 and 3, row_bcast:31 into rows 2 and 3
-    return add(v, shifted<0x143, 0xc>(v));
+    return equarx::wave_scan(v, [](uint32_t a, uint32_t b) { return add(a, b); });
 }
 
 struct Scan {

@@ -20,6 +20,25 @@ struct Divisor {
     __device__ __forceinline__ uint32_t of(uint32_t n) const { return (__umulhi(n, magic) + n) >> shift; }
 };
 
+// The other lane's value, zero where the row of sixteen has none.
+template <int kCtrl, int kRows = 0xf>
+__device__ __forceinline__ uint32_t shifted(uint32_t v)
+{
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, kCtrl, kRows, 0xf, false);
+}
+
+// A lane's value and those before it, as `add` adds; add(v, 0) is v.
+template <typename F>
+__device__ __forceinline__ uint32_t wave_scan(uint32_t v, F add)
+{
+    v = add(v, shifted<0x111>(v));              // row_shr:1, 2, 4, 8
+    v = add(v, shifted<0x112>(v));
+    v = add(v, shifted<0x114>(v));
+    v = add(v, shifted<0x118>(v));
+    v = add(v, shifted<0x142, 0xa>(v));         // row_bcast:15 into rows 1 and 3, row_bcast:31 into rows 2 and 3
+    return add(v, shifted<0x143, 0xc>(v));
+}
+
 // ---------------------------------------------------------------- rows of bf16
 
 // Elements [col, col + 8) of a row of `cols`; zeros past its end.
