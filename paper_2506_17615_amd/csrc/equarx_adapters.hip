@@ -38,6 +38,7 @@ inline size_t row_bytes(int64_t rows, int64_t cols, int64_t stride) { return (si
 // How a call is cut, by its sizes alone.
 struct Cut {
     Find find;              // how those who take the items have them
+    bool half;              // an item of many rows is two workgroups'
     bool few_of_each;       // many items of few rows: what counts is reading A
     int tile;               // rows of an item, at most
     int64_t items;          // at most
@@ -45,18 +46,24 @@ struct Cut {
     size_t order, list, bytes;              // of the workspace: t from 0 on
 };
 
-// Rows that are taken together, rows of A and waves of a workgroup.
+// Rows that are taken together, rows of A and waves of a workgroup; kParts workgroups have an item's rows.
 struct FewRows {
-    static constexpr int RT = 1, QT = 1, W = 8;
+    static constexpr int RT = 1, QT = 1, W = 8, kParts = 1;
 };
 // Where there are workgroups enough, of items of few rows that share none of A, more rows of A to one of x: 256 rows of 200 adapters of rank 16 39.4 ->
 // 35.2 us, 64 of 32 of rank 64 28.8 -> 25.9, 4096 of 200 112 -> 102; with fewer workgroups it loses (1 row 7.6 -> 8.3, 128 of 32 16.4 -> 17.1), and with many rows
 // of an adapter (512 of 4 of rank 64 23.3 -> 24.3).
 struct FewOfEach {
-    static constexpr int RT = 1, QT = 3, W = 8;
+    static constexpr int RT = 1, QT = 3, W = 8, kParts = 1;
+};
+// Half of an item's rows, where the workgroups are at most half as many as CUs, so that k is cut in two at least: us by 64 rows -> by 32: 2048 rows of 4 adapters,
+// 64 x 5376, 29.0 -> 27.1, 3000 of one 31.6 -> 28.6, 2048 of 16, two slices of 32 x 2048, 20.3 -> 17.4; in fewer pieces it loses (2048 of 64 47.3 -> 53.0,
+// 3500 of 16 43.2 -> 48.1).  It is so with 4096 rows and 64 adapters at most, whose rows are found.
+struct HalfMany {
+    static constexpr int RT = 2, QT = 4, W = 8, kParts = 2;
 };
 struct ManyRows {
-    static constexpr int RT = 4, QT = 4, W = 8;
+    static constexpr int RT = 4, QT = 4, W = 8, kParts = 1;
 };
 
 // Rows of one adapter are taken sixteen together, or 64: from 2048 rows on, 32 to an adapter or more.  Measured on MI355X, us by sixteen -> by 64, 5376 to
@@ -68,8 +75,8 @@ struct ManyRows {
 // 97.4 -> 94.4); more than 4096 rows only where no workgroup waits for another (6000 rows 32.9 -> 28.7; 8192 of 64 adapters, three such rounds, 68 -> 72).
 // Few rows, without barriers, an item a row: 64 rows of 64 adapters of rank 64 49.9 -> 30.1, 128 of 200 of rank 16 32.5 -> 21.8; of few adapters the many
 // workgroups of no item cost more (64 rows of 4 of rank 64 14.7 -> 21.7, 128 of 32 31.7 -> 38.9; 48 of 8 still 16.5 -> 14.6).
-// Columns: two workgroups of the second launch for every CU (64 rows 13.2 us, with four 14.3; 4096 42.3 -> 44.2 before rows were found in the first).  From 20 Mi outputs on these go past the
-// caches (4096 x 5376 44.2 -> 42.3, 4096 x 8192 58.0 -> 55.0; 2048 x 8192 34.7 -> 37.5; of 200 adapters 4096 x 8192 102 -> 98).
+// Columns: two workgroups of the second launch for every CU (64 rows 13.2 us, with four 14.3; 4096 42.3 -> 44.2 as the rows were still listed).  From 20 Mi
+// outputs on these go past the caches (4096 x 5376 44.2 -> 42.3, 4096 x 8192 58.0 -> 55.0; 2048 x 8192 34.7 -> 37.5; of 200 adapters 4096 x 8192 102 -> 98).
 constexpr int64_t kTallRows = 2048, kWorkgroupsOfFew = 256, kWorkgroupsOfMany = 256, kMostSplits = 4, kWorkgroupsOfColumns = 512,
                   kStreamFrom = (int64_t)20 << 20;
 
@@ -84,13 +91,14 @@ Cut cut_of(const Sizes &z)
     c.few_of_each = z.M < 32 * groups && (z.M / 16 + groups) * ((R + 15) / 16) >= kWorkgroupsOfFew;
     const int rank_tile = 16 * (tall ? ManyRows::QT : c.few_of_each ? FewOfEach::QT : FewRows::QT), waves = 8;
     c.rank_tiles = (int32_t)((R + rank_tile - 1) / rank_tile);
+    c.half = tall && HalfMany::kParts * c.items * c.rank_tiles <= kWorkgroupsOfMany / 2;
     const int64_t steps = (z.K + kStep - 1) / kStep;
     auto limited = [](int64_t v, int64_t hi) { return v < 1 ? 1 : v < hi ? v : hi; };
-    const int64_t busy = (z.M / c.tile + groups) * c.rank_tiles;
+    const int64_t busy = tall ? c.items * c.rank_tiles * (c.half ? HalfMany::kParts : 1) : (z.M / c.tile + groups) * c.rank_tiles;
     const int64_t splits = limited(tall ? kWorkgroupsOfMany / busy : (kWorkgroupsOfFew + busy / 2) / busy, limited((steps + waves - 1) / waves, kMostSplits));
     c.piece = (int32_t)((steps + splits - 1) / splits * kStep);
     c.splits = (int32_t)((z.K + c.piece - 1) / c.piece);
-    const bool long_found = tall && c.items * c.rank_tiles * c.splits <= kWorkgroupsOfMany;
+    const bool long_found = tall && busy * c.splits <= kWorkgroupsOfMany;
     c.find = few ? kFew : z.adapters > kFoundAdapters ? kListed : z.M <= kFound * 64 * waves ? kFound : long_found && z.M <= kFoundLong * 64 * waves ? kFoundLong : kListed;
     // columns of a workgroup: as many as leave enough workgroups
     c.columns = tall ? 64 : 64 * kFewWaves;
@@ -115,12 +123,12 @@ void launch(const Sizes &z, const Cut &c, const uint16_t *x, int64_t x_stride, c
     Item *const items = reinterpret_cast<Item *>(workspace + c.list);
     const int32_t R = z.rank * z.slices;
     if (kFind == kListed) ctx.launch(group_kernel, 1, 1024, ids, z.M, z.adapters, c.tile, order, items, c.items);
-    ctx.launch3d(shrink_kernel<S::RT, S::QT, S::W, kFind>, (unsigned)c.items, (unsigned)c.rank_tiles, (unsigned)c.splits, 64 * S::W, x, x_stride, a,
+    ctx.launch3d(shrink_kernel<S::RT, S::QT, S::W, S::kParts, kFind>, (unsigned)(c.items * S::kParts), (unsigned)c.rank_tiles, (unsigned)c.splits, 64 * S::W, x, x_stride, a,
                  t, z.M, z.K, R, c.piece, order, items, ids, z.adapters);
     const Expansion p{out, out_stride, b, factors, t, (int32_t)z.M, (int32_t)z.N, z.rank, z.slices, c.splits, c.chunks, c.tile, order, items, cut};
     auto expand = [&](auto kernel) { ctx.launch2d(kernel, (unsigned)c.items, (unsigned)cut.first_chunk[z.slices], 256, p); };
     const bool streams = z.M * z.N >= kStreamFrom;
-    if constexpr (S::RT > 1) {
+    if constexpr (S::RT * S::kParts > 1) {
         if (streams) {
             expand(z.rank <= 32 ? expand_many_kernel<1, true> : z.rank <= 64 ? expand_many_kernel<2, true> : expand_many_kernel<4, true>);
         } else {
@@ -192,14 +200,14 @@ int equarx_adapters(const void *x_bf16, int64_t x_stride, const void *a_bf16, co
     }
     auto pick = [&](auto shape) {
         using S = decltype(shape);
-        if constexpr (S::RT == 1) {
+        if constexpr (S::RT * S::kParts == 1) {
             if (c.find == kFew) return launch<S, kFew>;
         } else {
             if (c.find == kFoundLong) return launch<S, kFoundLong>;
         }
         return c.find == kFound ? launch<S, kFound> : launch<S, kListed>;
     };
-    auto *const go = c.tile != 16 ? pick(ManyRows{}) : c.few_of_each ? pick(FewOfEach{}) : pick(FewRows{});
+    auto *const go = c.half ? launch<HalfMany, kFound> : c.tile != 16 ? pick(ManyRows{}) : c.few_of_each ? pick(FewOfEach{}) : pick(FewRows{});
     go(z, c, static_cast<const uint16_t *>(x_bf16), x_stride, static_cast<const uint16_t *>(a_bf16), static_cast<const uint16_t *>(b_bf16), factors, ids,
        cut, static_cast<uint16_t *>(out_bf16), out_stride, static_cast<uint8_t *>(workspace), ctx);
     return ctx.status();

@@ -230,7 +230,7 @@ __device__ __forceinline__ u32x4 load8(const uint16_t *p) { return *reinterpret_
 __device__ __forceinline__ int32_t item_of(uint32_t x, uint32_t count) { return (int32_t)((x & 7) * (count / 8) + x / 8); }
 
 // ---------------------------------------------------------------- t = A x
-// A workgroup has an item's rows, 16 RT of them, 16 QT rows of A and a piece of k, of which its W waves take 64 in turn; their sums are
+// A workgroup has an item's rows or one of Parts of them, 16 RT, 16 QT rows of A and a piece of k, of which its W waves take 64 in turn; their sums are
 // added in order through LDS.  Sums of the pieces go to t [split][M][R].  A wave's next step is on its way
 // while it multiplies one; a second gained nothing.  64 rows of 32 adapters, 48 x 5376: 6.2 us, 2.7 TB/s of A; 4096 rows of 4, 64 x 5376: 14.3 without
 // what finds the rows (3 more), the 44 MB of x at 3.1 TB/s, of which a workgroup has a CU's LDS and 128 KB on their way.
@@ -241,7 +241,7 @@ constexpr int kStep = 64;
 // How an item is found: few rows, by a list, or, with so many rows a lane, among all.
 enum Find { kFew = -1, kListed = 0, kFound = 8, kFoundLong = 16 };
 
-template <int RT, int QT, int W, Find kFind>
+template <int RT, int QT, int W, int Parts, Find kFind>
 __global__ __launch_bounds__(64 * W) void shrink_kernel(Global<const uint16_t> x, int64_t x_stride, Global<const uint16_t> a, Global<float> t,
                                                         int32_t M, int32_t K, int32_t R, int32_t piece, Global<int32_t> order, Global<Item> items,
                                                         Global<const int32_t> ids, int32_t adapters)
@@ -249,9 +249,9 @@ __global__ __launch_bounds__(64 * W) void shrink_kernel(Global<const uint16_t> x
     constexpr int T = 16 * RT, Q = 16 * QT, kPitch = Q + 4, kTile = (T + Q) * 2 * kStep;
     constexpr int kSums = W * 16 * kPitch * 4, kAll = W * kTile > kSums ? W * kTile : kSums;
     __shared__ __align__(16) uint8_t lds[kAll];
-    __shared__ int32_t places[kFind == kFew ? W : 1][kFind == kListed ? 1 : T];
+    __shared__ int32_t places[kFind == kFew ? W : 1][kFind == kListed ? 1 : T * Parts];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l = lane & 15, g = lane >> 4;
-    const int32_t at = kFind == kFew ? (int32_t)blockIdx.x : item_of(blockIdx.x, gridDim.x);
+    const int32_t index = kFind == kFew ? (int32_t)blockIdx.x : item_of(blockIdx.x, gridDim.x), at = index / Parts, part = index % Parts;
     Item item;
     if constexpr (kFind == kFew) {
         const int32_t row = find_item(ids, M, adapters, at, places[wave], item);
@@ -261,16 +261,17 @@ __global__ __launch_bounds__(64 * W) void shrink_kernel(Global<const uint16_t> x
         }
     } else if constexpr (kFind != kListed) {
         static_assert(kFoundAdapters * 4 <= kAll, "counts have the operands' place");
-        find_rows<T, W, kFind>(ids, M, adapters, at, reinterpret_cast<int32_t *>(lds), places[0], item);
-        if (blockIdx.y == 0 && blockIdx.z == 0 && wave == 0) {
+        find_rows<T * Parts, W, kFind>(ids, M, adapters, at, reinterpret_cast<int32_t *>(lds), places[0], item);
+        if (part == 0 && blockIdx.y == 0 && blockIdx.z == 0 && wave == 0) {
             if (lane == 0) items[at] = item;
-            if (lane < item.count) order[at * T + lane] = places[0][lane];
+            if (lane < item.count) order[at * (T * Parts) + lane] = places[0][lane];
         }
     } else {
         item = items[at];
     }
-    if (item.count == 0) return;
-    const int32_t *const rows = kFind == kFew ? places[wave] : kFind != kListed ? places[0] : (const int32_t *)order + (int64_t)at * T;
+    item.count = item.count - part * T < T ? item.count - part * T : T;
+    if (item.count <= 0) return;
+    const int32_t *const rows = (kFind == kFew ? places[wave] : kFind != kListed ? places[0] : (const int32_t *)order + (int64_t)at * (T * Parts)) + part * T;
     const int32_t r0 = blockIdx.y * Q, k_from = blockIdx.z * piece, k_to = k_from + piece < K ? k_from + piece : K;
     const int in = lane / 8, eighth = lane % 8;                 // of the rows that are loaded
     const uint16_t *from[2 * (RT + QT)];

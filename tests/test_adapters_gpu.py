@@ -101,13 +101,13 @@ def test_rows_of_every_kind(M, K, widths, rank, adapters, kind):
 
 # Where a call goes over from one way of finding an item's rows to another, and the most and the fewest of each way.
 EDGES = [(24, 3), (25, 2), (25, 5), (48, 8), (64, 10), (64, 11), (65, 32), (65, 33), (256, 127), (256, 128), (257, 3), (511, 5), (512, 1024), (513, 1023),
-         (513, 1025), (2047, 1), (4095, 120), (4096, 127), (4096, 130), (4096, 1024), (4097, 4), (4097, 200), (6001, 1), (8192, 4), (8192, 100), (8193, 4)]
+         (513, 1025), (2047, 1), (4095, 120), (4096, 127), (4096, 130), (4096, 1024), (2048, 64), (2048, 30), (2500, 24), (3900, 3), (4097, 4), (4097, 200), (6001, 1), (8192, 4), (8192, 100), (8193, 4)]
 
 
 @pytest.mark.parametrize("kind", ("mixed", "grouped", "one", "none"))
 @pytest.mark.parametrize("M,adapters", EDGES)
 def test_every_row_is_found(M, adapters, kind):
-    case = _case(M + adapters, M, 40, (30, 8), 8, adapters, kind)
+    case = _case(M + adapters, M, 1100 if M * adapters < 10000 else 40, (30, 8), 8, adapters, kind)
     case["ids"][::37] = torch.tensor([-2 ** 31, 2 ** 31 - 1, adapters, 1 << 16])[torch.arange(len(case["ids"][::37])) % 4]
     _check(case, _call(_on(case)).cpu())
 
