@@ -42,6 +42,7 @@ struct Cut {
     bool few_of_each;       // many items of few rows: what counts is reading A
     int tile;               // rows of an item, at most
     int64_t items;          // at most
+    int32_t together;       // items of one XCD that follow each other
     int32_t rank_tiles, piece, splits, columns, chunks;
     size_t order, list, bytes;              // of the workspace: t from 0 on
 };
@@ -75,6 +76,9 @@ struct ManyRows {
 // 97.4 -> 94.4); more than 4096 rows only where no workgroup waits for another (6000 rows 32.9 -> 28.7; 8192 of 64 adapters, three such rounds, 68 -> 72).
 // Few rows, without barriers, an item a row: 64 rows of 64 adapters of rank 64 49.9 -> 30.1, 128 of 200 of rank 16 32.5 -> 21.8; of few adapters the many
 // workgroups of no item cost more (64 rows of 4 of rank 64 14.7 -> 21.7, 128 of 32 31.7 -> 38.9; 48 of 8 still 16.5 -> 14.6).
+// Items of an XCD that follow each other: as many as an adapter has in the mean, and by sixteen half a one more, since its last is seldom full.  With
+// an eighth of all for each XCD, what is left empty at the end was the last ones' (1024 rows of 200 adapters 65.2 -> 53.0 us, 8192 158 -> 124, 333 of rank
+// 64 116 -> 102); without the half 1024 of 32 of rank 64 60.4 -> 63.2, with it by 64 2048 of 8 27.7 -> 29.2.
 // Columns: two workgroups of the second launch for every CU (64 rows 13.2 us, with four 14.3; 4096 42.3 -> 44.2 as the rows were still listed).  From 20 Mi
 // outputs on these go past the caches (4096 x 5376 44.2 -> 42.3, 4096 x 8192 58.0 -> 55.0; 2048 x 8192 34.7 -> 37.5; of 200 adapters 4096 x 8192 102 -> 98).
 constexpr int64_t kTallRows = 2048, kWorkgroupsOfFew = 256, kWorkgroupsOfMany = 256, kMostSplits = 4, kWorkgroupsOfColumns = 512,
@@ -88,6 +92,7 @@ Cut cut_of(const Sizes &z)
     const bool few = z.M <= kFewRows && (z.M <= 24 || (z.M <= 64 ? 6 : 2) * groups >= z.M);
     c.tile = 16 * (tall ? ManyRows::RT : FewRows::RT);
     c.items = few ? z.M : (z.M / c.tile + groups + 7) / 8 * 8;
+    c.together = (int32_t)((2 * z.M + (tall ? 2 : 3) * groups * c.tile - 1) / (2 * groups * c.tile));
     c.few_of_each = z.M < 32 * groups && (z.M / 16 + groups) * ((R + 15) / 16) >= kWorkgroupsOfFew;
     const int rank_tile = 16 * (tall ? ManyRows::QT : c.few_of_each ? FewOfEach::QT : FewRows::QT), waves = 8;
     c.rank_tiles = (int32_t)((R + rank_tile - 1) / rank_tile);
@@ -124,8 +129,8 @@ void launch(const Sizes &z, const Cut &c, const uint16_t *x, int64_t x_stride, c
     const int32_t R = z.rank * z.slices;
     if (kFind == kListed) ctx.launch(group_kernel, 1, 1024, ids, z.M, z.adapters, c.tile, order, items, c.items);
     ctx.launch3d(shrink_kernel<S::RT, S::QT, S::W, S::kParts, kFind>, (unsigned)(c.items * S::kParts), (unsigned)c.rank_tiles, (unsigned)c.splits, 64 * S::W, x, x_stride, a,
-                 t, z.M, z.K, R, c.piece, order, items, ids, z.adapters);
-    const Expansion p{out, out_stride, b, factors, t, (int32_t)z.M, (int32_t)z.N, z.rank, z.slices, c.splits, c.chunks, c.tile, order, items, cut};
+                 t, z.M, z.K, R, c.piece, order, items, ids, z.adapters, c.together * S::kParts);
+    const Expansion p{out, out_stride, b, factors, t, (int32_t)z.M, (int32_t)z.N, z.rank, z.slices, c.splits, c.chunks, c.together, order, items, cut};
     auto expand = [&](auto kernel) { ctx.launch2d(kernel, (unsigned)c.items, (unsigned)cut.first_chunk[z.slices], 256, p); };
     const bool streams = z.M * z.N >= kStreamFrom;
     if constexpr (S::RT * S::kParts > 1) {

@@ -225,9 +225,13 @@ __device__ __forceinline__ u32x4 load8(const uint16_t *p) { return *reinterpret_
 // cycle at 64 bytes a lane's quad would be one), and those bounded both kernels (4096 rows, rank 64: 18 and 32 us).  So rows come in whole
 // 128 bytes, eight lanes a row, and through LDS to the lanes that multiply; each wave has a place of its own there, and no barrier is needed.
 
-// Items of one adapter, which follow each other, go to one XCD: workgroups go round the eight, `x` of `count` (a multiple of eight) is
-// item x / 8 of the x % 8th eighth.
-__device__ __forceinline__ int32_t item_of(uint32_t x, uint32_t count) { return (int32_t)((x & 7) * (count / 8) + x / 8); }
+// Items of one adapter, which follow each other, go to one XCD, and all XCDs have as many: `together` items, as many as an adapter has in the mean, are one
+// XCD's, the next the next one's.  Workgroups go round the eight: which item `x` of `count` (a multiple of eight) is.
+__device__ __forceinline__ int32_t item_of(uint32_t x, uint32_t count, uint32_t together)
+{
+    const uint32_t turns = x / (8 * together) * (8 * together), each = turns + 8 * together <= count ? together : (count - turns) / 8;
+    return (int32_t)(turns + (x & 7) * each + (x - turns) / 8);
+}
 
 // ---------------------------------------------------------------- t = A x
 // A workgroup has an item's rows or one of Parts of them, 16 RT, 16 QT rows of A and a piece of k, of which its W waves take 64 in turn; their sums are
@@ -244,14 +248,14 @@ enum Find { kFew = -1, kListed = 0, kFound = 8, kFoundLong = 16 };
 template <int RT, int QT, int W, int Parts, Find kFind>
 __global__ __launch_bounds__(64 * W) void shrink_kernel(Global<const uint16_t> x, int64_t x_stride, Global<const uint16_t> a, Global<float> t,
                                                         int32_t M, int32_t K, int32_t R, int32_t piece, Global<int32_t> order, Global<Item> items,
-                                                        Global<const int32_t> ids, int32_t adapters)
+                                                        Global<const int32_t> ids, int32_t adapters, int32_t together)
 {
     constexpr int T = 16 * RT, Q = 16 * QT, kPitch = Q + 4, kTile = (T + Q) * 2 * kStep;
     constexpr int kSums = W * 16 * kPitch * 4, kAll = W * kTile > kSums ? W * kTile : kSums;
     __shared__ __align__(16) uint8_t lds[kAll];
     __shared__ int32_t places[kFind == kFew ? W : 1][kFind == kListed ? 1 : T * Parts];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l = lane & 15, g = lane >> 4;
-    const int32_t index = kFind == kFew ? (int32_t)blockIdx.x : item_of(blockIdx.x, gridDim.x), at = index / Parts, part = index % Parts;
+    const int32_t index = kFind == kFew ? (int32_t)blockIdx.x : item_of(blockIdx.x, gridDim.x, together), at = index / Parts, part = index % Parts;
     Item item;
     if constexpr (kFind == kFew) {
         const int32_t row = find_item(ids, M, adapters, at, places[wave], item);
@@ -368,7 +372,7 @@ struct Expansion {
     int64_t out_stride;
     Global<const uint16_t> b;
     Global<const float> factors, t;
-    int32_t M, N, rank, slices, splits, chunks, tile;
+    int32_t M, N, rank, slices, splits, chunks, together;
     Global<const int32_t> order;
     Global<const Item> items;
     Slices cut;
@@ -591,7 +595,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void expand_few_kernel(const Expans
 {
     static_assert(16 * kResult <= 64 * kColumn<S>, "results have the columns' place");
     __shared__ __align__(16) uint8_t lds[kFewWaves][64 * kColumn<S>];
-    const int32_t at = kRows ? (int32_t)blockIdx.x : item_of(blockIdx.x, gridDim.x);
+    const int32_t at = kRows ? (int32_t)blockIdx.x : item_of(blockIdx.x, gridDim.x, p.together);
     SixteenRows<S, kNarrow, kStreams> sixteen(p, p.order + (int64_t)at * 16);
     const Item item = p.items[at];
     if (item.count == 0) return;
@@ -633,7 +637,7 @@ template <int S, bool kStreams>
 __global__ __launch_bounds__(256) void expand_many_kernel(const Expansion p)
 {
     __shared__ __align__(16) uint8_t lds[2][64 * kColumn<S>], results[4][16 * kResult];
-    const int32_t at = item_of(blockIdx.x, gridDim.x);
+    const int32_t at = item_of(blockIdx.x, gridDim.x, p.together);
     const int wave = threadIdx.x >> 6;
     SixteenRows<S, false, kStreams> sixteen(p, p.order + (int64_t)at * 64 + wave * 16);
     const Item item = p.items[at];
