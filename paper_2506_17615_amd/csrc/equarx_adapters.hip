@@ -52,7 +52,7 @@ struct FewRows {
     static constexpr int RT = 1, QT = 1, W = 8, kParts = 1;
 };
 // Where there are workgroups enough, of items of few rows that share none of A, more rows of A to one of x: 256 rows of 200 adapters of rank 16 39.4 ->
-// 35.2 us, 64 of 32 of rank 64 28.8 -> 25.9, 4096 of 200 112 -> 102; with fewer workgroups it loses (1 row 7.6 -> 8.3, 128 of 32 16.4 -> 17.1), and with many rows
+// 35.2 us, 64 of 32 of rank 64 28.8 -> 25.9, 4096 of 200 93.5 -> 88.1; with fewer workgroups it loses (1 row 7.6 -> 8.3, 128 of 32 16.4 -> 17.1), and with many rows
 // of an adapter (512 of 4 of rank 64 23.3 -> 24.3).
 struct FewOfEach {
     static constexpr int RT = 1, QT = 3, W = 8, kParts = 1;
@@ -67,8 +67,10 @@ struct ManyRows {
     static constexpr int RT = 4, QT = 4, W = 8, kParts = 1;
 };
 
-// Rows of one adapter are taken sixteen together, or 64: from 2048 rows on, 32 to an adapter or more.  Measured on MI355X, us by sixteen -> by 64, 5376 to
-// 8192 columns in three slices: 1024 rows of 4 adapters of rank 16 22.2 -> 27.0, of 8 of rank 64 35.1 -> 32.5.
+// Rows of one adapter are taken sixteen together, or 64, which reads A and B for more of them and leaves fewer workgroups.  Measured on MI355X, us by
+// sixteen -> by 64, 5376 to 8192 columns, R rows of A: R = 192, 1024 rows of 4 adapters 32.4 -> 30.0, of 32 60.4 -> 49.5, of 64 68.3 -> 62.9, of 100 81.7 -> 100,
+// 512 of 32 34.9 -> 34.3; R = 64, 1024 of 16 23.7 -> 22.8, of 64 38.2 -> 34.1, 512 of one 16.5 -> 18.7; R = 48, 1024 of 4 19.8 -> 21.4, 2048 of 8 30.5 -> 27.8, of 64
+// 47.3 -> 42.7, of 100 53.5 either way; R = 16, 2048 of one 21.4 -> 21.9, of 64 25.0 -> 31.4, of 100 26.9 -> 38.4, 4096 of 16 45.5 -> 39.4, of 128 52.6 -> 50.9.
 // k is cut where that gives more workgroups, as far as one for every CU: a workgroup of many rows has its CU's LDS for itself (one more than 256
 // is a round more: 4096 rows of 4 adapters 15.6 -> 22.6); of few a second one gains nothing (64 rows 12.8, with twice as many 13.6), and what is cut
 // has to be joined again (more than four pieces: 64 rows of 4 adapters of rank 16 12.9 -> 14.6).
@@ -81,14 +83,15 @@ struct ManyRows {
 // 64 116 -> 102); without the half 1024 of 32 of rank 64 60.4 -> 63.2, with it by 64 2048 of 8 27.7 -> 29.2.
 // Columns: two workgroups of the second launch for every CU (64 rows 13.2 us, with four 14.3; 4096 42.3 -> 44.2 as the rows were still listed).  From 20 Mi
 // outputs on these go past the caches (4096 x 5376 44.2 -> 42.3, 4096 x 8192 58.0 -> 55.0; 2048 x 8192 34.7 -> 37.5; of 200 adapters 4096 x 8192 102 -> 98).
-constexpr int64_t kTallRows = 2048, kWorkgroupsOfFew = 256, kWorkgroupsOfMany = 256, kMostSplits = 4, kWorkgroupsOfColumns = 512,
+constexpr int64_t kTallRows = 2048, kHighRank = 64, kWorkgroupsOfFew = 256, kWorkgroupsOfMany = 256, kMostSplits = 4, kWorkgroupsOfColumns = 512,
                   kStreamFrom = (int64_t)20 << 20;
 
 Cut cut_of(const Sizes &z)
 {
     Cut c{};
     const int64_t R = (int64_t)z.rank * z.slices, groups = z.M < z.adapters ? z.M : z.adapters;
-    const bool tall = z.M >= 32 * groups && z.M >= kTallRows && z.N >= 8;
+    const int64_t rows_of_each = R >= kHighRank ? 16 : R >= 48 || z.M >= 4096 ? 32 : 64;
+    const bool tall = z.M >= rows_of_each * groups && z.M >= (R >= kHighRank ? kTallRows / 2 : kTallRows) && z.N >= 8;
     const bool few = z.M <= kFewRows && (z.M <= 24 || (z.M <= 64 ? 6 : 2) * groups >= z.M);
     c.tile = 16 * (tall ? ManyRows::RT : FewRows::RT);
     c.items = few ? z.M : (z.M / c.tile + groups + 7) / 8 * 8;

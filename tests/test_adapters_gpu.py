@@ -82,7 +82,7 @@ SIZES = [(1, 8, (8,), 8, 1), (1, 4096, (4096, 2048, 2048), 16, 32), (3, 1, (1,),
          (100, 300, (31, 1, 900, 70), 64, 9), (31, 1024, (129,), 128, 6), (128, 333, (400, 1), 128, 2), (200, 2049, (333,), 40, 64),
          (333, 130, (1000,), 8, 5), (700, 96, (90,), 16, 300), (1000, 777, (300, 200), 56, 3), (4096, 256, (128,), 64, 4),
          (2111, 515, (77, 300, 5), 72, 8000), (200, 700, (300, 20), 16, 130), (256, 264, (70,), 48, 300), (64, 3, (7,), 128, 64), (2048, 90, (6,), 16, 2),
-         (5000, 8, (9, 8), 8, 20)]
+         (5000, 8, (9, 8), 8, 20), (1024, 700, (70, 40), 32, 64), (1030, 1200, (100, 30, 9), 128, 3), (1500, 513, (77,), 72, 90)]
 
 
 @pytest.mark.parametrize("kind", ("mixed", "grouped", "one", "distinct", "none"))
