@@ -76,6 +76,8 @@ class ShardedAttention:
             raise ValueError("ids: there are no adapters")
         nq, nk, more = self.heads * self.dim, self.kv_heads * self.dim, self.adapters
         max_queries = max(max_queries, -(-tokens // max(page_table.shape[0], 1)))      # no run can be shorter than the mean
+        # attention leaves rows of no sequence as they are: they would be another step's, or what the memory held
+        self.attended[:, :tokens].zero_()
         for p in range(self.shards):
             qkv, attended, cache, partial = self.qkv[p, :tokens], self.attended[p, :tokens], self.caches[p], self.partials[p, :tokens]
             eq.equarx_mx4_linear(x, *self.w_qkv[p], qkv, self.workspace)
@@ -91,13 +93,15 @@ class ShardedAttention:
 
     def __call__(self, x, slots, q_starts, page_table, lengths, max_queries, out, ids=None):
         """out bf16 [tokens, hidden] <- the layer for x bf16 [tokens, hidden], whose sequence b is q_starts[b] .. q_starts[b + 1] - 1
-        and stands at the end of lengths[b] tokens, its own among them; slots: where its keys and values go."""
+        and stands at the end of lengths[b] tokens, its own among them; slots: where its keys and values go.  Rows of no sequence
+        become zeros."""
         self._project(x, slots, q_starts, page_table, lengths, max_queries, ids)
         tokens = x.shape[0]
         eq.equarx_reduce_fused([self.partials[p, :tokens].reshape(-1) for p in range(self.shards)], self.wire_block, out.view(-1))
 
     def normed(self, x, slots, q_starts, page_table, lengths, max_queries, residual, weight, out, eps=1e-6, ids=None):
-        """The layer for normed rows x: residual <- residual + what __call__ writes, out <- its norm times weight, the next layer's x."""
+        """The layer for normed rows x: residual <- residual + what __call__ writes, out <- its norm times weight, the next layer's x.
+        Residual rows of no sequence stay as they are."""
         self._project(x, slots, q_starts, page_table, lengths, max_queries, ids)
         tokens = x.shape[0]
         eq.equarx_norm_reduced([self.partials[p, :tokens] for p in range(self.shards)], self.wire_block, weight, eps, residual, out)
@@ -129,7 +133,7 @@ class Requests:
     """Sequences in places of a page table on the device: what a step of them reads, made there by one launch or two.
 
     rows: of a step, at most.  A step's q_starts, slots and row_tags are those of its first `rows` rows; rows behind the last sequence have slot -1 and
-    tag -1, which no call writes or reads for."""
+    tag -1: nothing is kept in the cache for them, no adapter is theirs, and the layer adds nothing to them."""
 
     def __init__(self, sequences, width, pages, page, rows):
         self.page, self.pages = page, eq.alloc_pages(sequences, width, pages)
