@@ -591,7 +591,8 @@ size_t equarx_cache_attention_most_workspace_bytes(int32_t heads, int32_t dim, i
  *              tokens holds the entries of its first ceil(L / page) pages;
  *   lengths    int32 [sequences];
  *   free       int32 [pages]: a stack of the pages that nobody holds, free_count of
- *              them (int32 [1]), the top one last.
+ *              them (int32 [1]), the top one last;
+ *   seen       int32 [sequences] or NULL: written by equarx_pages_extend (below).
  *   sequences and width up to 2^20, pages up to 2^30, page from 1 to 65536, pages * page and
  *   the table up to 2^40 (EQUARX_BAD_SHAPE).  A page is one sequence's.  Values out of range are taken
  *   as the nearest in it (lengths, free_count) or for no page (table, when it is given back).
@@ -605,8 +606,15 @@ size_t equarx_cache_attention_most_workspace_bytes(int32_t heads, int32_t dim, i
  * more than `rows`; else if the pages that it and those before it want (as far as they passed these two) are more than the
  * stack holds, and it wants any.  Pages come from the top of the stack, in the same order.
  *
+ * With seen == NULL the rows of the step are those of the tokens that were given, without gaps: a sequence that gets none
+ * moves the rows of those after it.  With seen, rows are where they were asked for, so that activations laid out by counts
+ * belong to their sequences whoever gets none: sequence b has counts[b] rows (as far as `rows` go) behind those of the
+ * sequences before it, also where it got none (these rows then are as rows of no sequence); it gets none if its last
+ * row is beyond `rows`, where those that the table has no room for count too; and seen[b] is the length for
+ * equarx_cache_attention: 0 if it wanted tokens and got none, so that its rows see nothing and become zeros, else lengths[b].
+ *
  *   q_starts   int32 [sequences + 1]: rows of the step before each sequence's and, last,
- *              of all;
+ *              of all (with seen, `rows` at most);
  *   granted    int32 [sequences] or NULL: the tokens that it got;
  *   slots      int64 [rows]: where row r's token goes; -1 for rows of no sequence;
  *   positions  int32 [rows] or NULL: its place in its sequence, or -1;
@@ -623,6 +631,7 @@ typedef struct equarx_pages {
     int32_t *free_count;
     int64_t width, pages;
     int32_t sequences, page;
+    int32_t *seen;
 } equarx_pages;
 
 int equarx_pages_trim(const equarx_pages *pages, const int32_t *keep, void *stream);

@@ -86,7 +86,8 @@ class _CNormOutputs(ctypes.Structure):
 class _CPages(ctypes.Structure):
     """equarx_pages of include/equarx.h."""
     _fields_ = [("table", ctypes.c_void_p), ("lengths", ctypes.c_void_p), ("free", ctypes.c_void_p), ("free_count", ctypes.c_void_p),
-                ("width", ctypes.c_int64), ("pages", ctypes.c_int64), ("sequences", ctypes.c_int32), ("page", ctypes.c_int32)]
+                ("width", ctypes.c_int64), ("pages", ctypes.c_int64), ("sequences", ctypes.c_int32), ("page", ctypes.c_int32),
+                ("seen", ctypes.c_void_p)]
 
 
 # name -> (restype, argtypes); SIGNATURES mirrors include/equarx.h, DEVTOOLS_SIGNATURES include/equarx_devtools.h
@@ -898,11 +899,14 @@ def equarx_pages_trim(pages: Pages, page: int, keep) -> None:
     _check(load().equarx_pages_trim(ctypes.byref(c), _ptr(keep), _stream()), "equarx_pages_trim")
 
 
-def equarx_pages_extend(pages: Pages, page: int, counts, q_starts, slots, granted=None, positions=None, tags=None, row_tags=None) -> None:
+def equarx_pages_extend(pages: Pages, page: int, counts, q_starts, slots, granted=None, positions=None, tags=None, row_tags=None,
+                        seen=None) -> None:
     """Gives every sequence counts[b] more tokens, or none where table, rows or stack have no room for them (granted: what it got), and
     tells the rows of the step: q_starts int32 [sequences + 1], slots int64 [rows], positions int32 [rows], row_tags int32 [rows] its
-    sequence's of tags int32 [sequences]; -1 in rows of no sequence."""
-    status = _native.equarx_pages_extend(pages, page, counts, q_starts, slots, granted, positions, tags, row_tags)
+    sequence's of tags int32 [sequences]; -1 in rows of no sequence.  The rows are those of the tokens that were given; with seen int32
+    [sequences] they are where counts has them, those of a sequence that got none being no sequence's, and seen is its length for the
+    attention: 0 where it wanted tokens and got none."""
+    status = _native.equarx_pages_extend(pages, page, counts, q_starts, slots, granted, positions, tags, row_tags, seen)
     if status >= 0:
         return _check(status, "equarx_pages_extend")
     c = _need_pages(pages, page)
@@ -911,9 +915,10 @@ def equarx_pages_extend(pages: Pages, page: int, counts, q_starts, slots, grante
     _need_exactly(counts, torch.int32, c.sequences, "counts")
     _need_exactly(q_starts, torch.int32, c.sequences + 1, "q_starts")
     for t, count, what in ((granted, c.sequences, "granted"), (positions, rows, "positions"), (tags, c.sequences, "tags"),
-                           (row_tags, rows, "row_tags")):
+                           (row_tags, rows, "row_tags"), (seen, c.sequences, "seen")):
         if t is not None:
             _need_exactly(t, torch.int32, count, what)
+    c.seen = _ptr(seen)
     _check(load().equarx_pages_extend(ctypes.byref(c), _ptr(counts), _ptr(q_starts), _ptr(slots), _ptr(granted), _ptr(positions), _ptr(tags),
                                       _ptr(row_tags), rows, _stream()), "equarx_pages_extend")
 

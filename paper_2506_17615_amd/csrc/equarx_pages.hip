@@ -30,7 +30,7 @@ int check_pages(const equarx_pages *p)
 Pool pool_of(const equarx_pages &p)
 {
     const int64_t room = p.width * p.page;
-    return {p.table, p.lengths, p.free, p.free_count, p.width, (int32_t)p.pages, p.sequences, (int32_t)(room < INT32_MAX ? room : INT32_MAX),
+    return {p.table, p.lengths, p.free, p.free_count, p.seen, p.width, (int32_t)p.pages, p.sequences, (int32_t)(room < INT32_MAX ? room : INT32_MAX),
             Divisor((uint32_t)p.page)};
 }
 
@@ -75,7 +75,7 @@ int equarx_pages_extend(const equarx_pages *pages, const int32_t *counts, int32_
     if (pages->sequences == 0 && rows == 0) return EQUARX_OK;
     if (!q_starts || (pages->sequences > 0 && !counts) || (rows > 0 && !slots)) return EQUARX_NULL_POINTER;
     if (rows > 0 && pages->sequences > 0 && !tags != !row_tags) return EQUARX_NULL_POINTER;
-    if (misaligned(counts, 4) || misaligned(q_starts, 4) || misaligned(slots, 8) || misaligned(granted, 4) || misaligned(positions, 4) ||
+    if (misaligned(pages->seen, 4) || misaligned(counts, 4) || misaligned(q_starts, 4) || misaligned(slots, 8) || misaligned(granted, 4) || misaligned(positions, 4) ||
         misaligned(tags, 4) || misaligned(row_tags, 4))
         return EQUARX_MISALIGNED;
     Aliasing mem;
@@ -85,6 +85,7 @@ int equarx_pages_extend(const equarx_pages *pages, const int32_t *counts, int32_
     mem.reads(tags, sequences * 4);
     mem.writes(q_starts, (sequences + 1) * 4);
     mem.writes(granted, sequences * 4);
+    mem.writes(pages->seen, sequences * 4);
     mem.writes(slots, (size_t)rows * 8);
     mem.writes(positions, (size_t)rows * 4);
     mem.writes(row_tags, (size_t)rows * 4);

@@ -7,7 +7,7 @@ namespace equarx {
 namespace pages {
 
 struct Pool {
-    Global<int32_t> table, lengths, free, free_count;
+    Global<int32_t> table, lengths, free, free_count, seen;      // seen may be null
     int64_t width;
     int32_t pages, sequences, most;     // most: tokens that the table has room for, as far as a length can say it
     Divisor page;
@@ -66,7 +66,9 @@ __device__ __forceinline__ int32_t pages_of(const Pool &p, int32_t tokens) { ret
 
 __device__ __forceinline__ int32_t within(int32_t v, int32_t most) { return v < 0 ? 0 : v < most ? v : most; }
 
-// The last i of [0, n) with from[i] <= at, from[0] being 0.
+__device__ __forceinline__ uint32_t umin(uint32_t a, uint32_t b) { return a < b ? a : b; }
+
+// The last i of [0, n) with from[i] <= at, from[0] being one.
 template <typename T>
 __device__ __forceinline__ int32_t last_from(const T *from, int32_t n, uint32_t at)
 {
@@ -142,7 +144,8 @@ __device__ __forceinline__ void tell_nothing(const Rows &to, int32_t row)
 }
 
 // One workgroup decides and hands out.  A thread a sequence; one scan says what all of them want, and if rows and stack have it, that is
-// what they get; else two more say who goes without.  Then a thread an entry of the table, and, with `tell`, a thread a row.
+// what they get; else two more say who goes without.  Then a thread an entry of the table, and, with `tell`, a thread a row.  Where rows
+// stay as they were asked for (p.seen), those before a sequence come from its neighbour: sums that stay at kMany are no differences.
 __global__ __launch_bounds__(kTeam) void extend_kernel(const Pool p, Global<const int32_t> counts, Global<int32_t> q_starts,
                                                        Global<int32_t> granted, const Rows to, int32_t tell)
 {
@@ -150,22 +153,25 @@ __global__ __launch_bounds__(kTeam) void extend_kernel(const Pool p, Global<cons
     __shared__ int32_t held_of[kTeam], begin_of[kTeam], had[kTeam];
     const int i = threadIdx.x;
     const int32_t free = p.sequences > 0 ? within(p.free_count[0], p.pages) : 0;       // without sequences there need be no pages
-    uint32_t rows = 0, pages = 0, got_rows = 0;          // wanted by the sequences before these 1024, and got
+    const bool stay = p.seen.address != 0;
+    uint32_t rows = 0, pages = 0, got_rows = 0;          // wanted by the sequences before these 1024, and got (or, if they stay, had)
     int32_t taken = 0;
     for (int32_t b0 = 0; b0 < p.sequences; b0 += kTeam) {
         const int32_t b = b0 + i, here = p.sequences - b0 < kTeam ? p.sequences - b0 : kTeam;
+        const uint32_t first_row = got_rows;
         int32_t n = 0;
-        uint32_t want = 0;
+        uint32_t want = 0, asked = 0;
         if (b < p.sequences) {
             n = within(p.lengths[b], p.most);
             const int32_t count = counts[b];
             if (count > 0 && count <= p.most - n) want = (uint32_t)count;
+            asked = stay ? (uint32_t)within(count, (int32_t)kMany) : want < kMany ? want : kMany;
         }
         const int32_t held = pages_of(p, n);
         uint32_t need = (uint32_t)(pages_of(p, n + (int32_t)want) - held);
         Scan s[2];
-        scan<2>({want < kMany ? want : kMany, need}, s, parts);
-        uint32_t begin = got_rows + s[0].upto - want;                  // with all of them served
+        scan<2>({asked, need}, s, parts);
+        uint32_t begin = got_rows + s[0].upto - asked;                 // with all of them served
         const bool enough = rows == got_rows && pages == (uint32_t)taken && add(rows, s[0].all) <= (uint32_t)to.rows &&
                             add(pages, s[1].all) <= (uint32_t)free;
         if (enough) {
@@ -174,6 +180,12 @@ __global__ __launch_bounds__(kTeam) void extend_kernel(const Pool p, Global<cons
             taken = (int32_t)pages;
         } else {
             const uint32_t rows_upto = add(rows, s[0].upto);
+            uint32_t before = 0;
+            if (stay) {
+                from[i] = rows_upto;
+                __syncthreads();
+                before = i > 0 ? from[i - 1] : rows;
+            }
             rows = add(rows, s[0].all);
             if (rows_upto > (uint32_t)to.rows) want = need = 0;
             Scan some[1];
@@ -182,19 +194,20 @@ __global__ __launch_bounds__(kTeam) void extend_kernel(const Pool p, Global<cons
             pages = add(pages, some[0].all);
             if (need > 0 && pages_upto > (uint32_t)free) want = need = 0;
             scan<2>({want, need}, s, parts);
-            begin = got_rows + s[0].upto - want;
-            got_rows += s[0].all;
+            begin = stay ? umin(before, (uint32_t)to.rows) : got_rows + s[0].upto - want;
+            got_rows = stay ? umin(rows, (uint32_t)to.rows) : got_rows + s[0].all;
             taken += (int32_t)s[1].all;
         }
         if (b < p.sequences) {
             q_starts[b] = (int32_t)begin;
             p.lengths[b] = n + (int32_t)want;
             if (granted.address) granted[b] = (int32_t)want;
+            if (stay) p.seen[b] = asked > 0 && want == 0 ? 0 : n + (int32_t)want;
         }
         from[i] = s[1].upto - need;                     // of the entries that are handed out here
         held_of[i] = held;
         begin_of[i] = (int32_t)begin;
-        had[i] = n;
+        had[i] = want > 0 ? n : -1;
         // the first entry's page: those before are the sequences' before these
         const int32_t top = free - 1 - (taken - (int32_t)s[1].all);
         const uint32_t all = s[1].all;
@@ -205,9 +218,13 @@ __global__ __launch_bounds__(kTeam) void extend_kernel(const Pool p, Global<cons
         }
         __syncthreads();
         if (tell) {
-            for (uint32_t row = (uint32_t)(got_rows - s[0].all) + i; row < got_rows; row += kTeam) {
+            for (uint32_t row = first_row + i; row < got_rows; row += kTeam) {
                 const int32_t q = last_from(begin_of, here, row);
-                tell_row(p, to, (int32_t)row, b0 + q, begin_of[q], had[q]);
+                if (had[q] < 0) {
+                    tell_nothing(to, (int32_t)row);
+                } else {
+                    tell_row(p, to, (int32_t)row, b0 + q, begin_of[q], had[q]);
+                }
             }
             __syncthreads();
         }
@@ -239,8 +256,12 @@ __global__ __launch_bounds__(256) void tell_kernel(const Pool p, Global<const in
         return;
     }
     const int32_t b = fits ? last_from(starts, p.sequences, (uint32_t)row) : last_from((const int32_t *)q_starts, p.sequences, (uint32_t)row);
-    const int32_t begin = q_starts[b];
-    tell_row(p, to, row, b, begin, p.lengths[b] - (q_starts[b + 1] - begin));
+    const int32_t begin = q_starts[b], now = p.seen.address ? p.seen[b] : p.lengths[b];
+    if (now == 0) {
+        tell_nothing(to, row);
+        return;
+    }
+    tell_row(p, to, row, b, begin, now - (q_starts[b + 1] - begin));
 }
 
 }  // namespace pages

@@ -593,6 +593,7 @@ bool some_pages(PyObject *o, PyObject *page, equarx_pages &p)
     p.free_count = static_cast<int32_t *>(count.ptr);
     p.pages = free.count;
     p.page = (int32_t)size;
+    p.seen = nullptr;
     return true;
 }
 
@@ -605,11 +606,12 @@ int pages_trim(PyObject *const *a)
     return call(lib.equarx_pages_trim, &p, static_cast<const int32_t *>(keep.ptr));
 }
 
-int pages_extend(PyObject *const *a)
+// With `seen`, or without that argument.
+int pages_extend(PyObject *const *a, bool with_seen)
 {
     current_device = c10::hip::current_device();
     equarx_pages p;
-    Buffer counts, starts, slots, granted, positions, tags, row_tags;
+    Buffer counts, starts, slots, granted, positions, tags, row_tags, seen;
     if (!some_pages(a[0], a[1], p) || !exactly(counts, a[2], kInt, p.sequences) || !exactly(starts, a[3], kInt, (int64_t)p.sequences + 1))
         return kNotPlain;
     if (!slots.of(a[4], kLong) || !here(slots.t)) return kNotPlain;
@@ -617,6 +619,8 @@ int pages_extend(PyObject *const *a)
     if (a[6] != Py_None && !exactly(positions, a[6], kInt, slots.count)) return kNotPlain;
     if (a[7] != Py_None && !exactly(tags, a[7], kInt, p.sequences)) return kNotPlain;
     if (a[8] != Py_None && !exactly(row_tags, a[8], kInt, slots.count)) return kNotPlain;
+    if (with_seen && a[9] != Py_None && !exactly(seen, a[9], kInt, p.sequences)) return kNotPlain;
+    p.seen = static_cast<int32_t *>(seen.ptr);
     return call(lib.equarx_pages_extend, &p, static_cast<const int32_t *>(counts.ptr), static_cast<int32_t *>(starts.ptr),
                 static_cast<int64_t *>(slots.ptr), static_cast<int32_t *>(granted.ptr), static_cast<int32_t *>(positions.ptr),
                 static_cast<const int32_t *>(tags.ptr), static_cast<int32_t *>(row_tags.ptr), slots.count);
@@ -708,9 +712,13 @@ ENTRY(13, equarx_cache_attention, cache_attention(a))
 ENTRY(11, equarx_norm, norm(a))
 ENTRY(12, equarx_norm_reduced, norm_reduced(a))
 ENTRY(3, equarx_pages_trim, pages_trim(a))
-ENTRY(9, equarx_pages_extend, pages_extend(a))
 ENTRY(8, equarx_adapters, adapters(a))
 #undef ENTRY
+PyObject *py_equarx_pages_extend(PyObject *, PyObject *const *a, Py_ssize_t count)
+{
+    if (count == 10) return enter<10>(a, count, [](PyObject *const *a) { return pages_extend(a, true); });
+    return enter<9>(a, count, [](PyObject *const *a) { return pages_extend(a, false); });
+}
 
 // bind({name: address}): where the library's entry points are.
 PyObject *bind(PyObject *, PyObject *table)

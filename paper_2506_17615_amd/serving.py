@@ -132,19 +132,21 @@ def captured(step):
 class Requests:
     """Sequences in places of a page table on the device: what a step of them reads, made there by one launch or two.
 
-    rows: of a step, at most.  A step's q_starts, slots and row_tags are those of its first `rows` rows; rows behind the last sequence have slot -1 and
-    tag -1: nothing is kept in the cache for them, no adapter is theirs, and the layer adds nothing to them."""
+    rows: of a step, at most.  A step's q_starts, slots and row_tags are those of its first `rows` rows, counts[b] of sequence b after those of the
+    sequences before it.  Rows behind the last sequence, and of one that got none of the tokens it wanted (granted[b] is 0: no pages are
+    left, or no room), have slot -1 and tag -1: nothing is kept in the cache for them, no adapter is theirs, and the layer adds nothing to them."""
 
     def __init__(self, sequences, width, pages, page, rows):
         self.page, self.pages = page, eq.alloc_pages(sequences, width, pages)
         ints = lambda n, dtype=torch.int32: torch.zeros(n, dtype=dtype, device="cuda")
-        self.q_starts, self.granted, self.tags = ints(sequences + 1), ints(sequences), ints(sequences) - 1
+        self.q_starts, self.granted, self.seen, self.tags = ints(sequences + 1), ints(sequences), ints(sequences), ints(sequences) - 1
         self.slots, self.row_tags = ints(rows, torch.int64), ints(rows)
 
     def step(self, counts, rows):
-        """counts int32 [sequences] more tokens for every sequence, up to `rows` in all."""
-        eq.equarx_pages_extend(self.pages, self.page, counts, self.q_starts, self.slots[:rows], self.granted, None, self.tags, self.row_tags[:rows])
-        return dict(slots=self.slots[:rows], q_starts=self.q_starts, page_table=self.pages.table, lengths=self.pages.lengths), self.row_tags[:rows]
+        """counts int32 [sequences] more tokens for every sequence, up to `rows` in all: all that it wants, or none."""
+        eq.equarx_pages_extend(self.pages, self.page, counts, self.q_starts, self.slots[:rows], self.granted, None, self.tags, self.row_tags[:rows],
+                               self.seen)
+        return dict(slots=self.slots[:rows], q_starts=self.q_starts, page_table=self.pages.table, lengths=self.seen), self.row_tags[:rows]
 
     def keep(self, tokens):
         """Takes every sequence back to its first tokens[b] (0: it has ended)."""

@@ -2,6 +2,7 @@
 import pytest
 import torch
 
+import serving_ref as ref
 import test_serving_requests_gpu as layers
 from paper_2506_17615_amd import binding as eq
 from paper_2506_17615_amd import serving
@@ -59,3 +60,83 @@ def test_a_graph_forgets_what_the_last_step_left():
         torch.cuda.synchronize()
         assert torch.equal(stream[2:], before[2:]) and not torch.equal(stream[:2], before[:2])
         assert stream.isfinite().all() and out[:8].isfinite().all()
+
+
+def _check_caches(layer, before, x, seqs):
+    """The caches hold what they held, and in the tokens' slots the keys and values of the sequences' own rows: seqs has (row, count, slots)."""
+    nq, nk = layer.heads * layer.dim, layer.kv_heads * layer.dim
+    slots = torch.full((x.shape[0],), -1)
+    for row, count, at in seqs:
+        slots[row:row + count] = at
+    for p, cache in enumerate(layer.caches):
+        _, k, v = (t.unflatten(1, (-1, layer.dim)) for t in layer.qkv[p, :x.shape[0]].split([nq, nk, nk], dim=1))
+        want = eq.Cache(*(t.clone() for t in before[p]))
+        eq.equarx_cache_write(want, k, v, slots.cuda())
+        assert all(torch.equal(a, b) for a, b in zip(want, cache))
+
+
+def test_a_refused_sequence_moves_no_other():
+    """A captured decode step whose pages run out: every sequence's row stays its own, with its own slot, adapter and attention, and the refused one's
+    residual stays as it is."""
+    sequences, pages, lengths = 4, 4, [5, 16, 3, 9]
+    layer, whole, bf16 = layers._layer(40, sequences, pages, 3 * PAGE)
+    requests = serving.Requests(sequences, 3, pages, PAGE, 40)
+    tags = [2, 0, -1, 1]
+    requests.tags.copy_(_on(tags))
+    weight, stream = 1 + bf16(HIDDEN), 3 * bf16(40, HIDDEN)
+    x, out = bf16(40, HIDDEN), torch.empty_like(stream)
+    step, ids = requests.step(_on(lengths), 40)
+    layer.normed(x, **step, max_queries=16, residual=stream, weight=weight, out=out, ids=ids)
+    assert requests.granted.tolist() == lengths and not int(requests.pages.free_count)
+
+    one = _on([1] * sequences)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step, ids = requests.step(one, sequences)
+        layer.normed(x[:4], **step, max_queries=1, residual=stream[:4], weight=weight, out=out[:4], ids=ids)
+
+    def replay(refused, bad):
+        x.copy_(10 * bf16(40, HIDDEN))
+        if bad:                                                         # what a row holds that nobody asks for
+            x[refused] = float("nan")
+        before, caches = stream.clone(), [[t.clone() for t in c] for c in layer.caches]
+        graph.replay()
+        torch.cuda.synchronize()
+        served = [b for b in range(sequences) if b != refused]
+        for b in served:
+            lengths[b] += 1
+        assert requests.granted.tolist() == [int(b != refused) for b in range(sequences)]
+        assert requests.pages.lengths.tolist() == lengths and requests.q_starts.tolist() == [0, 1, 2, 3, 4]
+        table = requests.pages.table.cpu()
+        slot = [int(table[b, (lengths[b] - 1) // PAGE]) * PAGE + (lengths[b] - 1) % PAGE for b in range(sequences)]
+        assert requests.slots[:4].tolist() == [-1 if b == refused else slot[b] for b in range(sequences)]
+        assert requests.row_tags[:4].tolist() == [-1 if b == refused else tags[b] for b in range(sequences)]
+        _check_caches(layer, caches, x[:4], [(b, 1, torch.tensor([slot[b]])) for b in served])
+        assert not layer.attended[:, refused].any()
+        assert torch.equal(stream[refused], before[refused]) and out[refused].isfinite().all()
+        for p in range(layer.shards):
+            _check_attention(layer, p, table, lengths, served)
+        if not bad:
+            layers._check_step(layer, whole, x[:4], requests.row_tags[:4], 4)
+            layers._check_norm(layer, before[:4], stream[:4], weight, out[:4], 4)
+
+    for bad in (False, True, False):
+        replay(1, bad)                                                  # its seventeenth token would need a page
+    requests.keep(_on([100, 100, 100, 0]))                              # the last one ends and begins anew: the second, before it, has its page
+    lengths[3] = 0
+    for bad in (True, False):
+        replay(3, bad)
+
+
+def _check_attention(layer, p, table, lengths, served):
+    """The attended rows of the last step against 64-bit arithmetic over what the cache holds."""
+    r = ref.CacheRef(layer.caches[p].k_codes.shape[0], layer.kv_heads, PAGE, layer.dim, 64)
+    kc, ks, vc, vs = (t.cpu() for t in layer.caches[p])
+    r.codes = [kc.permute(0, 2, 1, 3).reshape(r.codes[0].shape), vc.permute(0, 2, 4, 1, 3).reshape(r.codes[1].shape)]
+    r.scales = [t.permute(0, 3, 1, 2).reshape(r.scales[0].shape) for t in (ks, vs)]
+    for b in served:
+        q = layer.qkv[p, b:b + 1, :layer.heads * layer.dim].reshape(1, layer.heads, layer.dim).double().cpu()
+        want, _, mass, size = ref.attention(r, q, table[b].tolist(), lengths[b], layer.dim ** -0.5, True, 0)
+        e = (layer.dim + 8) * 2.0 ** -23 * size + 2.0 ** -20 + (lengths[b] + 64) * 2.0 ** -23
+        bound = 2.0 ** -8 * want.abs() + (2.0 ** -15 + 2.02 * e[..., None]) * mass
+        assert ((layer.attended[p, b:b + 1].double().cpu() - want).abs() <= bound).all(), (p, b)
