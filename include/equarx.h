@@ -658,7 +658,8 @@ int equarx_pages_extend(const equarx_pages *pages, const int32_t *counts, int32_
  *   (EQUARX_BAD_SHAPE).  K == 0 changes nothing.
  *   workspace          device, equarx_adapters_workspace_bytes(...) bytes, 256-byte aligned (may be NULL where
  *                      that is 0); nothing in it needs clearing.  Never less for fewer rows.
- * Sums are fp32; t meets B as a sum of two bf16, to 2^-16.  The order of a row's sums depends on
+ * Sums are fp32; t, times a factor that is below one in magnitude, meets B as a sum of two bf16, to 2^-16; a factor from one on
+ * is multiplied to the sums, in the addition to out.  The order of a row's sums depends on
  * the sizes alone: not on its place, its neighbours or their adapters.  Rows of one adapter are brought together
  * wherever they are.  No output may overlap another buffer of the call (EQUARX_BAD_SHAPE).
  */

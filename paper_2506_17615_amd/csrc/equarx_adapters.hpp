@@ -383,11 +383,14 @@ template <int S>
 constexpr int kColumn = S * 64 + 16;
 constexpr int kResult = 64 * 4 + 16;
 
+constexpr float kMostBf16 = 0x1.fep127f;
+
 // A wave's sixteen rows of an item.
 template <int S, bool kNarrow, bool kStreams>
 struct SixteenRows {
     int lane = threadIdx.x & 63, l = lane & 15, g = lane >> 4, in = lane / 8, eighth = lane % 8;
     int32_t count, N;
+    float after;                // what of the factor the sums are multiplied by
     uint16_t *row[2];
     u32x4 t[2 * S];
     struct Before {
@@ -427,9 +430,14 @@ struct SixteenRows {
             }
     }
 
-    // The rows' t of slice s times the factor: lane l has row l % 16, eight entries of each step.
+    // The rows' t of slice s: lane l has row l % 16, eight entries of each step.  A factor below one is multiplied to t, where sums of B t might
+    // pass fp32's range and their product with it not; another to the sums (`after`), where its product with t might.  The larger half of t is
+    // bf16's largest where rounding would make it infinite, and the smaller one the rest: of an infinity an infinity, of a NaN a NaN.
     __device__ __forceinline__ void join(const Expansion &p, int s, float factor)
     {
+        const bool below = __builtin_fabsf(factor) < 1.0f;
+        const float ahead = below ? factor : 1.0f;
+        after = below ? 1.0f : factor;
         const int32_t R = p.slices * p.rank;
         const float *const from = p.t + (int64_t)mine * R + s * p.rank;
         // in order, and several asked for together: one after the other is a latency each
@@ -470,9 +478,11 @@ struct SixteenRows {
         for (int q = 0; q < S; ++q) {
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                const v4f f = q * 32 + g * 8 < p.rank ? v[q][h] * factor : v4f{0, 0, 0, 0};
-                const u32x2 high = {narrow_bf16x2(f[0], f[1]), narrow_bf16x2(f[2], f[3])};
+                const v4f f = q * 32 + g * 8 < p.rank ? v[q][h] * ahead : v4f{0, 0, 0, 0};
                 float w[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) w[i] = __builtin_amdgcn_fmed3f(f[i], -kMostBf16, kMostBf16);
+                const u32x2 high = {narrow_bf16x2(w[0], w[1]), narrow_bf16x2(w[2], w[3])};
                 widen_bf16x4(high, w);
                 const u32x2 low = {narrow_bf16x2(f[0] - w[0], f[1] - w[1]), narrow_bf16x2(f[2] - w[2], f[3] - w[3])};
                 t[q][2 * h] = high.x;
@@ -514,7 +524,8 @@ struct SixteenRows {
             widen_bf16x8(kNarrow || n + 8 <= N ? before.v[half] : drop_elements(before.v[half], n + 8 - N), f);
             u32x4 v;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] = narrow_bf16x2(f[2 * i] + d[i / 2][i % 2 * 2], f[2 * i + 1] + d[i / 2][i % 2 * 2 + 1]);
+            for (int i = 0; i < 4; ++i)
+                v[i] = narrow_bf16x2(__builtin_fmaf(d[i / 2][i % 2 * 2], after, f[2 * i]), __builtin_fmaf(d[i / 2][i % 2 * 2 + 1], after, f[2 * i + 1]));
             if (n0 + 64 <= n_end) {                             // all of the wave's columns
                 auto *const to = reinterpret_cast<u32x4_anywhere *>(row[half] + n);
                 if (half * 8 + in < count) {
