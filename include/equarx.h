@@ -614,7 +614,7 @@ size_t equarx_cache_attention_most_workspace_bytes(int32_t heads, int32_t dim, i
  * equarx_cache_attention: 0 if it wanted tokens and got none, so that its rows see nothing and become zeros, else lengths[b].
  *
  *   q_starts   int32 [sequences + 1]: rows of the step before each sequence's and, last,
- *              of all (with seen, `rows` at most);
+ *              of all (with seen, `rows` at most); may be NULL without sequences and rows;
  *   granted    int32 [sequences] or NULL: the tokens that it got;
  *   slots      int64 [rows]: where row r's token goes; -1 for rows of no sequence;
  *   positions  int32 [rows] or NULL: its place in its sequence, or -1;

@@ -72,7 +72,7 @@ int equarx_pages_extend(const equarx_pages *pages, const int32_t *counts, int32_
     LaunchCtx ctx(stream);
     if (int st = check_pages(pages)) return st;
     if (rows < 0 || rows > kMostRows) return EQUARX_BAD_SHAPE;
-    if (pages->sequences == 0 && rows == 0) return EQUARX_OK;
+    if (pages->sequences == 0 && rows == 0 && !q_starts) return EQUARX_OK;
     if (!q_starts || (pages->sequences > 0 && !counts) || (rows > 0 && !slots)) return EQUARX_NULL_POINTER;
     if (rows > 0 && pages->sequences > 0 && !tags != !row_tags) return EQUARX_NULL_POINTER;
     if (misaligned(pages->seen, 4) || misaligned(counts, 4) || misaligned(q_starts, 4) || misaligned(slots, 8) || misaligned(granted, 4) || misaligned(positions, 4) ||
