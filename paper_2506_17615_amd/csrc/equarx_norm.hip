@@ -254,6 +254,7 @@ int equarx_norm_reduced(const void *const *partials_bf16, int32_t P, int32_t blo
     if (P < 1 || P > EQUARX_MAX_PARTIALS || rows < 0 || cols < 0 || rows > kMostRows || cols > kMostCols || cols % block != 0)
         return EQUARX_BAD_SHAPE;
     if (rows == 0 || cols == 0) return EQUARX_OK;
+    if (int st = check_rows(rows, cols, cols)) return st;
     if (!partials_bf16) return EQUARX_NULL_POINTER;
     Aliasing mem;
     PartialTable tab;
