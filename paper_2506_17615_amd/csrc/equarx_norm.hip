@@ -91,7 +91,7 @@ void advance(Inputs &in, Outputs &to, int64_t at, int64_t cols)
 
 // From so many elements on bf16 outputs are written past the caches, which would not hold them for the next call as they would a decode
 // step's.  Measured on MI355X, us with ordinary stores -> past the caches: 4096 x 5376 32.1 -> 29.2, 16384 x 1024 23.1 -> 20.4, 1024 x 5376
-// 9.6 -> 9.1, 65536 x 128 8.4 -> 8.1.
+// 9.6 -> 9.1.  Rows that are not read through a descriptor have ordinary stores.
 constexpr int64_t kStreamFrom = (int64_t)4 << 20;
 
 template <int L_, int K_, int A_ = 1>
@@ -237,7 +237,8 @@ int equarx_norm(const void *x_bf16, int64_t x_stride, void *residual_bf16, int64
             Inputs i = in;
             Outputs o = to;
             advance(i, o, at, cols);
-            ctx.launch(!whole ? rows_kernel<L, K, false, false> : rows * cols < kStreamFrom ? rows_kernel<L, K, true, false> : rows_kernel<L, K, true, true>,
+            constexpr bool kMayStream = by_descriptor<L, true>;
+            ctx.launch(!whole ? rows_kernel<L, K, false, false> : rows * cols < kStreamFrom ? rows_kernel<L, K, true, false> : rows_kernel<L, K, true, kMayStream>,
                        workgroups<L>(count), Place<L>::T,
                        static_cast<const uint16_t *>(x_bf16) + at * x_stride, x_stride, count, cols, i, o);
         });
