@@ -29,7 +29,9 @@
  *     WRITES (an output, the workspace, a kept wire) may not overlap any other
  *     buffer of the call, not even partly -- EQUARX_BAD_SHAPE -- except where
  *     an entry point says that an output may BE an input; the two must then
- *     coincide exactly.  Buffers that are only read may overlap freely.
+ *     coincide exactly.  Buffers that are only read may overlap freely.  A
+ *     tensor with a stride counts as all bytes from its first element to its
+ *     last: two column ranges of one tensor overlap.
  *   - The library keeps no state between calls (the one exception, the static
  *     array of equarx_reduce_quantized_static, is described there) and may be
  *     called from several threads at once (on different streams, or on one).
@@ -376,8 +378,8 @@ int equarx_reduce_variant_hops_strided(const void *const *partials_bf16, int32_t
  *   h = bf16(x + residual), stored to residual (without a residual h = x)
  *   y = fl32(fl32(h * i) * g),  i = fl32(1 / sqrt(mean over the row of h^2 + eps)),
  *   g = weight, fl32(1 + weight) with EQUARX_NORM_ONE_PLUS, or 1 without a weight.
- * The mean is taken in 64 bits: results do not depend on how a row is divided.  y
- * goes to any of three outputs, rounded once for each:
+ * The sum is taken in 64 bits, in an order that depends on rows and cols: it reaches
+ * i's last bit in one row of about 10^8.  y goes to any of three outputs, rounded once for each:
  *   out_bf16              bf16, row i at out_bf16 + i * out_stride;
  *   codes, scales         the form of equarx_quantize, blocks of `block` elements
  *                         (EQUARX_BAD_BLOCK) that divide a row (EQUARX_BAD_SHAPE):

@@ -277,7 +277,7 @@ __global__ __launch_bounds__(Place<L>::T) void rows_kernel(Global<const uint16_t
 // The chain of chain_kernel over a row's blocks, B / 8 lanes each, whole blocks a row; its last dequantization is rounded to
 // bf16, as equarx_reduce_fused writes it, and is the row that is normed.
 
-// A: partials that are asked for together; of one at a time they are many, and read past the caches.  kWhole: of residual and output; the
+// A: partials that are asked for together.  One at a time where rows are many (hence past the caches), short, or of any stride.  kWhole: of residual and output; the
 // partials and the weight always are.
 template <int B, int L, int K, int A, bool kWhole, bool kStreams>
 __global__ __launch_bounds__(Place<L>::T) void reduced_kernel(int P, int64_t rows, int64_t cols, const Inputs in, const Outputs to,
