@@ -140,3 +140,25 @@ def _check_attention(layer, p, table, lengths, served):
         e = (layer.dim + 8) * 2.0 ** -23 * size + 2.0 ** -20 + (lengths[b] + 64) * 2.0 ** -23
         bound = 2.0 ** -8 * want.abs() + (2.0 ** -15 + 2.02 * e[..., None]) * mass
         assert ((layer.attended[p, b:b + 1].double().cpu() - want).abs() <= bound).all(), (p, b)
+
+
+@pytest.mark.parametrize("long", (300, 40))
+def test_prompts_that_get_nothing_keep_nothing(long):
+    """One that the pages have no room for, and one that ends behind the last row."""
+    layer, _, bf16 = layers._layer(400, 4, 4, 25 * PAGE)
+    requests = serving.Requests(4, 25, 4, PAGE, 400)
+    requests.tags.copy_(_on([1, 2, 0, 1]))
+    weight, before = 1 + bf16(HIDDEN), 3 * bf16(400, HIDDEN)
+    x, out, stream = bf16(400, HIDDEN), torch.empty_like(before), before.clone()
+    x[24:] = float("nan")
+    rows = 24 + long + 76
+    caches = [[t.clone() for t in c] for c in layer.caches]
+    step, ids = requests.step(_on([19, 5, long, 200]), rows)
+    layer.attended.fill_(float("nan"))
+    layer.normed(x[:rows], **step, max_queries=300, residual=stream[:rows], weight=weight, out=out[:rows], ids=ids)
+    assert requests.granted.tolist() == [19, 5, 0, 0] and requests.q_starts.tolist() == [0, 19, 24, 24 + long, rows]
+    assert step["lengths"].tolist() == [19, 5, 0, 0] and requests.pages.lengths.tolist() == [19, 5, 0, 0]
+    assert (step["slots"][24:] == -1).all() and (ids[24:] == -1).all()
+    _check_caches(layer, caches, x[:rows], [(0, 24, step["slots"][:24].cpu())])
+    assert not layer.attended[:, 24:rows].any() and torch.equal(stream[24:], before[24:])
+    assert stream.isfinite().all() and out[:rows].isfinite().all() and not torch.equal(stream[:24], before[:24])
